@@ -376,6 +376,151 @@ dbw_status dbw_profile_enable(dbw_ctx* ctx, int32_t mode);
 dbw_status dbw_kernel_time(dbw_ctx* ctx, int32_t group, double* total_ms, int64_t* launches);
 dbw_status dbw_profile_reset(dbw_ctx* ctx);
 
+/* ---------------------------------------------------------------------------
+ * Operators for language models: what a simulation whose workers hold ragged
+ * minibatches of tokens, and whose parameters are a language model's, needs
+ * beside the calls above.  A layer with weights W_i [d][C] maps T token rows,
+ * sorted by group, to T rows of C values; a group is a worker with its own
+ * minibatch, or an expert.  The worker gradients G [n][d][C] of these calls
+ * are what dbw_aggregate_fastest and dbw_grad_stats_static take.
+ *
+ * The calls need no context.  They run on `stream` (a hipStream_t, NULL for
+ * the default stream) of the current device, allocate nothing, and can be
+ * captured into a HIP graph.  offsets (DEVICE int32 [n+1], non-decreasing, in
+ * [0, T]) give the rows offsets[i] .. offsets[i+1]-1 of group i; a group may
+ * be empty.  Rows before offsets[0] and from offsets[n] on belong to no group:
+ * they are not read, and rows of an output there are left as they were.
+ * (Offsets that break these rules never lead outside the arrays: each is
+ * taken as the nearest allowed value; the results are then unspecified.)
+ * Errors: DBW_EINVAL, DBW_EUNSUPPORTED, DBW_EHIP; dbw_last_error(NULL) then
+ * gives the text, per calling thread. */
+typedef enum { DBW_F32 = 0, DBW_BF16 = 1, DBW_F16 = 2 } dbw_dtype;
+
+/* Products of ragged groups:
+ *   FORWARD      Y[t]  = X[t] W_i         (a = X, b = W, out = Y  [T][C])
+ *   INPUT_GRAD   dX[t] = dY[t] W_i^T      (a = dY, b = W, out = dX [T][d])
+ *   WEIGHT_GRAD  G_i = sum_t X[t]^T dY[t] (a = X, b = dY, out = G [n][d][C];
+ *                zero for an empty group)
+ * for the rows t of group i.  Inputs are bf16 or fp16 (dtype), the output is
+ * of their type or fp32 (out_dtype); sums are held in fp32 and rounded once.
+ * ld_d and ld_C are the row strides, in elements, of the arrays [T][d] (X or
+ * dX) and [T][C] (Y or dY), ld_W that of every W_i or G_i (>= C), and st_W the
+ * distance of W_{i+1} from W_i.  st_W = 0, for FORWARD and INPUT_GRAD only,
+ * gives all groups the same W.  Every stride and pointer that is a multiple
+ * of 16 bytes, with d and C multiples of 8, makes the loads wide; others are
+ * slower.  NaN and infinities of one group's rows never reach another's. */
+typedef enum { DBW_GROUP_FORWARD = 0, DBW_GROUP_INPUT_GRAD = 1, DBW_GROUP_WEIGHT_GRAD = 2 } dbw_group_form;
+typedef struct {
+  int32_t form;      /* dbw_group_form                                       */
+  int32_t dtype;     /* DBW_BF16 or DBW_F16                                  */
+  int32_t out_dtype; /* dtype or DBW_F32                                     */
+  int32_t n;         /* groups, in [1, DBW_MAX_N]                            */
+  int32_t d, C;      /* in [1, 2^20]                                         */
+  int64_t T;         /* rows, in [0, 2^31)                                   */
+  int64_t ld_d, ld_C, ld_W; /* row strides, below 2^21                       */
+  int64_t st_W;
+} dbw_group_shape;
+
+/* Bytes of workspace that dbw_group_product needs for a shape (HOST out; 0
+ * where the work is not split over a long sum).  Needs no device. */
+dbw_status dbw_group_workspace(const dbw_group_shape* shape, int64_t* bytes);
+
+/* One product.  offsets, a, b, out and workspace are DEVICE; out must not
+ * overlap the inputs, and rows (or G_i) of out must not overlap each other.
+ * workspace holds at least dbw_group_workspace bytes, 16-byte aligned (NULL
+ * where that is 0); its contents need no clearing and are used up when the
+ * call is done: calls that may run at the same time need their own. */
+dbw_status dbw_group_product(const dbw_group_shape* shape, const int32_t* offsets, const void* a, const void* b,
+                             void* out, void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Mean cross entropy of each worker's tokens, and its gradient.  Z (DEVICE
+ * [T][C] of dtype, row stride ld_Z elements) are logits, y (DEVICE int32 [T])
+ * labels; a negative label masks its row (padding, prompt tokens): its logits
+ * are not read, it adds nothing and its gradient is zero.  With count_i the
+ * rows of worker i that are not masked:
+ *   loss[i] = (1/count_i) sum_t (log sum_c exp Z[t][c] - Z[t][y_t])
+ *                                          (DEVICE float [n]; 0 if count_i = 0)
+ *   dZ[t][c] = (scale/count_i) (softmax(Z[t])_c - [c = y_t])
+ * dZ (DEVICE, of dtype, row stride ld_dZ) may be NULL (no gradient) or Z
+ * itself.  Sums are held in fp32, a worker's over its rows in fp64 in a fixed
+ * order.  Logits of -infinity have probability 0; a row with a NaN, a
+ * +infinity or only -infinities, and a row whose label is >= C, give a NaN
+ * loss and a NaN gradient row.  scale must be finite.  n in [1, DBW_MAX_N],
+ * C in [1, 2^24], T below 2^31.  workspace (DEVICE, 16-byte aligned, at least
+ * dbw_token_workspace bytes): as for dbw_group_product. */
+int64_t dbw_token_workspace(int32_t n, int64_t T);
+dbw_status dbw_token_loss(int32_t n, int64_t T, int32_t C, int32_t dtype, const int32_t* offsets, const void* Z,
+                          int64_t ld_Z, const int32_t* y, double scale, void* dZ, int64_t ld_dZ, float* loss,
+                          void* workspace, int64_t workspace_bytes, void* stream);
+
+/* AdamW over many tensors at once (the server's update of such a model).  One
+ * step over all tensors, with t the number of steps made, this one included:
+ *   norm = |grad_scale| sqrt(sum g^2) over all tensors,
+ *   f    = grad_scale, times max_norm / norm where 0 < max_norm < norm,
+ *   m <- beta1 m + (1 - beta1) f g,     v <- beta2 v + (1 - beta2) (f g)^2,
+ *   w <- (1 - lr decay) w - lr m / (1 - beta1^t) / (sqrt(v / (1 - beta2^t)) + eps)
+ * with a tensor's lr = hyper.lr * lr_scale and decay = weight_decay.  With
+ * max_norm > 0, a norm that is not finite leaves everything as it was, t
+ * included.  w is fp32; w_low (nullable) gets a copy rounded to low_dtype.
+ *
+ * state_bits = 32: m and v are float [count].  state_bits = 8: m holds m, and
+ * v holds r = sqrt(v), as e4m3 codes (uint8 [count]) times a power of two for
+ * each 256 values from the tensor's start, m_scale and v_scale (uint8
+ * [ceil(count/256)], the biased exponent e of 2^(e-127)).  The scale puts the
+ * largest finite magnitude of the 256, or 2^-118 if that is more, into (224,
+ * 448].  A value between two codes takes the upper with the probability of its
+ * place between them, by 16 bits of a mix of seed, t, tensor and index (see
+ * dbw_adamw_bits), so that m and r keep their mean although a step's change
+ * is far below a code; an r above 0 never becomes 0 (m/r stays bounded).
+ * Values that are not finite become NaN codes.  The update itself uses m and
+ * v before they are rounded. */
+typedef struct {
+  float* w;         /* DEVICE [count]                                        */
+  const void* g;    /* DEVICE [count] of g_dtype                             */
+  void *m, *v;      /* DEVICE [count]                                        */
+  uint8_t *m_scale, *v_scale; /* DEVICE; NULL with 32-bit states             */
+  void* w_low;      /* DEVICE [count] of low_dtype, or NULL                  */
+  int64_t count;    /* >= 0                                                  */
+  double lr_scale, weight_decay; /* finite, >= 0                             */
+} dbw_adamw_tensor;
+typedef struct {
+  int32_t state_bits; /* 8 or 32                                             */
+  int32_t g_dtype;    /* dbw_dtype of every g                                */
+  int32_t low_dtype;  /* DBW_BF16 or DBW_F16, of every w_low                 */
+  int32_t tensors;    /* in [1, 65536]                                       */
+  int64_t t;          /* steps made so far, >= 0                             */
+} dbw_adamw_config;
+typedef struct {
+  double lr, beta1, beta2, eps; /* lr >= 0, betas in [0, 1), eps >= 1e-30    */
+  double grad_scale;            /* finite                                    */
+  double max_norm;              /* 0: no clipping                            */
+  uint32_t seed;
+} dbw_adamw_hyper;
+typedef struct dbw_adamw dbw_adamw;
+
+/* A plan for these tensors on the current device: their addresses and t are
+ * kept on the device until dbw_adamw_destroy.  Tensors must not overlap each
+ * other; each pointer is aligned to its elements. */
+dbw_status dbw_adamw_create(const dbw_adamw_config* cfg, const dbw_adamw_tensor* tensors, dbw_adamw** out);
+void dbw_adamw_destroy(dbw_adamw* opt);
+
+/* One step on `stream` of the plan's device (allocates nothing; t lives on
+ * the device, so a captured step advances it at every replay).  norm, if not
+ * NULL, is DEVICE float [1] and gets the norm before clipping.  Steps of one
+ * plan must not run at the same time. */
+dbw_status dbw_adamw_step(dbw_adamw* opt, const dbw_adamw_hyper* hyper, float* norm, void* stream);
+
+/* t of a plan (checkpoint and resume; both wait for the plan's device). */
+dbw_status dbw_adamw_export(dbw_adamw* opt, int64_t* t);
+dbw_status dbw_adamw_import(dbw_adamw* opt, int64_t t);
+
+/* The 32 random bits of value `index` of tensor `tensor` at step t (HOST; the
+ * low 16 round m, the high 16 round r).  With mix(x): x ^= x >> 16, x *=
+ * 0x9E3779B1, x ^= x >> 15, x *= 0xB7E15163, x ^= x >> 16 in 32 bits, they are
+ * mix(lo * 0x6A09E667 + hi * 0xBB67AE85 + mix(mix(mix(seed) + t) + tensor))
+ * for the halves lo and hi of index. */
+uint32_t dbw_adamw_bits(uint32_t seed, int64_t t, int32_t tensor, int64_t index);
+
 #ifdef __cplusplus
 }
 #endif

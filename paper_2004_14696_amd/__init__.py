@@ -6,11 +6,13 @@ statistics, the DBW choice of k and the SGD update, all in hand-written HIP
 kernels for gfx950 behind the C ABI of ``include/dbw.h``.  This package is
 the Python binding of that library.
 """
-from .binding import (DBW_MLP, DBW_SOFTMAX, Config, Context, DBWError, grads_route, load_library,  # noqa: F401
-                      make_config, param_count, time_estimate)
+from .binding import (DBW_MLP, DBW_SOFTMAX, AdamW, Config, Context, DBWError, adamw_states,  # noqa: F401
+                      grads_route, group_input_grad, group_matmul, group_weight_grad, load_library, make_config,
+                      param_count, time_estimate, token_loss)
 
-__all__ = ["Config", "Context", "DBWError", "grads_route", "load_library", "make_config", "param_count",
-           "time_estimate", "DBW_SOFTMAX", "DBW_MLP", "config_from"]
+__all__ = ["AdamW", "Config", "Context", "DBWError", "adamw_states", "grads_route", "group_input_grad",
+           "group_matmul", "group_weight_grad", "load_library", "make_config", "param_count", "time_estimate",
+           "token_loss", "DBW_SOFTMAX", "DBW_MLP", "config_from"]
 
 
 def config_from(wl, S: int = 0) -> Config:

@@ -10,7 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import POINTER, c_double, c_int32, c_int64, c_size_t, c_uint8, c_void_p
+from ctypes import POINTER, c_double, c_int32, c_int64, c_size_t, c_uint8, c_uint32, c_void_p
 
 import numpy as np
 
@@ -26,6 +26,9 @@ DBW_G_ROWS_ALL, DBW_G_ROWS_SELECTED, DBW_G_ROWS_NONE = 0, 1, 2
 DBW_MAX_N, DBW_MAX_D = 1024, 64
 DBW_KT_GRADS, DBW_KT_AGGREGATE, DBW_KT_CHOOSE, DBW_KT_HOST_ESTIMATE, DBW_KT_HOST_STEP = 0, 1, 2, 3, 4
 DBW_KT_HOST_WAIT, DBW_KT_HOST_QUEUE = 5, 6
+DBW_F32, DBW_BF16, DBW_F16 = 0, 1, 2
+DBW_GROUP_FORWARD, DBW_GROUP_INPUT_GRAD, DBW_GROUP_WEIGHT_GRAD = 0, 1, 2
+ADAMW_BLOCK = 256   # values of one scale of the 8-bit states
 
 STATUS_NAMES = {0: "DBW_OK", -1: "DBW_EINVAL", -2: "DBW_ERANGE", -3: "DBW_EHIP",
                 -4: "DBW_ESTATE", -5: "DBW_EUNSUPPORTED"}
@@ -38,6 +41,9 @@ EXPORTED = (
     "dbw_profile_reset", "dbw_time_estimator_create", "dbw_time_estimator_destroy",
     "dbw_time_estimator_solve", "dbw_time_estimator_stats", "dbw_busy_export", "dbw_busy_import",
     "dbw_grad_stats_static", "dbw_grads_route",
+    "dbw_group_workspace", "dbw_group_product", "dbw_token_workspace", "dbw_token_loss",
+    "dbw_adamw_create", "dbw_adamw_destroy", "dbw_adamw_step", "dbw_adamw_export", "dbw_adamw_import",
+    "dbw_adamw_bits",
 )
 DBW_STATIC_SCRATCH_BYTES = 8 * 1024 * 1024
 
@@ -69,6 +75,28 @@ class EstimatorState(ctypes.Structure):
 class StepBuffers(ctypes.Structure):
     _fields_ = [(name, c_void_p) for name in
                 ("G", "loss", "g", "mask", "sqnorm", "stats", "T_hat", "objective", "k", "b")]
+
+
+class GroupShape(ctypes.Structure):
+    _fields_ = [("form", c_int32), ("dtype", c_int32), ("out_dtype", c_int32), ("n", c_int32), ("d", c_int32),
+                ("C", c_int32), ("T", c_int64), ("ld_d", c_int64), ("ld_C", c_int64), ("ld_W", c_int64),
+                ("st_W", c_int64)]
+
+
+class AdamWTensor(ctypes.Structure):
+    _fields_ = [("w", c_void_p), ("g", c_void_p), ("m", c_void_p), ("v", c_void_p), ("m_scale", c_void_p),
+                ("v_scale", c_void_p), ("w_low", c_void_p), ("count", c_int64), ("lr_scale", c_double),
+                ("weight_decay", c_double)]
+
+
+class AdamWConfig(ctypes.Structure):
+    _fields_ = [("state_bits", c_int32), ("g_dtype", c_int32), ("low_dtype", c_int32), ("tensors", c_int32),
+                ("t", c_int64)]
+
+
+class AdamWHyper(ctypes.Structure):
+    _fields_ = [("lr", c_double), ("beta1", c_double), ("beta2", c_double), ("eps", c_double),
+                ("grad_scale", c_double), ("max_norm", c_double), ("seed", c_uint32)]
 
 
 _lib = None
@@ -146,6 +174,27 @@ def load_library(path: str = LIB_PATH):
     lib.dbw_profile_reset.restype = st
     lib.dbw_grad_stats_static.argtypes = [c_int32, c_int64, P, P, c_int32, P, P, c_double, P, P, P]
     lib.dbw_grad_stats_static.restype = st
+    lib.dbw_group_workspace.argtypes = [POINTER(GroupShape), POINTER(c_int64)]
+    lib.dbw_group_workspace.restype = st
+    lib.dbw_group_product.argtypes = [POINTER(GroupShape), P, P, P, P, P, c_int64, P]
+    lib.dbw_group_product.restype = st
+    lib.dbw_token_workspace.argtypes = [c_int32, c_int64]
+    lib.dbw_token_workspace.restype = c_int64
+    lib.dbw_token_loss.argtypes = [c_int32, c_int64, c_int32, c_int32, P, P, c_int64, P, c_double, P, c_int64, P, P,
+                                   c_int64, P]
+    lib.dbw_token_loss.restype = st
+    lib.dbw_adamw_create.argtypes = [POINTER(AdamWConfig), POINTER(AdamWTensor), POINTER(P)]
+    lib.dbw_adamw_create.restype = st
+    lib.dbw_adamw_destroy.argtypes = [P]
+    lib.dbw_adamw_destroy.restype = None
+    lib.dbw_adamw_step.argtypes = [P, POINTER(AdamWHyper), P, P]
+    lib.dbw_adamw_step.restype = st
+    lib.dbw_adamw_export.argtypes = [P, POINTER(c_int64)]
+    lib.dbw_adamw_export.restype = st
+    lib.dbw_adamw_import.argtypes = [P, c_int64]
+    lib.dbw_adamw_import.restype = st
+    lib.dbw_adamw_bits.argtypes = [c_uint32, c_int64, c_int32, c_int64]
+    lib.dbw_adamw_bits.restype = c_uint32
     _lib = lib
     return lib
 
@@ -277,6 +326,296 @@ def grad_stats_static(G, mask, k, g, loss, V_window=0.0, sqnorm=None, stats=None
     if s != DBW_OK:
         raise DBWError(s, lib.dbw_last_error(None).decode())
     return sqnorm, stats
+
+
+# -- operators for language models ---------------------------------------------
+def _dtype_code(torch, dtype, name, allowed):
+    codes = {torch.float32: DBW_F32, torch.bfloat16: DBW_BF16, torch.float16: DBW_F16}
+    if dtype not in codes or codes[dtype] not in allowed:
+        raise ValueError(f"{name} has an unsupported type: {dtype}")
+    return codes[dtype]
+
+
+def _rows_of(t, shape, dtype, dev, name):
+    """Pointer and row stride of a tensor [..][rows][columns] with contiguous
+    columns."""
+    if t.device != dev or t.dtype != dtype or tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be {dtype} {tuple(shape)} on {dev}, not {t.dtype} {tuple(t.shape)} on {t.device}")
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"the last dimension of {name} must be contiguous")
+    # a single row has no stride of its own
+    return t.data_ptr(), t.stride(-2) if t.shape[-2] > 1 else t.shape[-1]
+
+
+def _flat(t, shape, dtype, dev, name):
+    if t.device != dev or t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {dev}")
+    return t.data_ptr()
+
+
+class _On:
+    """The device of a call's tensors made current, and its stream."""
+
+    def __init__(self, torch, dev, stream):
+        if dev.type != "cuda":
+            raise ValueError(f"tensors must live on a GPU, not {dev}")
+        self.switch = torch.cuda.device(dev) if torch.cuda.current_device() != dev.index else None
+        self.stream = torch.cuda.current_stream(dev) if stream is None else stream
+
+    def __enter__(self):
+        if self.switch is not None:
+            self.switch.__enter__()
+        return self.stream
+
+    def __exit__(self, *exc):
+        if self.switch is not None:
+            self.switch.__exit__(*exc)
+
+
+def _workspace(torch, nbytes, dev, workspace):
+    if workspace is None:
+        return torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
+    if workspace.device != dev or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be a contiguous tensor on {dev}")
+    return workspace
+
+
+def _group(form, a, b, offsets, out, out_dtype, W_shape, workspace, stream):
+    torch = _torch()
+    lib = load_library()
+    dev = a.device
+    if offsets.dim() != 1 or offsets.numel() < 2:
+        raise ValueError("offsets must be [n + 1]")
+    n = offsets.numel() - 1
+    po = _flat(offsets, (n + 1,), torch.int32, dev, "offsets")
+    if a.dim() != 2:
+        raise ValueError("token rows must be [T][columns]")
+    T = a.shape[0]
+    if out_dtype is None:
+        out_dtype = a.dtype if out is None else out.dtype
+    d, C = W_shape
+    names = {DBW_GROUP_FORWARD: ("X", "W", "Y"), DBW_GROUP_INPUT_GRAD: ("dY", "W", "dX"),
+             DBW_GROUP_WEIGHT_GRAD: ("X", "dY", "G")}[form]
+    s = GroupShape(form=form, dtype=_dtype_code(torch, a.dtype, names[0], (DBW_BF16, DBW_F16)),
+                   out_dtype=_dtype_code(torch, out_dtype, "the output", (DBW_F32, DBW_BF16, DBW_F16)),
+                   n=n, d=d, C=C, T=T)
+    if form == DBW_GROUP_WEIGHT_GRAD:
+        out = torch.empty((n, d, C), dtype=out_dtype, device=dev) if out is None else out
+        pa, s.ld_d = _rows_of(a, (T, d), a.dtype, dev, "X")
+        pb, s.ld_C = _rows_of(b, (T, C), a.dtype, dev, "dY")
+        pc, s.ld_W = _rows_of(out, (n, d, C), out_dtype, dev, "G")
+        s.st_W = out.stride(0)
+    else:
+        K, N = (d, C) if form == DBW_GROUP_FORWARD else (C, d)
+        out = torch.empty((T, N), dtype=out_dtype, device=dev) if out is None else out
+        pa, lda = _rows_of(a, (T, K), a.dtype, dev, names[0])
+        pb, s.ld_W = _rows_of(b, (n, d, C) if b.dim() == 3 else (d, C), a.dtype, dev, "W")
+        pc, ldo = _rows_of(out, (T, N), out_dtype, dev, names[2])
+        s.ld_d, s.ld_C = (lda, ldo) if form == DBW_GROUP_FORWARD else (ldo, lda)
+        # one matrix for all groups has no distance to the next one
+        s.st_W = b.stride(0) if b.dim() == 3 else 0
+        if b.dim() == 3 and n == 1:
+            s.st_W = 0
+    with _On(torch, dev, stream) as on:
+        need = c_int64()
+        st = lib.dbw_group_workspace(ctypes.byref(s), ctypes.byref(need))
+        if st != DBW_OK:
+            raise DBWError(st, lib.dbw_last_error(None).decode())
+        ws = _workspace(torch, need.value, dev, workspace)
+        st = lib.dbw_group_product(ctypes.byref(s), po, pa, pb, pc, ws.data_ptr() if ws is not None else None,
+                                   ws.numel() * ws.element_size() if ws is not None else 0, on.cuda_stream)
+    if st != DBW_OK:
+        raise DBWError(st, lib.dbw_last_error(None).decode())
+    return out
+
+
+def group_matmul(X, W, offsets, out=None, out_dtype=None, workspace=None, stream=None):
+    """Y[t] = X[t] W_i for the rows t = offsets[i] .. offsets[i+1]-1 of each
+    group i (dbw_group_product, FORWARD).  X [T][d] bf16 or fp16, W [n][d][C], or
+    [d][C] for all groups, offsets [n+1] int32; rows may be strided.  Returns
+    Y [T][C] in ``out_dtype`` (that of X, or float32); rows of no group keep
+    what ``out`` held."""
+    if W.dim() not in (2, 3):
+        raise ValueError("W must be [n][d][C] or [d][C]")
+    return _group(DBW_GROUP_FORWARD, X, W, offsets, out, out_dtype, tuple(W.shape[-2:]), workspace, stream)
+
+
+def group_input_grad(dY, W, offsets, out=None, out_dtype=None, workspace=None, stream=None):
+    """dX[t] = dY[t] W_i^T: the gradient of group_matmul to its rows
+    (dbw_group_product, INPUT_GRAD).  Returns dX [T][d]."""
+    if W.dim() not in (2, 3):
+        raise ValueError("W must be [n][d][C] or [d][C]")
+    return _group(DBW_GROUP_INPUT_GRAD, dY, W, offsets, out, out_dtype, tuple(W.shape[-2:]), workspace, stream)
+
+
+def group_weight_grad(X, dY, offsets, out=None, out_dtype=None, workspace=None, stream=None):
+    """G_i = sum over the rows t of group i of X[t]^T dY[t]: the gradient of
+    group_matmul to its weights, or the worker gradients of workers with
+    ragged minibatches (dbw_group_product, WEIGHT_GRAD).  Returns G [n][d][C]
+    in ``out_dtype`` (float32 unless given)."""
+    if dY.dim() != 2 or X.dim() != 2:
+        raise ValueError("X must be [T][d] and dY [T][C]")
+    torch = _torch()
+    if out_dtype is None:
+        out_dtype = torch.float32 if out is None else out.dtype
+    return _group(DBW_GROUP_WEIGHT_GRAD, X, dY, offsets, out, out_dtype, (X.shape[1], dY.shape[1]), workspace, stream)
+
+
+def token_loss(Z, y, offsets, scale=1.0, dZ=None, loss=None, grad=True, workspace=None, stream=None):
+    """Mean cross entropy of each worker's tokens and its gradient
+    (dbw_token_loss).  Z [T][C] float32, bfloat16 or float16 logits, y [T] int32
+    labels (negative: the row is masked), offsets [n+1] int32.  Returns
+    (loss [n] float32, dZ [T][C] of the type of Z, times ``scale``); dZ may be
+    Z, to write the gradient in its place; ``grad`` False: no gradient (None)."""
+    torch = _torch()
+    lib = load_library()
+    dev = Z.device
+    if Z.dim() != 2 or offsets.dim() != 1 or offsets.numel() < 2:
+        raise ValueError("Z must be [T][C] and offsets [n + 1]")
+    T, C = Z.shape
+    n = offsets.numel() - 1
+    code = _dtype_code(torch, Z.dtype, "Z", (DBW_F32, DBW_BF16, DBW_F16))
+    po = _flat(offsets, (n + 1,), torch.int32, dev, "offsets")
+    py = _flat(y, (T,), torch.int32, dev, "y")
+    pz, ld_Z = _rows_of(Z, (T, C), Z.dtype, dev, "Z")
+    if dZ is None and grad:
+        dZ = torch.empty((T, C), dtype=Z.dtype, device=dev)
+    pd, ld_dZ = _rows_of(dZ, (T, C), Z.dtype, dev, "dZ") if dZ is not None else (None, 0)
+    loss = torch.empty(n, dtype=torch.float32, device=dev) if loss is None else loss
+    pl = _flat(loss, (n,), torch.float32, dev, "loss")
+    with _On(torch, dev, stream) as on:
+        need = lib.dbw_token_workspace(n, T)
+        ws = _workspace(torch, max(need, 0), dev, workspace)
+        st = lib.dbw_token_loss(n, T, C, code, po, pz, ld_Z, py, float(scale), pd, ld_dZ, pl,
+                                ws.data_ptr() if ws is not None else None,
+                                ws.numel() * ws.element_size() if ws is not None else 0, on.cuda_stream)
+    if st != DBW_OK:
+        raise DBWError(st, lib.dbw_last_error(None).decode())
+    return loss, dZ
+
+
+def adamw_states(w, bits=32):
+    """Zero states of AdamW for the tensors ``w``: keyword arguments m, v (and
+    m_scale, v_scale with 8 bits)."""
+    torch = _torch()
+    if bits == 32:
+        return {"m": [torch.zeros_like(t) for t in w], "v": [torch.zeros_like(t) for t in w]}
+    if bits != 8:
+        raise ValueError("states have 8 or 32 bits")
+    codes = lambda: [torch.zeros(t.shape, dtype=torch.uint8, device=t.device).view(torch.float8_e4m3fn) for t in w]  # noqa: E731
+    scales = lambda: [torch.ones(-(-t.numel() // ADAMW_BLOCK), dtype=torch.uint8, device=t.device)                   # noqa: E731
+                      .view(torch.float8_e8m0fnu) for t in w]
+    return {"m": codes(), "v": codes(), "m_scale": scales(), "v_scale": scales()}
+
+
+class AdamW:
+    """AdamW over a list of tensors (dbw_adamw_*), updated in place.
+
+    w float32 tensors, g their gradients (all of one type: float32, bfloat16 or
+    float16), m and v their states: float32, or float8_e4m3fn codes with
+    m_scale and v_scale, one float8_e8m0fnu for each 256 values (adamw_states
+    makes either).  low: bfloat16 or float16 copies of w, written by every step.
+    weight_decay and lr_scale: a number, or one for each tensor.  step: steps
+    made before.  The tensors' memory is kept, so gradients are written into
+    the same g before every step."""
+
+    def __init__(self, w, g, m, v, m_scale=None, v_scale=None, low=None, weight_decay=0.0, lr_scale=1.0, step=0):
+        torch = _torch()
+        self.lib = load_library()
+        self.h = None
+        w, g, m, v = list(w), list(g), list(m), list(v)
+        n = len(w)
+        if n == 0:
+            raise ValueError("no tensors")
+        bits = 32 if m_scale is None and v_scale is None else 8
+        lists = {"g": g, "m": m, "v": v}
+        if bits == 8:
+            if m_scale is None or v_scale is None:
+                raise ValueError("8-bit states need m_scale and v_scale")
+            m_scale, v_scale = list(m_scale), list(v_scale)
+            lists |= {"m_scale": m_scale, "v_scale": v_scale}
+        if low is not None:
+            low = list(low)
+            lists["low"] = low
+        per = lambda x: list(x) if isinstance(x, (list, tuple)) else [x] * n   # noqa: E731
+        decay, scale = per(weight_decay), per(lr_scale)
+        for name, x in {**lists, "weight_decay": decay, "lr_scale": scale}.items():
+            if len(x) != n:
+                raise ValueError(f"{name} must have one entry for each of the {n} tensors")
+        dev = w[0].device
+        state = torch.float32 if bits == 32 else torch.float8_e4m3fn
+        table = (AdamWTensor * n)()
+        low_type = low[0].dtype if low is not None else torch.bfloat16
+        cfg = AdamWConfig(state_bits=bits, tensors=n, t=int(step),
+                          g_dtype=_dtype_code(torch, g[0].dtype, "g", (DBW_F32, DBW_BF16, DBW_F16)),
+                          low_dtype=_dtype_code(torch, low_type, "low", (DBW_BF16, DBW_F16)))
+        for i, t in enumerate(table):
+            shape = w[i].shape
+            t.count = w[i].numel()
+            blocks = (-(-t.count // ADAMW_BLOCK),)
+            t.w = _flat(w[i], shape, torch.float32, dev, f"w[{i}]")
+            t.g = _flat(g[i], shape, g[0].dtype, dev, f"g[{i}]")
+            t.m = _flat(m[i], shape, state, dev, f"m[{i}]")
+            t.v = _flat(v[i], shape, state, dev, f"v[{i}]")
+            if bits == 8:
+                t.m_scale = _flat(m_scale[i], blocks, torch.float8_e8m0fnu, dev, f"m_scale[{i}]")
+                t.v_scale = _flat(v_scale[i], blocks, torch.float8_e8m0fnu, dev, f"v_scale[{i}]")
+            if low is not None:
+                t.w_low = _flat(low[i], shape, low_type, dev, f"low[{i}]")
+            t.lr_scale, t.weight_decay = float(scale[i]), float(decay[i])
+        self.device = dev
+        self._keep = (w, lists)      # the plan holds their addresses
+        handle = c_void_p()
+        with _On(torch, dev, None):
+            st = self.lib.dbw_adamw_create(ctypes.byref(cfg), table, ctypes.byref(handle))
+        if st != DBW_OK:
+            raise DBWError(st, self.lib.dbw_last_error(None).decode())
+        self.h = handle
+
+    def step(self, lr, beta1=0.9, beta2=0.999, eps=1e-8, max_norm=0.0, grad_scale=1.0, seed=0, norm=None, stream=None):
+        """One step.  grad_scale multiplies the gradients; max_norm > 0 clips
+        their norm (over all tensors).  Returns the norm before clipping, a
+        float32 scalar tensor, where max_norm or ``norm`` (a tensor to write
+        it to) is given, else None."""
+        torch = _torch()
+        if norm is None and max_norm:
+            norm = torch.empty((), dtype=torch.float32, device=self.device)
+        pn = _flat(norm, norm.shape, torch.float32, self.device, "norm") if norm is not None else None
+        if norm is not None and norm.numel() != 1:
+            raise ValueError("norm must have one element")
+        hyper = AdamWHyper(lr=lr, beta1=beta1, beta2=beta2, eps=eps, grad_scale=grad_scale, max_norm=max_norm,
+                           seed=int(seed) & 0xFFFFFFFF)
+        with _On(torch, self.device, stream) as on:
+            st = self.lib.dbw_adamw_step(self.h, ctypes.byref(hyper), pn, on.cuda_stream)
+        if st != DBW_OK:
+            raise DBWError(st, self.lib.dbw_last_error(None).decode())
+        return norm
+
+    @property
+    def t(self) -> int:
+        """Steps made (waits for the device)."""
+        out = c_int64()
+        st = self.lib.dbw_adamw_export(self.h, ctypes.byref(out))
+        if st != DBW_OK:
+            raise DBWError(st, self.lib.dbw_last_error(None).decode())
+        return out.value
+
+    @t.setter
+    def t(self, value: int):
+        st = self.lib.dbw_adamw_import(self.h, int(value))
+        if st != DBW_OK:
+            raise DBWError(st, self.lib.dbw_last_error(None).decode())
+
+    def close(self):
+        if self.h is not None:
+            self.lib.dbw_adamw_destroy(self.h)
+            self.h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
 
 
 # ---------------------------------------------------------------------------

@@ -22,7 +22,7 @@ BUILD_DIR = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libdbw.so")
 
 SOURCES = ["dbw_api.cpp", "time_estimate.cpp", "k_ps.hip", "k_softmax.hip", "k_mlp.hip", "k_cnn.hip",
-           "dbw_static.hip"]
+           "dbw_static.hip", "lm_api.cpp", "k_group.hip", "k_token.hip", "k_adamw.hip"]
 ARCH = "gfx950"
 COMMON = [
     "-O3", "-std=c++17", f"--offload-arch={ARCH}", "-fPIC", "-fvisibility=hidden",
