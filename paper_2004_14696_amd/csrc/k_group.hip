@@ -1,25 +1,21 @@
 // Products of ragged groups on the matrix cores: Y[t] = X[t] W_i,
 // dX[t] = dY[t] W_i^T and G_i = sum over the rows of a group of X[t]^T dY[t].
 //
-// One kernel computes a tile of BM x BN outputs, 64 terms of the sum a step.
+// One kernel computes a tile of BM x BN outputs, BK terms of the sum a step.
 // An operand is either contiguous along the sum (X, dY, and W in dX) or along
-// the output (W in Y, both operands of G): the first is kept in LDS as rows of
-// 64 terms and read 16 bytes a lane, the second as it lies in memory, one row
-// a term, and read with the transposing LDS load, so nothing is transposed
-// beforehand.  Rows of another group, and what lies behind an edge, are
-// replaced by zeros on the way into registers, in both operands: NaN and
-// infinities there reach no sum.
+// the output (W in Y, both operands of G): the first is kept in LDS as lines
+// of BK terms and read 16 bytes a lane, the second as it lies in memory, one
+// line a term, and read with the transposing LDS load, so nothing is
+// transposed beforehand.  Rows of another group, and what lies behind an edge,
+// are zeros in LDS, in both operands: NaN and infinities there reach no sum.
 //
-// Steps are pipelined: the loads of the next one are in flight while the
-// present one is multiplied, and go from registers to the other LDS buffer
-// after it, with one barrier a step.
+// Steps are pipelined: while one is multiplied, the loads of the next STAGES -
+// 1 are in flight, straight into LDS, with one barrier a step.
 //
 // v_mfma_f32_16x16x32 takes, in lane l = 16 g + c, row c and terms 8 g .. 8 g
 // + 7 of each operand; its result r of a lane is row 4 g + r of the first
 // operand, row c of the second.  The output's columns go in as the first
-// operand, and tile j of four stands for the columns 16 (c / 4) + 4 j + c % 4
-// of 64, so that a lane ends up with 16 consecutive columns of one output row
-// and stores 16 bytes at a time.
+// operand, so a lane has four consecutive columns of one output row.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -30,8 +26,6 @@
 
 namespace dbw {
 namespace {
-
-constexpr int BK = 64;   // terms of the sum a step
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -58,129 +52,217 @@ struct Tile {
 };
 
 // One operand's part of a step: L outputs x BK terms, by THREADS threads.
-// SWAP: contiguous along the output.  WIDE: whole 16-byte chunks everywhere.
-template <typename E, int L, int THREADS, bool SWAP, bool WIDE>
+// SWAP: contiguous along the output, kept as it lies in memory, a line of L
+// outputs for each term; else a line of BK terms for each output.
+template <typename E, int L, int BK, int THREADS, bool SWAP>
 struct Operand {
-  static constexpr int CHUNKS = L * BK / 8 / THREADS;   // 16-byte chunks a thread
-  static constexpr int LINE = SWAP ? L / 8 : BK / 8;    // chunks of a line in memory
-  static_assert(L * BK / 8 % THREADS == 0 && THREADS % LINE == 0, "whole chunks a thread");
+  static constexpr int CHUNKS = L * BK / 8 / THREADS;   // chunks of 16 bytes a thread
+  static constexpr int LINE = (SWAP ? L : BK) / 8;      // chunks of a line
   static constexpr int STEP = THREADS / LINE;           // lines between a thread's chunks
   static constexpr int BYTES = L * BK * 2;
+  static_assert(L * BK / 8 % THREADS == 0 && THREADS % LINE == 0, "whole chunks a thread");
+  static_assert(BK == 64 || BK == 32, "turn() is for lines of eight or four chunks");
 
-  lm_u32x4 held[CHUNKS];
+  // A line's chunks are turned by its number, so that the lanes that read
+  // together meet in no bank: rows of 16 bytes at 16 outputs, or 8 bytes of
+  // four terms r = 0..3 of two of the four groups of eight terms.
+  static __device__ __forceinline__ int turn(int line) {
+    if (SWAP) return (line & 3) << 1 | (L >= 128 ? ((line >> 3) & 1) << 3 : 0);
+    return LINE == 8 ? line & 7 : (line >> 1) & 3;
+  }
 
-  // Rows of 64 terms: the chunk of 8 terms is moved by its row, so that the
-  // lanes of a fragment (rows 4 a + b of tiles, see below) meet in no bank.
-  static __device__ __forceinline__ int turn(int row) { return (row & 3) | (((row >> 2) ^ (row >> 4)) & 1) << 2; }
+  // Line and chunk (of memory) that thread tid's chunk i of a stage holds.
+  static __device__ __forceinline__ int line(int tid, int i) { return tid / LINE + i * STEP; }
+  static __device__ __forceinline__ int chunk(int tid, int i) { return tid % LINE ^ turn(line(tid, i)); }
 
-  __device__ __forceinline__ void load(const E* p, int64_t ld, int64_t k, int64_t k1, int length, int tid) {
-    const int line = tid / LINE, chunk = tid % LINE;
-    const E* base = SWAP ? p + k * ld : p + k;
-    const int64_t left = k1 - k;                         // terms from k on
-    if (WIDE) {
-      const __amdgpu_buffer_rsrc_t r = make_rsrc(base, static_cast<uint32_t>(kMaxBufferBytes));
+  // Byte offset in memory of chunk i from the first term of a step with `left`
+  // terms, or one behind every buffer: such loads give 0.
+  static __device__ __forceinline__ uint32_t offset(int64_t ld, int64_t left, int length, int tid, int i) {
+    const int at = line(tid, i), first = chunk(tid, i) * 8;
+    const bool in = SWAP ? at < left && first < length : at < length && first < left;
+    return in ? static_cast<uint32_t>((at * ld + first) * 2) : kOutOfRange;
+  }
+
+  // Fragments of a lane: terms 32 kk + 8 g .. + 7 of outputs first + 16 i + c.
+  template <int N>
+  static __device__ __forceinline__ void fragments(const char* lds, int first, int kk, int lane, lm_u32x4 (&f)[N]) {
+    const int c = lane % 16, g = lane / 16;
+    if constexpr (SWAP) {
+      // a transposing load takes, for each 16 lanes, four terms of 16 outputs:
+      // lane 4 r + q gives the address of term r, outputs 4 q .. 4 q + 3, and
+      // lane c gets the terms of output c; another takes the next four terms
+      // (whose lines are turned alike)
+      const int r = c / 4, q = c % 4, at = kk * 32 + g * 8 + r;
+      typedef __attribute__((address_space(3))) const char* P;
+      uint32_t p[N];
 #pragma unroll
-      for (int i = 0; i < CHUNKS; ++i) {
-        const int at = line + i * STEP;
-        const bool in = SWAP ? at < left && chunk * 8 < length : at < length && chunk * 8 < left;
-        const uint32_t off = in ? static_cast<uint32_t>((at * ld + chunk * 8) * 2) : kOutOfRange;
-        held[i] = __builtin_bit_cast(lm_u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, 0));
-      }
+      for (int i = 0; i < N; ++i)
+        p[i] = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(
+            (P)(lds + at * (L * 2) + (((first + 16 * i) / 8 + q / 2) ^ turn(at)) * 16 + q % 2 * 8)));
+      lm_u32x2 x[N][2];
+      read_turned(p, x);
+#pragma unroll
+      for (int i = 0; i < N; ++i) f[i] = lm_u32x4{x[i][0][0], x[i][0][1], x[i][1][0], x[i][1][1]};
     } else {
 #pragma unroll
-      for (int i = 0; i < CHUNKS; ++i) {
-        const int at = line + i * STEP;
-        const int64_t lines = SWAP ? left : length, in_line = (SWAP ? length : left) - chunk * 8;
-        lm_u32x4 v = {0, 0, 0, 0};
-        if (at < lines && in_line > 0) {
-          const E* q = base + at * ld + chunk * 8;
-          if (in_line >= 8) {
-            v = *reinterpret_cast<const lm_u32x4_any*>(q);
-          } else {
-            typedef E V __attribute__((ext_vector_type(8)));
-            V x = __builtin_bit_cast(V, v);
-#pragma unroll
-            for (int j = 0; j < 7; ++j)
-              if (j < in_line) x[j] = q[j];
-            v = __builtin_bit_cast(lm_u32x4, x);
-          }
-        }
-        held[i] = v;
+      for (int i = 0; i < N; ++i) {
+        const int row = first + 16 * i + c;
+        f[i] = *reinterpret_cast<const lm_u32x4*>(lds + row * (BK * 2) + ((kk * 4 + g) ^ turn(row)) * 16);
       }
     }
   }
 
-  __device__ __forceinline__ void store(char* lds, int tid) const {
-    const int line = tid / LINE, chunk = tid % LINE;
-#pragma unroll
-    for (int i = 0; i < CHUNKS; ++i) {
-      const int at = line + i * STEP;
-      if (SWAP) {
-        // pieces of four columns, piece ^ (at & 3), and 32 columns apart every
-        // other eight lines: the lines 8 g + r that the transposing load
-        // takes at once meet in no bank
-        const int c = chunk ^ ((at >> 1) & 1) ^ (L >= 128 ? ((at >> 3) & 1) << 3 : 0);
-        const lm_u32x4 v = held[i];
-        const lm_u32x4 w = {v[2], v[3], v[0], v[1]};
-        *reinterpret_cast<lm_u32x4*>(lds + at * (L * 2) + c * 16) = at & 1 ? w : v;
-      } else {
-        *reinterpret_cast<lm_u32x4*>(lds + at * (BK * 2) + (chunk ^ turn(at)) * 16) = held[i];
-      }
-    }
+  // The transposing loads of N tiles, and the wait for them, in one statement:
+  // as builtins, the compiler would first wait for every load on its way to LDS.
+  static __device__ __forceinline__ void read_turned(const uint32_t (&p)[4], lm_u32x2 (&x)[4][2]) {
+    asm volatile(
+        "ds_read_b64_tr_b16 %0, %8\n\tds_read_b64_tr_b16 %1, %8 offset:%12\n\t"
+        "ds_read_b64_tr_b16 %2, %9\n\tds_read_b64_tr_b16 %3, %9 offset:%12\n\t"
+        "ds_read_b64_tr_b16 %4, %10\n\tds_read_b64_tr_b16 %5, %10 offset:%12\n\t"
+        "ds_read_b64_tr_b16 %6, %11\n\tds_read_b64_tr_b16 %7, %11 offset:%12\n\t"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(x[0][0]), "=&v"(x[0][1]), "=&v"(x[1][0]), "=&v"(x[1][1]), "=&v"(x[2][0]), "=&v"(x[2][1]),
+          "=&v"(x[3][0]), "=&v"(x[3][1])
+        : "v"(p[0]), "v"(p[1]), "v"(p[2]), "v"(p[3]), "n"(4 * L * 2)
+        : "memory");
   }
-
-  // Fragment of a lane: terms 32 kk + 8 g .. + 7 of output `first` + (row c
-  // of tile j).  PERM: tile j of each 64 outputs takes 16 (c / 4) + 4 j + c % 4.
-  template <bool PERM>
-  static __device__ __forceinline__ lm_u32x4 fragment(const char* lds, int first, int tile, int kk, int lane) {
-    const int c = lane % 16, g = lane / 16;
-    const int base = PERM ? first + tile / 4 * 64 : first + tile * 16, j = tile % 4;
-    if (SWAP) {
-      const int r = c / 4, at = kk * 32 + g * 8 + r;     // and at + 4: the same low bits
-      const int piece = PERM ? base / 4 + 4 * (c % 4) + j : base / 4 + c % 4;
-      const int p = (piece ^ r) ^ (L >= 128 ? (g & 1) << 4 : 0);
-      const char* q = lds + at * (L * 2) + p * 8;
-      typedef __attribute__((address_space(3))) s16x4* P;
-      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(q));
-      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(q + 4 * L * 2));
-      const lm_u32x2 x = __builtin_bit_cast(lm_u32x2, lo), y = __builtin_bit_cast(lm_u32x2, hi);
-      return lm_u32x4{x[0], x[1], y[0], y[1]};
-    }
-    const int row = PERM ? base + 16 * (c / 4) + 4 * j + c % 4 : base + c;
-    return *reinterpret_cast<const lm_u32x4*>(lds + row * (BK * 2) + ((kk * 4 + g) ^ turn(row)) * 16);
+  static __device__ __forceinline__ void read_turned(const uint32_t (&p)[8], lm_u32x2 (&x)[8][2]) {
+    asm volatile(
+        "ds_read_b64_tr_b16 %0, %16\n\tds_read_b64_tr_b16 %1, %16 offset:%24\n\t"
+        "ds_read_b64_tr_b16 %2, %17\n\tds_read_b64_tr_b16 %3, %17 offset:%24\n\t"
+        "ds_read_b64_tr_b16 %4, %18\n\tds_read_b64_tr_b16 %5, %18 offset:%24\n\t"
+        "ds_read_b64_tr_b16 %6, %19\n\tds_read_b64_tr_b16 %7, %19 offset:%24\n\t"
+        "ds_read_b64_tr_b16 %8, %20\n\tds_read_b64_tr_b16 %9, %20 offset:%24\n\t"
+        "ds_read_b64_tr_b16 %10, %21\n\tds_read_b64_tr_b16 %11, %21 offset:%24\n\t"
+        "ds_read_b64_tr_b16 %12, %22\n\tds_read_b64_tr_b16 %13, %22 offset:%24\n\t"
+        "ds_read_b64_tr_b16 %14, %23\n\tds_read_b64_tr_b16 %15, %23 offset:%24\n\t"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(x[0][0]), "=&v"(x[0][1]), "=&v"(x[1][0]), "=&v"(x[1][1]), "=&v"(x[2][0]), "=&v"(x[2][1]),
+          "=&v"(x[3][0]), "=&v"(x[3][1]), "=&v"(x[4][0]), "=&v"(x[4][1]), "=&v"(x[5][0]), "=&v"(x[5][1]),
+          "=&v"(x[6][0]), "=&v"(x[6][1]), "=&v"(x[7][0]), "=&v"(x[7][1])
+        : "v"(p[0]), "v"(p[1]), "v"(p[2]), "v"(p[3]), "v"(p[4]), "v"(p[5]), "v"(p[6]), "v"(p[7]), "n"(4 * L * 2)
+        : "memory");
   }
 };
 
-// 16 consecutive outputs of one row, `left` of them inside.
-template <typename E>
-__device__ __forceinline__ void store16(E* p, const float (&x)[16], int left) {
-  constexpr int N = 16 / sizeof(E);
-  typedef E V __attribute__((ext_vector_type(16 / sizeof(E))));
+// 16 bytes a lane from r + off to the wave's 1 KiB at `to`.
+__device__ __forceinline__ void load_lds(__amdgpu_buffer_rsrc_t r, char* to, uint32_t off) {
+  typedef __attribute__((address_space(3))) void* P;
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (P)to, 16, off, 0, 0, 0);
+}
+
+// Loads of a step straight into LDS: a wave's instruction fills 1 KiB, lane by
+// lane.  Needs whole chunks: every line of memory starts and ends at one.
+template <typename Op, typename E>
+struct Direct {
+  uint32_t off[Op::CHUNKS];
+  __device__ __forceinline__ void start(int64_t ld, int length, int tid) {
 #pragma unroll
-  for (int q = 0; q < 16 / N; ++q) {
-    V v;
+    for (int i = 0; i < Op::CHUNKS; ++i) off[i] = Op::offset(ld, int64_t{1} << 32, length, tid, i);
+  }
+  // (also of steps behind the last one: zeros, so that every stage counts the same)
+  template <bool SWAP>
+  __device__ __forceinline__ void load(const E* p, int64_t ld, int64_t k, int64_t k1, int length, int bk, char* lds,
+                                       int tid) const {
+    const int64_t left = k1 - k;
+    const __amdgpu_buffer_rsrc_t r = make_rsrc(SWAP ? p + k * ld : p + k, static_cast<uint32_t>(kMaxBufferBytes));
+    char* to = lds + tid / 64 * 1024;
+    constexpr int WAVES = Op::STEP * Op::LINE / 64;
+    if (left >= bk) {
 #pragma unroll
-    for (int j = 0; j < N; ++j) v[j] = static_cast<E>(x[q * N + j]);
-    if (left >= (q + 1) * N) {
-      *reinterpret_cast<lm_u32x4_any*>(p + q * N) = __builtin_bit_cast(lm_u32x4, v);
+      for (int i = 0; i < Op::CHUNKS; ++i)
+        load_lds(r, to + i * WAVES * 1024, off[i]);
     } else {
 #pragma unroll
-      for (int j = 0; j < N; ++j)
-        if (q * N + j < left) p[q * N + j] = v[j];
+      for (int i = 0; i < Op::CHUNKS; ++i)
+        load_lds(r, to + i * WAVES * 1024, Op::offset(ld, left, length, tid, i));
     }
+  }
+};
+
+// Loads of a step through registers, for lines at any address and of any
+// length.
+template <typename Op, typename E, int BK>
+struct Staged {
+  lm_u32x4 held[Op::CHUNKS];
+  template <bool SWAP>
+  __device__ __forceinline__ void load(const E* p, int64_t ld, int64_t k, int64_t k1, int length, int tid) {
+    const E* base = SWAP ? p + k * ld : p + k;
+    const int64_t left = k1 - k;
+    const __amdgpu_buffer_rsrc_t r = make_rsrc(base, static_cast<uint32_t>(kMaxBufferBytes));
+    // whole chunks in one load each, at any alignment, without a branch
+#pragma unroll
+    for (int i = 0; i < Op::CHUNKS; ++i) {
+      const int at = Op::line(tid, i), first = Op::chunk(tid, i) * 8;
+      const bool whole = at < (SWAP ? left : length) && first + 8 <= (SWAP ? length : left);
+      held[i] = __builtin_bit_cast(lm_u32x4, __builtin_amdgcn_raw_buffer_load_b128(
+                                                 r, whole ? static_cast<uint32_t>((at * ld + first) * 2) : kOutOfRange, 0, 0));
+    }
+    // and those that a line ends in, value by value
+    if ((SWAP ? length : left) < (SWAP ? Op::LINE * 8 : BK)) {
+#pragma unroll
+      for (int i = 0; i < Op::CHUNKS; ++i) {
+        const int at = Op::line(tid, i), first = Op::chunk(tid, i) * 8;
+        const int64_t in_line = (SWAP ? length : left) - first;
+        if (at < (SWAP ? left : length) && in_line > 0 && in_line < 8) {
+          const E* q = base + at * ld + first;
+          typedef E V __attribute__((ext_vector_type(8)));
+          V x = __builtin_bit_cast(V, lm_u32x4{0, 0, 0, 0});
+#pragma unroll
+          for (int j = 0; j < 7; ++j)
+            if (j < in_line) x[j] = q[j];
+          held[i] = __builtin_bit_cast(lm_u32x4, x);
+        }
+      }
+    }
+  }
+  __device__ __forceinline__ void store(char* lds, int tid) const {
+#pragma unroll
+    for (int i = 0; i < Op::CHUNKS; ++i)
+      *reinterpret_cast<lm_u32x4*>(lds + (i * Op::STEP * Op::LINE + tid) * 16) = held[i];
+  }
+};
+
+// Waits until at most `loads` of this wave's loads are outstanding and all its
+// LDS reads are done, then for the other waves.
+template <int loads>
+__device__ __forceinline__ void wait_step() {
+  static_assert(loads < 64, "six bits");
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt((loads & 15) | 7 << 4 | 0 << 8 | (loads >> 4) << 14);
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+template <typename E>
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+  typedef float F __attribute__((ext_vector_type(2)));
+  typedef E V __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(F{a, b}, V));
+}
+
+// N consecutive outputs of one row, `left` of them inside.
+template <typename O, int N>
+__device__ __forceinline__ void store_out(O* p, const lm_u32x4& v, int left) {
+  if (left >= N) {
+    *reinterpret_cast<lm_u32x4_any*>(p) = v;
+  } else {
+    typedef O V __attribute__((ext_vector_type(N)));
+    const V x = __builtin_bit_cast(V, v);
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+      if (j < left) p[j] = x[j];
   }
 }
 
-template <typename E, int BM, int BN, int WM, int WN, bool A_SWAP, bool B_SWAP, bool WIDE>
+template <typename E, int BM, int BN, int WM, int WN, int BK, int STAGES, bool A_SWAP, bool B_SWAP, bool WIDE>
 __device__ __forceinline__ void product(const Tile& t, bool out_f32, char* lds) {
   constexpr int THREADS = (BM / WM) * (BN / WN) * 64;
   constexpr int TM = WM / 16, TN = WN / 16;
-  constexpr bool PERM = WM % 64 == 0;
-  static_assert(WN % 64 == 0, "a lane's columns are those of four tiles");
-  typedef Operand<E, BM, THREADS, A_SWAP, WIDE> OpA;
-  typedef Operand<E, BN, THREADS, B_SWAP, WIDE> OpB;
+  typedef Operand<E, BM, BK, THREADS, A_SWAP> OpA;
+  typedef Operand<E, BN, BK, THREADS, B_SWAP> OpB;
   constexpr int STAGE = OpA::BYTES + OpB::BYTES;
-  const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
+  const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
   const int m0 = wave / (BN / WN) * WM, n0 = wave % (BN / WN) * WN;
   const E* a = static_cast<const E*>(t.a);
   const E* b = static_cast<const E*>(t.b);
@@ -191,63 +273,96 @@ __device__ __forceinline__ void product(const Tile& t, bool out_f32, char* lds) 
 #pragma unroll
     for (int j = 0; j < TN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-  OpA A;
-  OpB B;
-  int cur = 0;
-  if (t.k0 < t.k1) {
-    A.load(a, t.lda, t.k0, t.k1, t.rows, tid);
-    B.load(b, t.ldb, t.k0, t.k1, t.cols, tid);
-    A.store(lds, tid);
-    B.store(lds + OpA::BYTES, tid);
-  }
-  __syncthreads();
-  for (int64_t k = t.k0; k < t.k1; k += BK) {
-    const bool more = k + BK < t.k1;
-    if (more) {
-      A.load(a, t.lda, k + BK, t.k1, t.rows, tid);
-      B.load(b, t.ldb, k + BK, t.k1, t.cols, tid);
-    }
-    const char* la = lds + cur * STAGE;
+  const auto multiply = [&](const char* la) {
     const char* lb = la + OpA::BYTES;
 #pragma unroll
     for (int kk = 0; kk < BK / 32; ++kk) {
-      lm_u32x4 fb[TN];
+      lm_u32x4 fa[TM], fb[TN];
+      OpA::fragments(la, m0, kk, lane, fa);
+      OpB::fragments(lb, n0, kk, lane, fb);
 #pragma unroll
-      for (int j = 0; j < TN; ++j) fb[j] = OpB::template fragment<true>(lb, n0, j, kk, lane);
+      for (int i = 0; i < TM; ++i)
 #pragma unroll
-      for (int i = 0; i < TM; ++i) {
-        const lm_u32x4 fa = OpA::template fragment<PERM>(la, m0, i, kk, lane);
-#pragma unroll
-        for (int j = 0; j < TN; ++j) acc[i][j] = mma(fb[j], fa, acc[i][j], E{});
-      }
+        for (int j = 0; j < TN; ++j) acc[i][j] = mma(fb[j], fa[i], acc[i][j], E{});
     }
-    if (more) {
-      cur ^= 1;
-      A.store(lds + cur * STAGE, tid);
-      B.store(lds + cur * STAGE + OpA::BYTES, tid);
-      __syncthreads();
+  };
+
+  if constexpr (WIDE) {
+    Direct<OpA, E> A;
+    Direct<OpB, E> B;
+    A.start(t.lda, t.rows, tid);
+    B.start(t.ldb, t.cols, tid);
+    const auto issue = [&](int64_t k, int slot) {
+      A.template load<A_SWAP>(a, t.lda, k, t.k1, t.rows, BK, lds + slot * STAGE, wave * 64 + lane);
+      B.template load<B_SWAP>(b, t.ldb, k, t.k1, t.cols, BK, lds + slot * STAGE + OpA::BYTES, wave * 64 + lane);
+    };
+    if (t.k0 < t.k1) {
+#pragma unroll
+      for (int s = 0; s < STAGES - 1; ++s) issue(t.k0 + s * BK, s);
+      int slot = 0;
+      for (int64_t k = t.k0; k < t.k1; k += BK) {
+        // this step's loads have landed, and nobody reads the slot of the step
+        // before any more
+        wait_step<(STAGES - 2) * (OpA::CHUNKS + OpB::CHUNKS)>();
+        issue(k + (STAGES - 1) * BK, slot == 0 ? STAGES - 1 : slot - 1);
+        multiply(lds + slot * STAGE);
+        slot = slot == STAGES - 1 ? 0 : slot + 1;
+      }
+      // nothing may land in LDS behind the workgroup's end
+      wait_step<0>();
+    }
+  } else {
+    Staged<OpA, E, BK> A;
+    Staged<OpB, E, BK> B;
+    int cur = 0;
+    if (t.k0 < t.k1) {
+      A.template load<A_SWAP>(a, t.lda, t.k0, t.k1, t.rows, tid);
+      B.template load<B_SWAP>(b, t.ldb, t.k0, t.k1, t.cols, tid);
+      A.store(lds, tid);
+      B.store(lds + OpA::BYTES, tid);
+    }
+    __syncthreads();
+    for (int64_t k = t.k0; k < t.k1; k += BK) {
+      const bool more = k + BK < t.k1;
+      if (more) {
+        A.template load<A_SWAP>(a, t.lda, k + BK, t.k1, t.rows, tid);
+        B.template load<B_SWAP>(b, t.ldb, k + BK, t.k1, t.cols, tid);
+      }
+      multiply(lds + cur * STAGE);
+      if (more) {
+        cur ^= 1;
+        A.store(lds + cur * STAGE, tid);
+        B.store(lds + cur * STAGE + OpA::BYTES, tid);
+        __syncthreads();
+      }
     }
   }
 
   const int c = lane % 16, g = lane / 16;
 #pragma unroll
   for (int i = 0; i < TM; ++i) {
-    const int m = m0 + (PERM ? i / 4 * 64 + 16 * (c / 4) + 4 * (i % 4) + c % 4 : i * 16 + c);
+    const int m = m0 + i * 16 + c;
     if (m >= t.rows) continue;
+    if (out_f32) {
+      float* row = static_cast<float*>(t.out) + m * t.ldo;
 #pragma unroll
-    for (int q = 0; q < TN / 4; ++q) {
-      const int n = n0 + q * 64 + 16 * g;
-      if (n >= t.cols) continue;
-      float x[16];
+      for (int j = 0; j < TN; ++j) {
+        const int n = n0 + j * 16 + 4 * g;
+        if (n < t.cols) store_out<float, 4>(row + n, __builtin_bit_cast(lm_u32x4, acc[i][j]), t.cols - n);
+      }
+    } else {
+      // two tiles' lanes exchange halves (odd rows of 16 lanes against even
+      // ones): a lane then holds eight consecutive outputs of one of them
+      E* row = static_cast<E*>(t.out) + m * t.ldo;
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) x[4 * j + r] = acc[i][4 * q + j][r];
-      const int64_t at = static_cast<int64_t>(m) * t.ldo + n;
-      if (out_f32)
-        store16(static_cast<float*>(t.out) + at, x, t.cols - n);
-      else
-        store16(static_cast<E*>(t.out) + at, x, t.cols - n);
+      for (int j = 0; j < TN; j += 2) {
+        const auto x = __builtin_amdgcn_permlane16_swap(pack2<E>(acc[i][j][0], acc[i][j][1]),
+                                                        pack2<E>(acc[i][j + 1][0], acc[i][j + 1][1]), false, false);
+        const auto y = __builtin_amdgcn_permlane16_swap(pack2<E>(acc[i][j][2], acc[i][j][3]),
+                                                        pack2<E>(acc[i][j + 1][2], acc[i][j + 1][3]), false, false);
+        const int n = n0 + (j + g % 2) * 16 + g / 2 * 8;
+        if (n < t.cols) store_out<E, 8>(row + n, lm_u32x4{x[0], y[0], x[1], y[1]}, t.cols - n);
+      }
     }
   }
 }
@@ -261,23 +376,23 @@ struct GroupArgs {
   int64_t T, ld_d, ld_C, ld_W, st_W;
   int splits;
   int64_t part;
-  uint32_t row_tiles, col_tiles, blocks;
+  uint32_t row_tiles, col_tiles, blocks, run;
   int out_f32, out_bytes;
 };
 
 // Terms of one part of a sum of `length` terms: whole steps.
 __device__ __forceinline__ int64_t split_of(int64_t length, int splits) {
-  return ((length + BK - 1) / BK + splits - 1) / splits * BK;
+  return ((length + 63) / 64 + splits - 1) / splits * 64;
 }
 
-template <typename E, int BM, int BN, int WM, int WN, int FORM, bool WIDE>
+template <typename E, int BM, int BN, int WM, int WN, int BK, int STAGES, int FORM, bool WIDE>
 __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64, 2) void k_group(GroupArgs g) {
   constexpr bool A_SWAP = FORM == DBW_GROUP_WEIGHT_GRAD, B_SWAP = FORM != DBW_GROUP_INPUT_GRAD;
-  __shared__ __align__(16) char lds[2 * (BM + BN) * BK * 2];
+  __shared__ __align__(16) char lds[(WIDE ? STAGES : 2) * (BM + BN) * BK * 2];
   // Workgroups go to the eight XCDs in turn; consecutive tiles share an
-  // operand, so each XCD (and its L2) takes a run of them.
-  const uint32_t per = (g.blocks + 7) / 8;
-  const uint32_t id = blockIdx.x % 8 * per + blockIdx.x / 8;
+  // operand, so each XCD (and its L2) takes runs of them: g.run of every 8
+  // g.run, which spreads large and small groups over all XCDs.
+  const uint32_t id = blockIdx.x / (8 * g.run) * (8 * g.run) + blockIdx.x % 8 * g.run + blockIdx.x % (8 * g.run) / 8;
   if (id >= g.blocks) return;
   const int lane = threadIdx.x % 64;
   Tile t;
@@ -370,41 +485,48 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64, 2) void k_group(GroupAr
       t.out = static_cast<char*>(g.out) + (row * t.ldo + n) * g.out_bytes;
     }
   }
-  product<E, BM, BN, WM, WN, A_SWAP, B_SWAP, WIDE>(t, g.splits > 1 || g.out_f32, lds);
+  product<E, BM, BN, WM, WN, BK, STAGES, A_SWAP, B_SWAP, WIDE>(t, g.splits > 1 || g.out_f32, lds);
 }
 
-// out = the sum of the partial outputs, in the order of the parts.
+// out = the sum of the partial outputs, in the order of the parts; a thread
+// takes four columns of a row.
 template <typename O>
 __global__ __launch_bounds__(256) void k_group_sum(GroupArgs g, const float* __restrict__ parts) {
   const bool grad = g.form == DBW_GROUP_WEIGHT_GRAD;
-  const int N = g.form == DBW_GROUP_INPUT_GRAD ? g.d : g.C;
+  const uint32_t N = g.form == DBW_GROUP_INPUT_GRAD ? g.d : g.C, quads = (N + 3) / 4;
   // rows outside the groups stay as they were
-  const int64_t first = grad ? 0 : lm_offset(g.offsets, 0, g.T);
-  const int64_t end = grad ? static_cast<int64_t>(g.n) * g.d : lm_offset(g.offsets, g.n, g.T);
-  const int64_t all = (end - first) * N;
-  for (int64_t i = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) * 4; i < all;
-       i += static_cast<int64_t>(gridDim.x) * 1024) {
-    const float* p = parts + first * N + i;
-    float x[4] = {0.f, 0.f, 0.f, 0.f};
-    if (i + 4 <= all) {
-      for (int s = 0; s < g.splits; ++s) {
-        const lm_f32x4 v = *reinterpret_cast<const lm_f32x4_any*>(p + s * g.part);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) x[j] += v[j];
-      }
+  const uint32_t first = grad ? 0 : static_cast<uint32_t>(lm_offset(g.offsets, 0, g.T));
+  const uint32_t end = grad ? static_cast<uint32_t>(g.n) * g.d : static_cast<uint32_t>(lm_offset(g.offsets, g.n, g.T));
+  if (end <= first) return;
+  // (a split product has fewer than 512 tiles of outputs: 32 bits hold them)
+  const uint32_t all = (end - first) * quads;
+  for (uint32_t i = blockIdx.x * 256 + threadIdx.x; i < all; i += gridDim.x * 256) {
+    const uint32_t row = first + i / quads, n = i % quads * 4;
+    const float* p = parts + static_cast<int64_t>(row) * N + n;
+    const int left = N - n < 4 ? static_cast<int>(N - n) : 4;
+    f32x4 x = {0.f, 0.f, 0.f, 0.f};
+    if (left == 4) {
+#pragma unroll 4
+      for (int s = 0; s < g.splits; ++s) x += *reinterpret_cast<const lm_f32x4_any*>(p + s * g.part);
     } else {
       for (int s = 0; s < g.splits; ++s)
 #pragma unroll
         for (int j = 0; j < 3; ++j)
-          if (i + j < all) x[j] += p[s * g.part + j];
+          if (j < left) x[j] += p[s * g.part + j];
     }
+    O* q = static_cast<O*>(g.out) +
+           (grad ? row / g.d * g.st_W + row % g.d * g.ld_W : row * (g.form == DBW_GROUP_FORWARD ? g.ld_C : g.ld_d)) + n;
+    if constexpr (std::is_same_v<O, float>) {
+      store_out<float, 4>(q, __builtin_bit_cast(lm_u32x4, x), left);
+    } else {
+      const lm_u32x2 v = {pack2<O>(x[0], x[1]), pack2<O>(x[2], x[3])};
+      if (left == 4) {
+        *reinterpret_cast<lm_u32x2_any*>(q) = v;
+      } else {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      if (i + j >= all) break;
-      const int64_t row = first + (i + j) / N, n = (i + j) % N;
-      const int64_t at = grad ? row / g.d * g.st_W + row % g.d * g.ld_W + n
-                              : row * (g.form == DBW_GROUP_FORWARD ? g.ld_C : g.ld_d) + n;
-      static_cast<O*>(g.out)[at] = static_cast<O>(x[j]);
+        for (int j = 0; j < 3; ++j)
+          if (j < left) q[j] = static_cast<O>(x[j]);
+      }
     }
   }
 }
@@ -413,16 +535,18 @@ enum GroupVariant { SMALL = 0, MIDDLE = 1, LARGE = 2 };
 struct VariantSize {
   int bm, bn;
 };
-constexpr VariantSize kSize[] = {{32, 256}, {128, 128}, {256, 256}};
+constexpr VariantSize kSize[] = {{32, 256}, {128, 128}, {128, 256}};
 
 template <typename E, int FORM, bool WIDE>
 void launch_variant(const GroupPlan& plan, const GroupArgs& g, uint32_t grid, hipStream_t s) {
+  constexpr bool GRAD = FORM == DBW_GROUP_WEIGHT_GRAD;
+  constexpr int BK = WIDE && GRAD ? 32 : 64;
   if (plan.variant == LARGE)
-    k_group<E, 256, 256, 128, 64, FORM, WIDE><<<grid, 512, 0, s>>>(g);
-  else if (plan.variant == MIDDLE || FORM == DBW_GROUP_WEIGHT_GRAD)
-    k_group<E, 128, 128, 64, 64, FORM, WIDE><<<grid, 256, 0, s>>>(g);
-  else if constexpr (FORM != DBW_GROUP_WEIGHT_GRAD)
-    k_group<E, 32, 256, 32, 64, FORM, WIDE><<<grid, 256, 0, s>>>(g);
+    k_group<E, 128, 256, 64, 128, 32, 3, FORM, WIDE><<<grid, 256, 0, s>>>(g);
+  else if (plan.variant == MIDDLE || GRAD)
+    k_group<E, 128, 128, 64, 64, BK, 128 / BK, FORM, WIDE><<<grid, 256, 0, s>>>(g);
+  else if constexpr (!GRAD)
+    k_group<E, 32, 256, 32, 64, 64, 2, FORM, WIDE><<<grid, 256, 0, s>>>(g);
 }
 template <typename E, int FORM>
 void launch_wide(bool wide, const GroupPlan& plan, const GroupArgs& g, uint32_t grid, hipStream_t s) {
@@ -493,7 +617,8 @@ hipError_t launch_group(const dbw_group_shape& p, const GroupPlan& plan, const i
     wide = wide && even(a, p.ld_C) && even(b, p.ld_W) && p.st_W % 8 == 0;
   else
     wide = wide && even(a, p.ld_d) && even(b, p.ld_C);
-  const uint32_t grid = (g.blocks + 7) / 8 * 8;
+  g.run = std::min((g.blocks + 7) / 8, 32u);
+  const uint32_t grid = static_cast<uint32_t>(ceil_div(g.blocks, 8 * g.run)) * 8 * g.run;
   if (p.dtype == DBW_BF16)
     launch_form<__bf16>(wide, plan, g, grid, s);
   else
