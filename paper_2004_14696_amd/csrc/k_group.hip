@@ -15,7 +15,8 @@
 // v_mfma_f32_16x16x32 takes, in lane l = 16 g + c, row c and terms 8 g .. 8 g
 // + 7 of each operand; its result r of a lane is row 4 g + r of the first
 // operand, row c of the second.  The output's columns go in as the first
-// operand, so a lane has four consecutive columns of one output row.
+// operand, so a lane has four consecutive columns of one output row; they are
+// turned into whole lines in LDS.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -47,7 +48,7 @@ struct Tile {
   const void* b;
   void* out;
   int64_t lda, ldb, ldo;
-  int64_t k0, k1;
+  int k0, k1;
   int rows, cols;
 };
 
@@ -77,14 +78,15 @@ struct Operand {
 
   // Byte offset in memory of chunk i from the first term of a step with `left`
   // terms, or one behind every buffer: such loads give 0.
-  static __device__ __forceinline__ uint32_t offset(int64_t ld, int64_t left, int length, int tid, int i) {
+  static __device__ __forceinline__ uint32_t offset(int64_t ld, int left, int length, int tid, int i) {
     const int at = line(tid, i), first = chunk(tid, i) * 8;
     const bool in = SWAP ? at < left && first < length : at < length && first < left;
     return in ? static_cast<uint32_t>((at * ld + first) * 2) : kOutOfRange;
   }
 
-  // Fragments of a lane: terms 32 kk + 8 g .. + 7 of outputs first + 16 i + c.
-  template <int N>
+  // Fragments of a lane: terms 32 kk + 8 g .. + 7 of outputs first + 16 i + c,
+  // of the stage AT bytes into LDS.
+  template <int N, int AT>
   static __device__ __forceinline__ void fragments(const char* lds, int first, int kk, int lane, lm_u32x4 (&f)[N]) {
     const int c = lane % 16, g = lane / 16;
     if constexpr (SWAP) {
@@ -92,55 +94,63 @@ struct Operand {
       // lane 4 r + q gives the address of term r, outputs 4 q .. 4 q + 3, and
       // lane c gets the terms of output c; another takes the next four terms
       // (whose lines are turned alike)
-      const int r = c / 4, q = c % 4, at = kk * 32 + g * 8 + r;
+      const int r = c / 4, q = c % 4, line = g * 8 + r;
       typedef __attribute__((address_space(3))) const char* P;
       uint32_t p[N];
 #pragma unroll
       for (int i = 0; i < N; ++i)
         p[i] = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(
-            (P)(lds + at * (L * 2) + (((first + 16 * i) / 8 + q / 2) ^ turn(at)) * 16 + q % 2 * 8)));
+            (P)(lds + line * (L * 2) + (((first + 16 * i) / 8 + q / 2) ^ turn(line)) * 16 + q % 2 * 8)));
       lm_u32x2 x[N][2];
-      read_turned(p, x);
+      if (kk == 0)
+        read_turned<AT>(p, x);
+      else
+        read_turned<(BK == 64 ? AT + 32 * L * 2 : AT)>(p, x);
 #pragma unroll
       for (int i = 0; i < N; ++i) f[i] = lm_u32x4{x[i][0][0], x[i][0][1], x[i][1][0], x[i][1][1]};
     } else {
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         const int row = first + 16 * i + c;
-        f[i] = *reinterpret_cast<const lm_u32x4*>(lds + row * (BK * 2) + ((kk * 4 + g) ^ turn(row)) * 16);
+        f[i] = *reinterpret_cast<const lm_u32x4*>(lds + AT + row * (BK * 2) + ((kk * 4 + g) ^ turn(row)) * 16);
       }
     }
   }
 
   // The transposing loads of N tiles, and the wait for them, in one statement:
   // as builtins, the compiler would first wait for every load on its way to LDS.
+  template <int AT>
   static __device__ __forceinline__ void read_turned(const uint32_t (&p)[4], lm_u32x2 (&x)[4][2]) {
+    static_assert(AT + 4 * L * 2 < 65536, "sixteen bits");
     asm volatile(
-        "ds_read_b64_tr_b16 %0, %8\n\tds_read_b64_tr_b16 %1, %8 offset:%12\n\t"
-        "ds_read_b64_tr_b16 %2, %9\n\tds_read_b64_tr_b16 %3, %9 offset:%12\n\t"
-        "ds_read_b64_tr_b16 %4, %10\n\tds_read_b64_tr_b16 %5, %10 offset:%12\n\t"
-        "ds_read_b64_tr_b16 %6, %11\n\tds_read_b64_tr_b16 %7, %11 offset:%12\n\t"
+        "ds_read_b64_tr_b16 %0, %8 offset:%12\n\tds_read_b64_tr_b16 %1, %8 offset:%13\n\t"
+        "ds_read_b64_tr_b16 %2, %9 offset:%12\n\tds_read_b64_tr_b16 %3, %9 offset:%13\n\t"
+        "ds_read_b64_tr_b16 %4, %10 offset:%12\n\tds_read_b64_tr_b16 %5, %10 offset:%13\n\t"
+        "ds_read_b64_tr_b16 %6, %11 offset:%12\n\tds_read_b64_tr_b16 %7, %11 offset:%13\n\t"
         "s_waitcnt lgkmcnt(0)"
         : "=&v"(x[0][0]), "=&v"(x[0][1]), "=&v"(x[1][0]), "=&v"(x[1][1]), "=&v"(x[2][0]), "=&v"(x[2][1]),
           "=&v"(x[3][0]), "=&v"(x[3][1])
-        : "v"(p[0]), "v"(p[1]), "v"(p[2]), "v"(p[3]), "n"(4 * L * 2)
+        : "v"(p[0]), "v"(p[1]), "v"(p[2]), "v"(p[3]), "n"(AT), "n"(AT + 4 * L * 2)
         : "memory");
   }
+  template <int AT>
   static __device__ __forceinline__ void read_turned(const uint32_t (&p)[8], lm_u32x2 (&x)[8][2]) {
+    static_assert(AT + 4 * L * 2 < 65536, "sixteen bits");
     asm volatile(
-        "ds_read_b64_tr_b16 %0, %16\n\tds_read_b64_tr_b16 %1, %16 offset:%24\n\t"
-        "ds_read_b64_tr_b16 %2, %17\n\tds_read_b64_tr_b16 %3, %17 offset:%24\n\t"
-        "ds_read_b64_tr_b16 %4, %18\n\tds_read_b64_tr_b16 %5, %18 offset:%24\n\t"
-        "ds_read_b64_tr_b16 %6, %19\n\tds_read_b64_tr_b16 %7, %19 offset:%24\n\t"
-        "ds_read_b64_tr_b16 %8, %20\n\tds_read_b64_tr_b16 %9, %20 offset:%24\n\t"
-        "ds_read_b64_tr_b16 %10, %21\n\tds_read_b64_tr_b16 %11, %21 offset:%24\n\t"
-        "ds_read_b64_tr_b16 %12, %22\n\tds_read_b64_tr_b16 %13, %22 offset:%24\n\t"
-        "ds_read_b64_tr_b16 %14, %23\n\tds_read_b64_tr_b16 %15, %23 offset:%24\n\t"
+        "ds_read_b64_tr_b16 %0, %16 offset:%24\n\tds_read_b64_tr_b16 %1, %16 offset:%25\n\t"
+        "ds_read_b64_tr_b16 %2, %17 offset:%24\n\tds_read_b64_tr_b16 %3, %17 offset:%25\n\t"
+        "ds_read_b64_tr_b16 %4, %18 offset:%24\n\tds_read_b64_tr_b16 %5, %18 offset:%25\n\t"
+        "ds_read_b64_tr_b16 %6, %19 offset:%24\n\tds_read_b64_tr_b16 %7, %19 offset:%25\n\t"
+        "ds_read_b64_tr_b16 %8, %20 offset:%24\n\tds_read_b64_tr_b16 %9, %20 offset:%25\n\t"
+        "ds_read_b64_tr_b16 %10, %21 offset:%24\n\tds_read_b64_tr_b16 %11, %21 offset:%25\n\t"
+        "ds_read_b64_tr_b16 %12, %22 offset:%24\n\tds_read_b64_tr_b16 %13, %22 offset:%25\n\t"
+        "ds_read_b64_tr_b16 %14, %23 offset:%24\n\tds_read_b64_tr_b16 %15, %23 offset:%25\n\t"
         "s_waitcnt lgkmcnt(0)"
         : "=&v"(x[0][0]), "=&v"(x[0][1]), "=&v"(x[1][0]), "=&v"(x[1][1]), "=&v"(x[2][0]), "=&v"(x[2][1]),
           "=&v"(x[3][0]), "=&v"(x[3][1]), "=&v"(x[4][0]), "=&v"(x[4][1]), "=&v"(x[5][0]), "=&v"(x[5][1]),
           "=&v"(x[6][0]), "=&v"(x[6][1]), "=&v"(x[7][0]), "=&v"(x[7][1])
-        : "v"(p[0]), "v"(p[1]), "v"(p[2]), "v"(p[3]), "v"(p[4]), "v"(p[5]), "v"(p[6]), "v"(p[7]), "n"(4 * L * 2)
+        : "v"(p[0]), "v"(p[1]), "v"(p[2]), "v"(p[3]), "v"(p[4]), "v"(p[5]), "v"(p[6]), "v"(p[7]), "n"(AT),
+          "n"(AT + 4 * L * 2)
         : "memory");
   }
 };
@@ -151,32 +161,34 @@ __device__ __forceinline__ void load_lds(__amdgpu_buffer_rsrc_t r, char* to, uin
   __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (P)to, 16, off, 0, 0, 0);
 }
 
-// Loads of a step straight into LDS: a wave's instruction fills 1 KiB, lane by
-// lane.  Needs whole chunks: every line of memory starts and ends at one.
-template <typename Op, typename E>
+// Loads of one step after the other straight into LDS: a wave's instruction
+// fills 1 KiB, lane by lane.  Needs whole chunks: every line of memory starts
+// and ends at one.
+template <typename Op, typename E, int BK, bool SWAP>
 struct Direct {
+  static constexpr int WAVES = Op::STEP * Op::LINE / 64;
+  const E* p;                  // the next step's first term
+  int64_t ld, step;
+  int length;
   uint32_t off[Op::CHUNKS];
-  __device__ __forceinline__ void start(int64_t ld, int length, int tid) {
+  __device__ __forceinline__ Direct(const E* first, int64_t ld_, int length_, int k0, int tid)
+      : p(SWAP ? first + k0 * ld_ : first + k0), ld(ld_), step(SWAP ? BK * ld_ : BK), length(length_) {
 #pragma unroll
-    for (int i = 0; i < Op::CHUNKS; ++i) off[i] = Op::offset(ld, int64_t{1} << 32, length, tid, i);
+    for (int i = 0; i < Op::CHUNKS; ++i) off[i] = Op::offset(ld, BK, length, tid, i);
   }
-  // (also of steps behind the last one: zeros, so that every stage counts the same)
-  template <bool SWAP>
-  __device__ __forceinline__ void load(const E* p, int64_t ld, int64_t k, int64_t k1, int length, int bk, char* lds,
-                                       int tid) const {
-    const int64_t left = k1 - k;
-    const __amdgpu_buffer_rsrc_t r = make_rsrc(SWAP ? p + k * ld : p + k, static_cast<uint32_t>(kMaxBufferBytes));
-    char* to = lds + tid / 64 * 1024;
-    constexpr int WAVES = Op::STEP * Op::LINE / 64;
-    if (left >= bk) {
+  // `left` terms from the step's first on: also 0 or fewer, behind the last
+  // step, so that every step counts the same loads
+  __device__ __forceinline__ void load(int left, char* lds, int wave, int lane) {
+    const __amdgpu_buffer_rsrc_t r = make_rsrc(p, static_cast<uint32_t>(kMaxBufferBytes));
+    if (left >= BK) {
 #pragma unroll
-      for (int i = 0; i < Op::CHUNKS; ++i)
-        load_lds(r, to + i * WAVES * 1024, off[i]);
+      for (int i = 0; i < Op::CHUNKS; ++i) load_lds(r, lds + (i * WAVES + wave) * 1024, off[i]);
     } else {
 #pragma unroll
       for (int i = 0; i < Op::CHUNKS; ++i)
-        load_lds(r, to + i * WAVES * 1024, Op::offset(ld, left, length, tid, i));
+        load_lds(r, lds + (i * WAVES + wave) * 1024, Op::offset(ld, left, length, wave * 64 + lane, i));
     }
+    p += step;
   }
 };
 
@@ -186,9 +198,9 @@ template <typename Op, typename E, int BK>
 struct Staged {
   lm_u32x4 held[Op::CHUNKS];
   template <bool SWAP>
-  __device__ __forceinline__ void load(const E* p, int64_t ld, int64_t k, int64_t k1, int length, int tid) {
+  __device__ __forceinline__ void load(const E* p, int64_t ld, int k, int k1, int length, int tid) {
     const E* base = SWAP ? p + k * ld : p + k;
-    const int64_t left = k1 - k;
+    const int left = k1 - k;
     const __amdgpu_buffer_rsrc_t r = make_rsrc(base, static_cast<uint32_t>(kMaxBufferBytes));
     // whole chunks in one load each, at any alignment, without a branch
 #pragma unroll
@@ -203,7 +215,7 @@ struct Staged {
 #pragma unroll
       for (int i = 0; i < Op::CHUNKS; ++i) {
         const int at = Op::line(tid, i), first = Op::chunk(tid, i) * 8;
-        const int64_t in_line = (SWAP ? length : left) - first;
+        const int in_line = (SWAP ? length : left) - first;
         if (at < (SWAP ? left : length) && in_line > 0 && in_line < 8) {
           const E* q = base + at * ld + first;
           typedef E V __attribute__((ext_vector_type(8)));
@@ -242,10 +254,13 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
 }
 
 // N consecutive outputs of one row, `left` of them inside.
-template <typename O, int N>
+template <typename O, int N, bool STREAM = false>
 __device__ __forceinline__ void store_out(O* p, const lm_u32x4& v, int left) {
   if (left >= N) {
-    *reinterpret_cast<lm_u32x4_any*>(p) = v;
+    if (STREAM)
+      __builtin_nontemporal_store(v, reinterpret_cast<lm_u32x4_any*>(p));
+    else
+      *reinterpret_cast<lm_u32x4_any*>(p) = v;
   } else {
     typedef O V __attribute__((ext_vector_type(N)));
     const V x = __builtin_bit_cast(V, v);
@@ -255,7 +270,47 @@ __device__ __forceinline__ void store_out(O* p, const lm_u32x4& v, int left) {
   }
 }
 
-template <typename E, int BM, int BN, int WM, int WN, int BK, int STAGES, bool A_SWAP, bool B_SWAP, bool WIDE>
+// A wave's outputs, by way of its part of LDS: a lane has four columns of one
+// row, memory takes whole lines.  Chunks of 16 bytes are turned by their row,
+// as the operands' are.
+template <typename O, int WM, int WN, int LDS, bool STREAM>
+__device__ __forceinline__ void write_out(const f32x4 (&acc)[WM / 16][WN / 16], const Tile& t, int m0, int n0, char* lds,
+                                          int lane) {
+  constexpr int BYTES = WN * sizeof(O), CH = BYTES / 16, N = 16 / sizeof(O);
+  constexpr int TILES = LDS / BYTES / 16 >= WM / 16 ? WM / 16 : LDS / BYTES >= 64 ? 4 : LDS / BYTES >= 32 ? 2 : 1;
+  constexpr int ROWS = 16 * TILES;                     // rows of a pass
+  static_assert(ROWS * BYTES <= LDS && WM % ROWS == 0 && ROWS * CH % 64 == 0, "whole passes");
+  const int c = lane % 16, g = lane / 16;
+#pragma unroll
+  for (int p = 0; p < WM / ROWS; ++p) {
+#pragma unroll
+    for (int i = 0; i < TILES; ++i) {
+      const int row = i * 16 + c;
+#pragma unroll
+      for (int j = 0; j < WN / 16; ++j) {
+        const f32x4 x = acc[p * TILES + i][j];
+        if constexpr (sizeof(O) == 4) {
+          *reinterpret_cast<f32x4*>(lds + row * BYTES + ((j * 4 + g) ^ (row & (CH - 1) & 15)) * 16) = x;
+        } else {
+          *reinterpret_cast<lm_u32x2*>(lds + row * BYTES + ((j * 2 + g / 2) ^ (row & (CH - 1) & 15)) * 16 + g % 2 * 8) =
+              lm_u32x2{pack2<O>(x[0], x[1]), pack2<O>(x[2], x[3])};
+        }
+      }
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+    for (int i = 0; i < ROWS * CH / 64; ++i) {
+      const int row = (i * 64 + lane) / CH, q = (i * 64 + lane) % CH;
+      const lm_u32x4 v = *reinterpret_cast<const lm_u32x4*>(lds + row * BYTES + (q ^ (row & (CH - 1) & 15)) * 16);
+      const int m = m0 + p * ROWS + row, n = n0 + q * N;
+      if (m < t.rows && n < t.cols) store_out<O, N, STREAM>(static_cast<O*>(t.out) + m * t.ldo + n, v, t.cols - n);
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  }
+}
+
+template <typename E, int BM, int BN, int WM, int WN, int BK, int STAGES, bool A_SWAP, bool B_SWAP, bool WIDE,
+          bool STREAM>
 __device__ __forceinline__ void product(const Tile& t, bool out_f32, char* lds) {
   constexpr int THREADS = (BM / WM) * (BN / WN) * 64;
   constexpr int TM = WM / 16, TN = WN / 16;
@@ -273,13 +328,13 @@ __device__ __forceinline__ void product(const Tile& t, bool out_f32, char* lds) 
 #pragma unroll
     for (int j = 0; j < TN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-  const auto multiply = [&](const char* la) {
-    const char* lb = la + OpA::BYTES;
+  const auto multiply = [&](const char* stages, auto slot) {
+    constexpr int AT = decltype(slot)::value * STAGE;
 #pragma unroll
     for (int kk = 0; kk < BK / 32; ++kk) {
       lm_u32x4 fa[TM], fb[TN];
-      OpA::fragments(la, m0, kk, lane, fa);
-      OpB::fragments(lb, n0, kk, lane, fb);
+      OpA::template fragments<TM, AT>(stages, m0, kk, lane, fa);
+      OpB::template fragments<TN, AT + OpA::BYTES>(stages, n0, kk, lane, fb);
 #pragma unroll
       for (int i = 0; i < TM; ++i)
 #pragma unroll
@@ -288,83 +343,74 @@ __device__ __forceinline__ void product(const Tile& t, bool out_f32, char* lds) 
   };
 
   if constexpr (WIDE) {
-    Direct<OpA, E> A;
-    Direct<OpB, E> B;
-    A.start(t.lda, t.rows, tid);
-    B.start(t.ldb, t.cols, tid);
-    const auto issue = [&](int64_t k, int slot) {
-      A.template load<A_SWAP>(a, t.lda, k, t.k1, t.rows, BK, lds + slot * STAGE, wave * 64 + lane);
-      B.template load<B_SWAP>(b, t.ldb, k, t.k1, t.cols, BK, lds + slot * STAGE + OpA::BYTES, wave * 64 + lane);
+    Direct<OpA, E, BK, A_SWAP> A(a, t.lda, t.rows, t.k0, tid);
+    Direct<OpB, E, BK, B_SWAP> B(b, t.ldb, t.cols, t.k0, tid);
+    const auto issue = [&](int left, int slot) {
+      A.load(left, lds + slot * STAGE, wave, lane);
+      B.load(left, lds + slot * STAGE + OpA::BYTES, wave, lane);
     };
-    if (t.k0 < t.k1) {
+    int left = t.k1 - t.k0;      // terms from the present step on
+    if (left > 0) {
 #pragma unroll
-      for (int s = 0; s < STAGES - 1; ++s) issue(t.k0 + s * BK, s);
-      int slot = 0;
-      for (int64_t k = t.k0; k < t.k1; k += BK) {
+      for (int s = 0; s < STAGES - 1; ++s) issue(left - s * BK, s);
+      // the slots in turn, each with its own code: their places are constants
+      const auto step = [&](auto slot) {
+        constexpr int SLOT = decltype(slot)::value;
         // this step's loads have landed, and nobody reads the slot of the step
         // before any more
         wait_step<(STAGES - 2) * (OpA::CHUNKS + OpB::CHUNKS)>();
-        issue(k + (STAGES - 1) * BK, slot == 0 ? STAGES - 1 : slot - 1);
-        multiply(lds + slot * STAGE);
-        slot = slot == STAGES - 1 ? 0 : slot + 1;
+        issue(left - (STAGES - 1) * BK, (SLOT + STAGES - 1) % STAGES);
+        multiply(lds, slot);
+        left -= BK;
+      };
+      for (;;) {
+        step(std::integral_constant<int, 0>{});
+        if (left <= 0) break;
+        step(std::integral_constant<int, 1>{});
+        if (left <= 0) break;
+        if constexpr (STAGES > 2) {
+          step(std::integral_constant<int, 2>{});
+          if (left <= 0) break;
+        }
+        if constexpr (STAGES > 3) {
+          step(std::integral_constant<int, 3>{});
+          if (left <= 0) break;
+        }
       }
-      // nothing may land in LDS behind the workgroup's end
+      // nothing may land in LDS any more: the outputs go through it
       wait_step<0>();
     }
   } else {
     Staged<OpA, E, BK> A;
     Staged<OpB, E, BK> B;
-    int cur = 0;
-    if (t.k0 < t.k1) {
-      A.template load<A_SWAP>(a, t.lda, t.k0, t.k1, t.rows, tid);
-      B.template load<B_SWAP>(b, t.ldb, t.k0, t.k1, t.cols, tid);
-      A.store(lds, tid);
-      B.store(lds + OpA::BYTES, tid);
-    }
-    __syncthreads();
-    for (int64_t k = t.k0; k < t.k1; k += BK) {
-      const bool more = k + BK < t.k1;
-      if (more) {
-        A.template load<A_SWAP>(a, t.lda, k + BK, t.k1, t.rows, tid);
-        B.template load<B_SWAP>(b, t.ldb, k + BK, t.k1, t.cols, tid);
-      }
-      multiply(lds + cur * STAGE);
-      if (more) {
-        cur ^= 1;
-        A.store(lds + cur * STAGE, tid);
-        B.store(lds + cur * STAGE + OpA::BYTES, tid);
-        __syncthreads();
+    int k = t.k0, left = t.k1 - t.k0;
+    const auto load = [&](int from) {
+      A.template load<A_SWAP>(a, t.lda, from, t.k1, t.rows, tid);
+      B.template load<B_SWAP>(b, t.ldb, from, t.k1, t.cols, tid);
+    };
+    const auto store = [&](int slot) {
+      A.store(lds + slot * STAGE, tid);
+      B.store(lds + slot * STAGE + OpA::BYTES, tid);
+      __syncthreads();
+    };
+    if (left > 0) {
+      load(k);
+      store(0);
+      for (int slot = 0; left > 0; slot ^= 1, left -= BK) {
+        if (left > BK) load(k += BK);
+        multiply(lds + slot * STAGE, std::integral_constant<int, 0>{});
+        if (left > BK) store(slot ^ 1);
       }
     }
+    __syncthreads();   // the outputs go through LDS
   }
 
-  const int c = lane % 16, g = lane / 16;
-#pragma unroll
-  for (int i = 0; i < TM; ++i) {
-    const int m = m0 + i * 16 + c;
-    if (m >= t.rows) continue;
-    if (out_f32) {
-      float* row = static_cast<float*>(t.out) + m * t.ldo;
-#pragma unroll
-      for (int j = 0; j < TN; ++j) {
-        const int n = n0 + j * 16 + 4 * g;
-        if (n < t.cols) store_out<float, 4>(row + n, __builtin_bit_cast(lm_u32x4, acc[i][j]), t.cols - n);
-      }
-    } else {
-      // two tiles' lanes exchange halves (odd rows of 16 lanes against even
-      // ones): a lane then holds eight consecutive outputs of one of them
-      E* row = static_cast<E*>(t.out) + m * t.ldo;
-#pragma unroll
-      for (int j = 0; j < TN; j += 2) {
-        const auto x = __builtin_amdgcn_permlane16_swap(pack2<E>(acc[i][j][0], acc[i][j][1]),
-                                                        pack2<E>(acc[i][j + 1][0], acc[i][j + 1][1]), false, false);
-        const auto y = __builtin_amdgcn_permlane16_swap(pack2<E>(acc[i][j][2], acc[i][j][3]),
-                                                        pack2<E>(acc[i][j + 1][2], acc[i][j + 1][3]), false, false);
-        const int n = n0 + (j + g % 2) * 16 + g / 2 * 8;
-        if (n < t.cols) store_out<E, 8>(row + n, lm_u32x4{x[0], y[0], x[1], y[1]}, t.cols - n);
-      }
-    }
-  }
+  constexpr int LDS = (WIDE ? STAGES : 2) * STAGE / (THREADS / 64);   // bytes a wave
+  char* mine = lds + wave * LDS;
+  if (out_f32)
+    write_out<float, WM, WN, LDS, STREAM>(acc, t, m0, n0, mine, lane);
+  else
+    write_out<E, WM, WN, LDS, STREAM>(acc, t, m0, n0, mine, lane);
 }
 
 struct GroupArgs {
@@ -412,8 +458,8 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64, 2) void k_group(GroupAr
     t.b = static_cast<const E*>(g.b) + n;
     t.lda = g.ld_d;
     t.ldb = g.ld_C;
-    t.k0 = first + std::min<int64_t>(length, split * step);
-    t.k1 = first + std::min<int64_t>(length, (split + 1) * step);
+    t.k0 = static_cast<int>(first + std::min<int64_t>(length, split * step));
+    t.k1 = static_cast<int>(first + std::min<int64_t>(length, (split + 1) * step));
     t.rows = std::min(BM, g.d - m);
     t.cols = std::min(BN, g.C - n);
     if (g.splits > 1) {
@@ -473,8 +519,8 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64, 2) void k_group(GroupAr
     t.ldb = g.ld_W;
     t.a = static_cast<const E*>(g.a) + row * t.lda;
     t.b = static_cast<const E*>(g.b) + group * g.st_W + (FORM == DBW_GROUP_FORWARD ? n : n * g.ld_W);
-    t.k0 = std::min<int64_t>(K, split * step);
-    t.k1 = std::min<int64_t>(K, (split + 1) * step);
+    t.k0 = static_cast<int>(std::min<int64_t>(K, split * step));
+    t.k1 = static_cast<int>(std::min<int64_t>(K, (split + 1) * step));
     t.rows = static_cast<int>(std::min<int64_t>(BM, end - row));
     t.cols = std::min(BN, N - n);
     if (g.splits > 1) {
@@ -485,7 +531,7 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64, 2) void k_group(GroupAr
       t.out = static_cast<char*>(g.out) + (row * t.ldo + n) * g.out_bytes;
     }
   }
-  product<E, BM, BN, WM, WN, BK, STAGES, A_SWAP, B_SWAP, WIDE>(t, g.splits > 1 || g.out_f32, lds);
+  product<E, BM, BN, WM, WN, BK, STAGES, A_SWAP, B_SWAP, WIDE, FORM == DBW_GROUP_WEIGHT_GRAD>(t, g.splits > 1 || g.out_f32, lds);
 }
 
 // out = the sum of the partial outputs, in the order of the parts; a thread
@@ -531,22 +577,28 @@ __global__ __launch_bounds__(256) void k_group_sum(GroupArgs g, const float* __r
   }
 }
 
+constexpr int64_t kTarget = 512;
 enum GroupVariant { SMALL = 0, MIDDLE = 1, LARGE = 2 };
 struct VariantSize {
   int bm, bn;
 };
-constexpr VariantSize kSize[] = {{32, 256}, {128, 128}, {128, 256}};
+constexpr VariantSize kSize[] = {{32, 128}, {128, 128}, {128, 256}};
 
 template <typename E, int FORM, bool WIDE>
 void launch_variant(const GroupPlan& plan, const GroupArgs& g, uint32_t grid, hipStream_t s) {
   constexpr bool GRAD = FORM == DBW_GROUP_WEIGHT_GRAD;
   constexpr int BK = WIDE && GRAD ? 32 : 64;
-  if (plan.variant == LARGE)
-    k_group<E, 128, 256, 64, 128, 32, 3, FORM, WIDE><<<grid, 256, 0, s>>>(g);
-  else if (plan.variant == MIDDLE || GRAD)
-    k_group<E, 128, 128, 64, 64, BK, 128 / BK, FORM, WIDE><<<grid, 256, 0, s>>>(g);
-  else if constexpr (!GRAD)
-    k_group<E, 32, 256, 32, 64, 64, 2, FORM, WIDE><<<grid, 256, 0, s>>>(g);
+  if constexpr (WIDE && FORM != DBW_GROUP_INPUT_GRAD)
+    if (plan.variant == LARGE) {
+      k_group<E, 128, 256, 64, 128, 32, 3, FORM, WIDE><<<grid, 256, 0, s>>>(g);
+      return;
+    }
+  if constexpr (!GRAD)
+    if (plan.variant == SMALL) {
+      k_group<E, 32, 128, 16, 64, 64, 3, FORM, WIDE><<<grid, 256, 0, s>>>(g);
+      return;
+    }
+  k_group<E, 128, 128, 64, 64, BK, 128 / BK, FORM, WIDE><<<grid, 256, 0, s>>>(g);
 }
 template <typename E, int FORM>
 void launch_wide(bool wide, const GroupPlan& plan, const GroupArgs& g, uint32_t grid, hipStream_t s) {
@@ -569,34 +621,59 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 }  // namespace
 
-GroupPlan group_plan(const dbw_group_shape& p) {
+namespace {
+
+// The plan with a given variant; splits = 0: as many as fill the GPU.
+GroupPlan plan_of(const dbw_group_shape& p, int variant, int splits) {
   GroupPlan plan;
   const bool grad = p.form == DBW_GROUP_WEIGHT_GRAD;
   const int64_t groups = p.st_W == 0 && !grad ? 1 : p.n;
-  const int64_t M = grad ? p.d : p.T, N = p.form == DBW_GROUP_INPUT_GRAD ? p.d : p.C;
-  const int64_t rows = grad ? M : std::max<int64_t>(1, p.T / groups);   // of one group, on average
-  const auto tiles = [&](int v) {
-    const int64_t per = ceil_div(rows, kSize[v].bm) * ceil_div(N, kSize[v].bn);
-    return per * groups;
-  };
-  plan.variant = rows <= 48 && !grad ? SMALL : tiles(LARGE) >= 512 && rows >= 512 ? LARGE : MIDDLE;
-  const VariantSize size = kSize[plan.variant];
+  const int64_t N = p.form == DBW_GROUP_INPUT_GRAD ? p.d : p.C;
+  const int64_t rows = grad ? p.d : std::max<int64_t>(1, p.T / groups);   // of one group, on average
+  const VariantSize size = kSize[variant];
+  plan.variant = variant;
   // every group may end in a tile of its own
   plan.row_tiles = grad ? ceil_div(p.d, size.bm)
                         : std::min<int64_t>(p.T, p.T / size.bm + std::min<int64_t>(groups, p.T));
   plan.col_tiles = ceil_div(N, size.bn);
+  plan.tiles = std::max<int64_t>(1, ceil_div(rows, size.bm) * plan.col_tiles * groups);
   const int64_t K = grad ? p.T / p.n : p.form == DBW_GROUP_FORWARD ? p.d : p.C;
-  const int64_t blocks = std::max<int64_t>(1, tiles(plan.variant));
-  plan.splits = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({512 / blocks, K / 256, 64})));
+  plan.splits = splits ? splits
+                       : static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({kTarget / plan.tiles, K / 256, 64})));
   plan.part = grad ? static_cast<int64_t>(p.n) * p.d * p.C : p.T * N;
   plan.blocks = plan.row_tiles * plan.col_tiles * plan.splits * (grad ? p.n : 1);
   return plan;
 }
 
-hipError_t launch_group(const dbw_group_shape& p, const GroupPlan& plan, const int32_t* offsets, const void* a,
+}  // namespace
+
+GroupPlan group_plan(const dbw_group_shape& p) {
+  const bool grad = p.form == DBW_GROUP_WEIGHT_GRAD;
+  const int64_t groups = p.st_W == 0 && !grad ? 1 : p.n;
+  const GroupPlan middle = plan_of(p, MIDDLE, 0);
+  if (!grad && (p.T / groups <= 32 || middle.tiles <= 128)) return plan_of(p, SMALL, 0);
+  if (p.form != DBW_GROUP_INPUT_GRAD) {
+    const GroupPlan large = plan_of(p, LARGE, 1);
+    if (large.tiles >= 384) return large;
+  }
+  return middle;
+}
+
+hipError_t launch_group(const dbw_group_shape& p, GroupPlan plan, const int32_t* offsets, const void* a,
                         const void* b, void* out, float* workspace, hipStream_t s) {
   const bool grad = p.form == DBW_GROUP_WEIGHT_GRAD;
   if (!grad && p.T == 0) return hipSuccess;
+  // whole chunks of 16 bytes: every row starts at one and ends with one
+  const auto even = [](const void* q, int64_t ld) { return reinterpret_cast<uintptr_t>(q) % 16 == 0 && ld % 8 == 0; };
+  bool wide = p.d % 8 == 0 && p.C % 8 == 0;
+  if (p.form == DBW_GROUP_FORWARD)
+    wide = wide && even(a, p.ld_d) && even(b, p.ld_W) && p.st_W % 8 == 0;
+  else if (p.form == DBW_GROUP_INPUT_GRAD)
+    wide = wide && even(a, p.ld_C) && even(b, p.ld_W) && p.st_W % 8 == 0;
+  else
+    wide = wide && even(a, p.ld_d) && even(b, p.ld_C);
+  // (the large tile is for whole chunks; its plan has no parts either)
+  if (!wide && plan.variant == LARGE) plan = plan_of(p, MIDDLE, 1);
   GroupArgs g{};
   g.offsets = offsets; g.a = a; g.b = b; g.form = p.form; g.n = p.n; g.d = p.d; g.C = p.C;
   g.T = p.T; g.ld_d = p.ld_d; g.ld_C = p.ld_C; g.ld_W = p.ld_W;
@@ -608,15 +685,6 @@ hipError_t launch_group(const dbw_group_shape& p, const GroupPlan& plan, const i
   g.out_bytes = elem_bytes(p.out_dtype);
   g.blocks = static_cast<uint32_t>(plan.blocks);
   g.out = plan.splits > 1 ? workspace : out;
-  // whole chunks of 16 bytes: every row starts at one and ends with one
-  const auto even = [](const void* q, int64_t ld) { return reinterpret_cast<uintptr_t>(q) % 16 == 0 && ld % 8 == 0; };
-  bool wide = p.d % 8 == 0 && p.C % 8 == 0;
-  if (p.form == DBW_GROUP_FORWARD)
-    wide = wide && even(a, p.ld_d) && even(b, p.ld_W) && p.st_W % 8 == 0;
-  else if (p.form == DBW_GROUP_INPUT_GRAD)
-    wide = wide && even(a, p.ld_C) && even(b, p.ld_W) && p.st_W % 8 == 0;
-  else
-    wide = wide && even(a, p.ld_d) && even(b, p.ld_C);
   g.run = std::min((g.blocks + 7) / 8, 32u);
   const uint32_t grid = static_cast<uint32_t>(ceil_div(g.blocks, 8 * g.run)) * 8 * g.run;
   if (p.dtype == DBW_BF16)

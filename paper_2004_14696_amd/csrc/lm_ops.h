@@ -124,10 +124,11 @@ struct GroupPlan {
   int64_t row_tiles = 0;  // most row tiles (FORWARD, INPUT_GRAD) or tiles of d (WEIGHT_GRAD)
   int64_t col_tiles = 0;
   int64_t part = 0;       // floats of one partial output (splits > 1)
+  int64_t tiles = 0;      // output tiles, with rows spread evenly over the groups
   int64_t blocks = 0;     // workgroups
 };
 GroupPlan group_plan(const dbw_group_shape& p);
-hipError_t launch_group(const dbw_group_shape& p, const GroupPlan& plan, const int32_t* offsets, const void* a,
+hipError_t launch_group(const dbw_group_shape& p, GroupPlan plan, const int32_t* offsets, const void* a,
                         const void* b, void* out, float* workspace, hipStream_t s);
 
 }  // namespace dbw
