@@ -1,7 +1,9 @@
 // Token loss: mean cross entropy of each worker's rows, and its gradient.
-//   k_token_count  live rows of each worker -> 1 / count
+//   k_token_count  live rows of each worker, in parts (few rows: counted by
+//                  k_token_rows itself)
 //   k_token_rows   a workgroup (or a wave) to a row: loss and gradient
-//   k_token_mean   a workgroup to a worker: the mean of its rows' losses
+//   k_token_sum    sums of the workers' row losses, in parts (many rows only)
+//   k_token_mean   a workgroup to a worker: the mean
 //
 // k_token_rows is bound by memory: T C logits read once and as many gradients
 // written once.  A row stays in registers, as it was loaded, between the
@@ -10,10 +12,12 @@
 // operations a value, against a second read of the row).  Rows beyond what a
 // workgroup's registers hold are read a second time.
 //
-// softmax(z)_c = exp(z_c - max) / sum exp(z - max), in fp32.  The maximum is
-// subtracted before the product with log2(e), which could overflow.
+// softmax(z)_c = 2^(b z_c - b max) / sum 2^(b z - b max) with b = log2(e), in
+// fp32: one fused multiply-add and one exponential a value.  b max is rounded;
+// that factor is the same above and below, and is taken out of the loss.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 
 #include "lm_ops.h"
@@ -24,40 +28,51 @@ namespace {
 constexpr int64_t kMaxGrid = int64_t{1} << 20;
 constexpr float kLog2e = 1.44269504088896341f;
 
-__global__ __launch_bounds__(256) void k_token_count(int n, int64_t T, const int32_t* __restrict__ offsets,
-                                                     const int32_t* __restrict__ y, float* __restrict__ inv) {
-  const int i = blockIdx.x;
-  const int64_t a = lm_offset(offsets, i, T), b = lm_offset(offsets, i + 1, T);
-  int count = 0;
-  for (int64_t t = a + threadIdx.x; t < b; t += 256) count += y[t] >= 0;
+// Rows [a, b) of part `part` of the rows of worker i.
+__device__ __forceinline__ void part_rows(const TokenArgs& g, int i, int part, int64_t* a, int64_t* b) {
+  const int64_t first = lm_offset(g.offsets, i, g.T), end = lm_offset(g.offsets, i + 1, g.T);
+  const int64_t all = end > first ? end - first : 0, each = (all + g.parts - 1) / g.parts;
+  *a = first + (part * each < all ? part * each : all);
+  *b = first + ((part + 1) * each < all ? (part + 1) * each : all);
+}
+
+__device__ __forceinline__ int wave_sum(int v) {
 #pragma unroll
-  for (int d = 32; d; d /= 2) count += __shfl_xor(count, d);
+  for (int d = 32; d; d /= 2) v += __shfl_xor(v, d);
+  return v;
+}
+__device__ __forceinline__ double wave_sum(double v) {
+#pragma unroll
+  for (int d = 32; d; d /= 2) v += __shfl_xor(v, d);
+  return v;
+}
+
+__global__ __launch_bounds__(256) void k_token_count(TokenArgs g) {
+  const int i = blockIdx.x / g.parts, part = blockIdx.x % g.parts;
+  int64_t a, b;
+  part_rows(g, i, part, &a, &b);
+  int count = 0;
+#pragma unroll 4
+  for (int64_t t = a + threadIdx.x; t < b; t += 256) count += g.y[t] >= 0;
+  count = wave_sum(count);
   __shared__ int waves[4];
   if (threadIdx.x % 64 == 0) waves[threadIdx.x / 64] = count;
   __syncthreads();
-  if (threadIdx.x == 0) {
-    const int all = waves[0] + waves[1] + waves[2] + waves[3];
-    inv[i] = all ? static_cast<float>(1.0 / all) : 0.f;
-  }
+  if (threadIdx.x == 0) g.counts[blockIdx.x] = waves[0] + waves[1] + waves[2] + waves[3];
 }
 
-__global__ __launch_bounds__(256) void k_token_mean(int n, int64_t T, const int32_t* __restrict__ offsets,
-                                                    const float* __restrict__ row_loss, const int32_t* __restrict__ y,
-                                                    float* __restrict__ loss) {
-  const int i = blockIdx.x;
-  const int64_t a = lm_offset(offsets, i, T), b = lm_offset(offsets, i + 1, T);
+// Sum and number of the live rows [a, b), for thread 0 (in a fixed order).
+__device__ __forceinline__ void sum_rows(const TokenArgs& g, int64_t a, int64_t b, double* all, int* live) {
   double sum = 0.0;
   int count = 0;
+#pragma unroll 4
   for (int64_t t = a + threadIdx.x; t < b; t += 256) {
-    const bool live = y[t] >= 0;
-    count += live;
-    sum += live ? row_loss[t] : 0.f;
+    const bool is = g.y[t] >= 0;
+    count += is;
+    sum += is ? g.row_loss[t] : 0.f;
   }
-#pragma unroll
-  for (int d = 32; d; d /= 2) {
-    sum += __shfl_xor(sum, d);
-    count += __shfl_xor(count, d);
-  }
+  sum = wave_sum(sum);
+  count = wave_sum(count);
   __shared__ double sums[4];
   __shared__ int counts[4];
   if (threadIdx.x % 64 == 0) {
@@ -65,10 +80,37 @@ __global__ __launch_bounds__(256) void k_token_mean(int n, int64_t T, const int3
     counts[threadIdx.x / 64] = count;
   }
   __syncthreads();
+  *all = (sums[0] + sums[1]) + (sums[2] + sums[3]);
+  *live = counts[0] + counts[1] + counts[2] + counts[3];
+}
+
+__global__ __launch_bounds__(256) void k_token_sum(TokenArgs g) {
+  int64_t a, b;
+  part_rows(g, blockIdx.x / g.parts, blockIdx.x % g.parts, &a, &b);
+  double sum;
+  int count;
+  sum_rows(g, a, b, &sum, &count);
   if (threadIdx.x == 0) {
-    const int all = counts[0] + counts[1] + counts[2] + counts[3];
-    loss[i] = all ? static_cast<float>(((sums[0] + sums[1]) + (sums[2] + sums[3])) / all) : 0.f;
+    g.sums[blockIdx.x] = sum;
+    g.counts[blockIdx.x] = count;
   }
+}
+
+__global__ __launch_bounds__(256) void k_token_mean(TokenArgs g) {
+  const int i = blockIdx.x;
+  double sum = 0.0;
+  int count = 0;
+  if (g.parts > 1) {
+    for (int p = 0; p < g.parts; ++p) {
+      sum += g.sums[i * g.parts + p];
+      count += g.counts[i * g.parts + p];
+    }
+  } else {
+    int64_t a, b;
+    part_rows(g, i, 0, &a, &b);
+    sum_rows(g, a, b, &sum, &count);
+  }
+  if (threadIdx.x == 0) g.loss[i] = count ? static_cast<float>(sum / count) : 0.f;
 }
 
 // Sixteen bytes of logits.
@@ -77,25 +119,6 @@ struct Pack {
   static constexpr int N = 16 / sizeof(E);
   typedef E V __attribute__((ext_vector_type(16 / sizeof(E))));
 };
-
-template <typename E>
-__device__ __forceinline__ lm_u32x4 load_pack(const E* p, int64_t n, E fill) {
-  if (n >= Pack<E>::N) return *reinterpret_cast<const lm_u32x4_any*>(p);
-  typename Pack<E>::V v;
-#pragma unroll
-  for (int j = 0; j < Pack<E>::N; ++j) v[j] = j < n ? p[j] : fill;
-  return __builtin_bit_cast(lm_u32x4, v);
-}
-template <typename E>
-__device__ __forceinline__ void store_pack(E* p, int64_t n, typename Pack<E>::V v) {
-  if (n >= Pack<E>::N) {
-    *reinterpret_cast<lm_u32x4_any*>(p) = __builtin_bit_cast(lm_u32x4, v);
-  } else {
-#pragma unroll
-    for (int j = 0; j < Pack<E>::N; ++j)
-      if (j < n) p[j] = v[j];
-  }
-}
 
 template <int THREADS>
 __device__ __forceinline__ float row_max(float v, float* lds) {
@@ -125,50 +148,80 @@ __device__ __forceinline__ float row_sum(float v, float* lds) {
   return v;
 }
 
+// 2^(b x - b max) of a row, b max rounded.  Where b max would overflow, a value
+// below max is so far below that any base will do.
+struct Powers {
+  float b, bm;
+  __device__ __forceinline__ void set(float max) {
+#pragma clang fp contract(off)   // bm is the rounded product wherever it is used
+    const bool large = !(fabsf(max) < 0x1p126f);
+    b = large ? 1.f : kLog2e;
+    bm = b * max;
+  }
+  __device__ __forceinline__ float operator()(float x) const { return __builtin_amdgcn_exp2f(fmaf(x, b, -bm)); }
+  // another maximum: the factor of powers taken before (from -infinity: 0)
+  __device__ __forceinline__ float move(float max) {
+#pragma clang fp contract(off)
+    const float was = bm;
+    set(max);
+    return __builtin_amdgcn_exp2f(was - bm);
+  }
+  // log of the factor that the rounding of b max put on every power
+  __device__ __forceinline__ float lost(float max) const {
+    return fabsf(max) < 0x1p126f ? fmaf(max, b, -bm) * 0.693147180559945309f : 0.f;
+  }
+};
+
 // One row by THREADS threads, PACKS packs of 16 bytes a thread held in
 // registers; PACKS = 0: the row is read twice.
 template <typename E, int THREADS, int PACKS>
 __device__ __forceinline__ void token_row(const TokenArgs& a, int64_t t, int tid, float* lds) {
   constexpr int N = Pack<E>::N;
   typedef typename Pack<E>::V V;
+  const int lane = threadIdx.x % 64;
   // the worker of the row: how many of offsets[1..n] are at most t
   if (t < lm_offset(a.offsets, 0, a.T)) return;
   int worker = 0;
-  for (int i = threadIdx.x % 64; i < a.n; i += 64) worker += lm_offset(a.offsets, i + 1, a.T) <= t;
-#pragma unroll
-  for (int d = 32; d; d /= 2) worker += __shfl_xor(worker, d);
+  for (int i = lane; i < a.n; i += 64) worker += lm_offset(a.offsets, i + 1, a.T) <= t;
+  worker = wave_sum(worker);
   if (worker >= a.n) return;
 
   const E* z = static_cast<const E*>(a.Z) + t * a.ld_Z;
   E* dz = a.dZ ? static_cast<E*>(a.dZ) + t * a.ld_dZ : nullptr;
   const int y = a.y[t];
   const int C = a.C;
+  // the row in whole packs at whole 16 bytes of memory, and the values before
+  // and behind them, one a thread
+  const int off = static_cast<int>(reinterpret_cast<uintptr_t>(z) % 16 / sizeof(E));
+  const int head = off ? (N - off < C ? N - off : C) : 0;
+  const int packs = (C - head) / N;
+  const int edge = tid < head ? tid : head + packs * N + tid - head;
+  const bool has_edge = tid < head || (tid < 2 * N && edge < C);
+  const E* zb = z + head;
+  E* db = dz + head;
   if (y < 0) {
     if (dz) {
-      V zero;
-#pragma unroll
-      for (int j = 0; j < N; ++j) zero[j] = static_cast<E>(0.f);
-      for (int c = tid * N; c < C; c += THREADS * N) store_pack<E>(dz + c, C - c, zero);
+      for (int p = tid; p < packs; p += THREADS) *reinterpret_cast<lm_u32x4_any*>(db + p * N) = lm_u32x4{0, 0, 0, 0};
+      if (has_edge) dz[edge] = static_cast<E>(0.f);
     }
     return;
   }
   const E low = static_cast<E>(-INFINITY);
   const float zy = y < C ? lm_to_f32(z[y]) : NAN;   // read before any store: dZ may be Z
-  float top = -INFINITY, sum = 0.f;
+  const float ze = has_edge ? lm_to_f32(z[edge]) : -INFINITY;
+  float top, sum;
+  Powers e;
   lm_u32x4 held[PACKS ? PACKS : 1];
   if (PACKS) {
+    V fill;
+#pragma unroll
+    for (int j = 0; j < N; ++j) fill[j] = low;
 #pragma unroll
     for (int p = 0; p < PACKS; ++p) {
-      const int c = (p * THREADS + tid) * N;
-      if (c < C) {
-        held[p] = load_pack<E>(z + c, C - c, low);
-      } else {
-        V v;
-#pragma unroll
-        for (int j = 0; j < N; ++j) v[j] = low;
-        held[p] = __builtin_bit_cast(lm_u32x4, v);
-      }
+      held[p] = __builtin_bit_cast(lm_u32x4, fill);
+      if (p * THREADS + tid < packs) held[p] = *reinterpret_cast<const lm_u32x4_any*>(zb + (p * THREADS + tid) * N);
     }
+    top = ze;
 #pragma unroll
     for (int p = 0; p < PACKS; ++p) {
       const V v = __builtin_bit_cast(V, held[p]);
@@ -176,70 +229,81 @@ __device__ __forceinline__ void token_row(const TokenArgs& a, int64_t t, int tid
       for (int j = 0; j < N; ++j) top = fmaxf(top, lm_to_f32(v[j]));
     }
     top = row_max<THREADS>(top, lds);
+    e.set(top);
+    sum = e(ze);
 #pragma unroll
     for (int p = 0; p < PACKS; ++p) {
+      asm volatile("" : "+v"(held[p]));   // unpacked anew: the values are not kept as fp32
       const V v = __builtin_bit_cast(V, held[p]);
 #pragma unroll
-      for (int j = 0; j < N; ++j) sum += __builtin_amdgcn_exp2f((lm_to_f32(v[j]) - top) * kLog2e);
+      for (int j = 0; j < N; ++j) sum += e(lm_to_f32(v[j]));
     }
     sum = row_sum<THREADS>(sum, lds);
   } else {
-    // running maximum and sum of every thread, joined at the end
-    float mx = -INFINITY;
-    for (int c = tid * N; c < C; c += THREADS * N) {
-      const V v = __builtin_bit_cast(V, load_pack<E>(z + c, C - c, low));
+    // running maximum and sum of every thread, joined at the end; a thread
+    // that has seen only -infinities keeps 0
+    float mx = ze;
+    e.set(mx);
+    sum = ze == -INFINITY ? 0.f : e(ze);
+    for (int p = tid; p < packs; p += THREADS) {
+      const V v = __builtin_bit_cast(V, static_cast<lm_u32x4>(*reinterpret_cast<const lm_u32x4_any*>(zb + p * N)));
       float m = mx;
 #pragma unroll
       for (int j = 0; j < N; ++j) m = fmaxf(m, lm_to_f32(v[j]));
-      // a thread that has seen only -infinities keeps 0 (NaNs pass)
-      sum = m == mx ? sum : sum * __builtin_amdgcn_exp2f((mx - m) * kLog2e);
-      mx = m;
+      if (m != mx) {
+        sum *= e.move(m);
+        mx = m;
+      }
 #pragma unroll
       for (int j = 0; j < N; ++j) {
         const float x = lm_to_f32(v[j]);
-        sum += x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((x - m) * kLog2e);
+        sum += x == -INFINITY ? 0.f : e(x);
       }
     }
     top = row_max<THREADS>(mx, lds);
-    sum = mx == -INFINITY && sum == 0.f && top != -INFINITY ? 0.f
-                                                              : sum * __builtin_amdgcn_exp2f((mx - top) * kLog2e);
+    sum *= e.move(top);
     sum = row_sum<THREADS>(sum, lds);
   }
-  if (tid == 0) a.row_loss[t] = logf(sum) + (top - zy);
+  if (tid == 0) a.row_loss[t] = logf(sum) - e.lost(top) + (top - zy);
   if (!dz) return;
-  const float s = a.scale * a.inv[worker];
+  // live rows of the worker (at least this one)
+  int count = 0;
+  if (a.parts == 0) {
+    const int64_t end = lm_offset(a.offsets, worker + 1, a.T);
+    for (int64_t r = lm_offset(a.offsets, worker, a.T) + lane; r < end; r += 64) count += a.y[r] >= 0;
+  } else if (lane < a.parts) {
+    count = a.counts[worker * a.parts + lane];
+  }
+  const float s = a.scale / static_cast<float>(wave_sum(count));
   const float f = y < C ? s / sum : NAN;
+  if (has_edge) dz[edge] = static_cast<E>(e(ze) * f - (edge == y ? s : 0.f));
+  const auto gradient = [&](const lm_u32x4& x, int p) {
+    const V v = __builtin_bit_cast(V, x);
+    const int at = y - head - p * N;
+    V o;
+#pragma unroll
+    for (int j = 0; j < N; ++j) o[j] = static_cast<E>(e(lm_to_f32(v[j])) * f);
+    *reinterpret_cast<lm_u32x4_any*>(db + p * N) = __builtin_bit_cast(lm_u32x4, o);
+    if (at >= 0 && at < N) dz[y] = static_cast<E>(e(zy) * f - s);   // (after its pack, by the same thread)
+  };
   if (PACKS) {
 #pragma unroll
     for (int p = 0; p < PACKS; ++p) {
-      const int c = (p * THREADS + tid) * N;
-      if (c < C) {
-        const V v = __builtin_bit_cast(V, held[p]);
-        V o;
-#pragma unroll
-        for (int j = 0; j < N; ++j) {
-          const float e = __builtin_amdgcn_exp2f((lm_to_f32(v[j]) - top) * kLog2e);
-          o[j] = static_cast<E>(e * f - (c + j == y ? s : 0.f));
-        }
-        store_pack<E>(dz + c, C - c, o);
-      }
+      asm volatile("" : "+v"(held[p]));
+      if (p * THREADS + tid < packs) gradient(held[p], p * THREADS + tid);
     }
   } else {
-    for (int c = tid * N; c < C; c += THREADS * N) {
-      const V v = __builtin_bit_cast(V, load_pack<E>(z + c, C - c, low));
-      V o;
-#pragma unroll
-      for (int j = 0; j < N; ++j) {
-        const float e = __builtin_amdgcn_exp2f((lm_to_f32(v[j]) - top) * kLog2e);
-        o[j] = static_cast<E>(e * f - (c + j == y ? s : 0.f));
-      }
-      store_pack<E>(dz + c, C - c, o);
-    }
+    for (int p = tid; p < packs; p += THREADS)
+      gradient(static_cast<lm_u32x4>(*reinterpret_cast<const lm_u32x4_any*>(zb + p * N)), p);
   }
 }
 
+// THREADS to a row (64: four rows to a workgroup).  A held pack takes four
+// registers: as many waves as leave that room without spilling, so that
+// workgroups load, compute and store beside each other.
 template <typename E, int THREADS, int PACKS>
-__global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void k_token_rows(TokenArgs a) {
+__global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS, PACKS <= 4 ? 8 : PACKS <= 8 ? 5 : 4) void k_token_rows(
+    TokenArgs a) {
   __shared__ float lds[THREADS / 64];
   const int tid = THREADS == 64 ? threadIdx.x % 64 : threadIdx.x;
   constexpr int ROWS = THREADS == 64 ? 4 : 1;   // rows of a workgroup
@@ -251,23 +315,37 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void k_token_rows(To
 template <typename E>
 void launch_rows(const TokenArgs& a, hipStream_t s) {
   constexpr int N = Pack<E>::N;
-  const int64_t packs = (a.C + N - 1) / N;
+  const int64_t packs = a.C / N;   // at most, by where the row starts
   // (a launch holds fewer than 2^32 threads: the kernel goes over the rest)
-  const uint32_t T = static_cast<uint32_t>(a.T < kMaxGrid ? a.T : kMaxGrid);
-  if (packs <= 64 * 8)
+  const uint32_t T = static_cast<uint32_t>(std::min(a.T, kMaxGrid));
+  if (packs <= 64 * 2)
+    k_token_rows<E, 64, 2><<<(T + 3) / 4, 256, 0, s>>>(a);
+  else if (packs <= 64 * 8)
     k_token_rows<E, 64, 8><<<(T + 3) / 4, 256, 0, s>>>(a);
+  else if (packs <= 256 * 4)
+    k_token_rows<E, 256, 4><<<T, 256, 0, s>>>(a);
   else if (packs <= 256 * 8)
     k_token_rows<E, 256, 8><<<T, 256, 0, s>>>(a);
-  else if (packs <= 1024 * 8)
-    k_token_rows<E, 1024, 8><<<T, 1024, 0, s>>>(a);
+  else if (packs <= 256 * 16)
+    k_token_rows<E, 256, 16><<<T, 256, 0, s>>>(a);
+  else if (packs <= 512 * 16)
+    k_token_rows<E, 512, 16><<<T, 512, 0, s>>>(a);
+  else if (packs <= 1024 * 16)
+    k_token_rows<E, 1024, 16><<<T, 1024, 0, s>>>(a);
   else
     k_token_rows<E, 1024, 0><<<T, 1024, 0, s>>>(a);
 }
 
 }  // namespace
 
-hipError_t launch_token_loss(const TokenArgs& a, hipStream_t s) {
-  if (a.dZ) k_token_count<<<a.n, 256, 0, s>>>(a.n, a.T, a.offsets, a.y, a.inv);
+hipError_t launch_token_loss(const TokenArgs& args, hipStream_t s) {
+  TokenArgs a = args;
+  // One workgroup goes over 16384 rows in some 10 us; more rows to a worker
+  // are taken in parts.  Up to 1024 rows in all, a row's wave counts its
+  // worker's labels itself (16 loads a lane) and saves a launch.
+  const int64_t rows = a.T / a.n;
+  a.parts = a.T <= 1024 ? 0 : static_cast<int>(std::min<int64_t>(kTokenParts, 1 + rows / 8192));
+  if (a.dZ && a.parts) k_token_count<<<a.n * a.parts, 256, 0, s>>>(a);
   if (a.T) {
     if (a.dtype == DBW_F32)
       launch_rows<float>(a, s);
@@ -276,7 +354,9 @@ hipError_t launch_token_loss(const TokenArgs& a, hipStream_t s) {
     else
       launch_rows<_Float16>(a, s);
   }
-  k_token_mean<<<a.n, 256, 0, s>>>(a.n, a.T, a.offsets, a.row_loss, a.y, a.loss);
+  a.parts = std::max(a.parts, 1);
+  if (a.parts > 1) k_token_sum<<<a.n * a.parts, 256, 0, s>>>(a);
+  k_token_mean<<<a.n, 256, 0, s>>>(a);
   return hipGetLastError();
 }
 

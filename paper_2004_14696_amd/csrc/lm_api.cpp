@@ -106,7 +106,7 @@ constexpr int64_t align256(int64_t b) { return (b + 255) / 256 * 256; }
 
 DBW_API int64_t dbw_token_workspace(int32_t n, int64_t T) {
   if (n < 1 || n > DBW_MAX_N || T < 0 || T >= (int64_t{1} << 31)) return -1;
-  return align256(4 * n) + 4 * T;
+  return int64_t{12} * n * dbw::kTokenParts + 4 * T;
 }
 
 DBW_API dbw_status dbw_token_loss(int32_t n, int64_t T, int32_t C, int32_t dtype, const int32_t* offsets,
@@ -141,8 +141,9 @@ DBW_API dbw_status dbw_token_loss(int32_t n, int64_t T, int32_t C, int32_t dtype
   a.n = n; a.C = C; a.T = T; a.dtype = dtype; a.offsets = offsets;
   a.Z = Z; a.ld_Z = ld_Z; a.y = y; a.scale = static_cast<float>(scale);
   a.dZ = dZ; a.ld_dZ = ld_dZ; a.loss = loss;
-  a.inv = static_cast<float*>(workspace);
-  a.row_loss = reinterpret_cast<float*>(static_cast<char*>(workspace) + align256(4 * n));
+  a.sums = static_cast<double*>(workspace);
+  a.counts = reinterpret_cast<int32_t*>(a.sums + n * dbw::kTokenParts);
+  a.row_loss = reinterpret_cast<float*>(a.counts + n * dbw::kTokenParts);
   const hipError_t err = dbw::launch_token_loss(a, static_cast<hipStream_t>(stream));
   if (err != hipSuccess) return set_free_error(DBW_EHIP, "%s: launch failed: %s", call, hipGetErrorString(err));
   return DBW_OK;

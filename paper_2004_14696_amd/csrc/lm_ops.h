@@ -57,8 +57,11 @@ struct TokenArgs {
   int64_t ld_dZ;
   float* loss;     // [n]
   float* row_loss; // workspace [T]
-  float* inv;      // workspace [n]: 1 / count, 0 without a live row
+  int32_t* counts; // workspace [n][parts]: live rows of a worker's part
+  double* sums;    // workspace [n][parts]: sums of their losses
+  int parts;       // parts of a worker's rows (set by the launch)
 };
+constexpr int kTokenParts = 64;
 hipError_t launch_token_loss(const TokenArgs& a, hipStream_t s);
 
 // ---------------------------------------------------------------------------
