@@ -329,103 +329,110 @@ def grad_stats_static(G, mask, k, g, loss, V_window=0.0, sqnorm=None, stats=None
 
 
 # -- operators for language models ---------------------------------------------
+_codes = None
+
+
 def _dtype_code(torch, dtype, name, allowed):
-    codes = {torch.float32: DBW_F32, torch.bfloat16: DBW_BF16, torch.float16: DBW_F16}
-    if dtype not in codes or codes[dtype] not in allowed:
+    global _codes
+    if _codes is None:
+        _codes = {torch.float32: DBW_F32, torch.bfloat16: DBW_BF16, torch.float16: DBW_F16}
+    code = _codes.get(dtype)
+    if code is None or code not in allowed:
         raise ValueError(f"{name} has an unsupported type: {dtype}")
-    return codes[dtype]
+    return code
 
 
 def _rows_of(t, shape, dtype, dev, name):
     """Pointer and row stride of a tensor [..][rows][columns] with contiguous
     columns."""
-    if t.device != dev or t.dtype != dtype or tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name} must be {dtype} {tuple(shape)} on {dev}, not {t.dtype} {tuple(t.shape)} on {t.device}")
-    if t.shape[-1] > 1 and t.stride(-1) != 1:
+    if t.device != dev or t.dtype != dtype or t.shape != shape:
+        raise ValueError(f"{name} must be {dtype} {shape} on {dev}, not {t.dtype} {tuple(t.shape)} on {t.device}")
+    strides = t.stride()
+    if strides[-1] != 1 and shape[-1] > 1:
         raise ValueError(f"the last dimension of {name} must be contiguous")
     # a single row has no stride of its own
-    return t.data_ptr(), t.stride(-2) if t.shape[-2] > 1 else t.shape[-1]
+    return t.data_ptr(), strides[-2] if shape[-2] > 1 else shape[-1]
 
 
 def _flat(t, shape, dtype, dev, name):
-    if t.device != dev or t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+    if t.device != dev or t.dtype != dtype or t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {dev}")
     return t.data_ptr()
 
 
-class _On:
-    """The device of a call's tensors made current, and its stream."""
+def _stream_of(torch, dev, stream):
+    """The raw handle of `stream`, or of the current stream of `dev`."""
+    if dev.type != "cuda":
+        raise ValueError(f"tensors must live on a GPU, not {dev}")
+    return torch._C._cuda_getCurrentRawStream(dev.index) if stream is None else stream.cuda_stream
 
-    def __init__(self, torch, dev, stream):
-        if dev.type != "cuda":
-            raise ValueError(f"tensors must live on a GPU, not {dev}")
-        self.switch = torch.cuda.device(dev) if torch.cuda.current_device() != dev.index else None
-        self.stream = torch.cuda.current_stream(dev) if stream is None else stream
 
-    def __enter__(self):
-        if self.switch is not None:
-            self.switch.__enter__()
-        return self.stream
-
-    def __exit__(self, *exc):
-        if self.switch is not None:
-            self.switch.__exit__(*exc)
+def _call(torch, lib, dev, function, *args):
+    """function(*args) with `dev` as the current device; raises its error."""
+    if torch.cuda.current_device() == dev.index:
+        st = function(*args)
+    else:
+        with torch.cuda.device(dev):
+            st = function(*args)
+    if st != DBW_OK:
+        raise DBWError(st, lib.dbw_last_error(None).decode())
 
 
 def _workspace(torch, nbytes, dev, workspace):
+    """Pointer, size and tensor of a workspace of at least nbytes."""
     if workspace is None:
-        return torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
-    if workspace.device != dev or not workspace.is_contiguous():
+        if nbytes <= 0:
+            return None, 0, None
+        workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+    elif workspace.device != dev or not workspace.is_contiguous():
         raise ValueError(f"workspace must be a contiguous tensor on {dev}")
-    return workspace
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
 
 
-def _group(form, a, b, offsets, out, out_dtype, W_shape, workspace, stream):
+_HALVES = (DBW_BF16, DBW_F16)
+_FLOATS = (DBW_F32, DBW_BF16, DBW_F16)
+
+
+def _group(form, a, b, offsets, out, out_dtype, d, C, workspace, stream):
     torch = _torch()
     lib = load_library()
-    dev = a.device
+    dev, dtype = a.device, a.dtype
     if offsets.dim() != 1 or offsets.numel() < 2:
         raise ValueError("offsets must be [n + 1]")
-    n = offsets.numel() - 1
-    po = _flat(offsets, (n + 1,), torch.int32, dev, "offsets")
     if a.dim() != 2:
         raise ValueError("token rows must be [T][columns]")
-    T = a.shape[0]
+    n, T = offsets.numel() - 1, a.shape[0]
+    po = _flat(offsets, (n + 1,), torch.int32, dev, "offsets")
     if out_dtype is None:
-        out_dtype = a.dtype if out is None else out.dtype
-    d, C = W_shape
-    names = {DBW_GROUP_FORWARD: ("X", "W", "Y"), DBW_GROUP_INPUT_GRAD: ("dY", "W", "dX"),
-             DBW_GROUP_WEIGHT_GRAD: ("X", "dY", "G")}[form]
-    s = GroupShape(form=form, dtype=_dtype_code(torch, a.dtype, names[0], (DBW_BF16, DBW_F16)),
-                   out_dtype=_dtype_code(torch, out_dtype, "the output", (DBW_F32, DBW_BF16, DBW_F16)),
-                   n=n, d=d, C=C, T=T)
+        out_dtype = dtype if out is None else out.dtype
+    codes = _dtype_code(torch, dtype, "the inputs", _HALVES), _dtype_code(torch, out_dtype, "the output", _FLOATS)
+    raw = _stream_of(torch, dev, stream)
     if form == DBW_GROUP_WEIGHT_GRAD:
-        out = torch.empty((n, d, C), dtype=out_dtype, device=dev) if out is None else out
-        pa, s.ld_d = _rows_of(a, (T, d), a.dtype, dev, "X")
-        pb, s.ld_C = _rows_of(b, (T, C), a.dtype, dev, "dY")
-        pc, s.ld_W = _rows_of(out, (n, d, C), out_dtype, dev, "G")
-        s.st_W = out.stride(0)
+        if out is None:
+            out = torch.empty((n, d, C), dtype=out_dtype, device=dev)
+        pa, ld_d = _rows_of(a, (T, d), dtype, dev, "X")
+        pb, ld_C = _rows_of(b, (T, C), dtype, dev, "dY")
+        pc, ld_W = _rows_of(out, (n, d, C), out_dtype, dev, "G")
+        st_W = out.stride(0)
     else:
-        K, N = (d, C) if form == DBW_GROUP_FORWARD else (C, d)
-        out = torch.empty((T, N), dtype=out_dtype, device=dev) if out is None else out
-        pa, lda = _rows_of(a, (T, K), a.dtype, dev, names[0])
-        pb, s.ld_W = _rows_of(b, (n, d, C) if b.dim() == 3 else (d, C), a.dtype, dev, "W")
-        pc, ldo = _rows_of(out, (T, N), out_dtype, dev, names[2])
-        s.ld_d, s.ld_C = (lda, ldo) if form == DBW_GROUP_FORWARD else (ldo, lda)
+        forward = form == DBW_GROUP_FORWARD
+        K, N = (d, C) if forward else (C, d)
+        if out is None:
+            out = torch.empty((T, N), dtype=out_dtype, device=dev)
+        pa, lda = _rows_of(a, (T, K), dtype, dev, "X" if forward else "dY")
+        pb, ld_W = _rows_of(b, (n, d, C) if b.dim() == 3 else (d, C), dtype, dev, "W")
+        pc, ldo = _rows_of(out, (T, N), out_dtype, dev, "Y" if forward else "dX")
+        ld_d, ld_C = (lda, ldo) if forward else (ldo, lda)
         # one matrix for all groups has no distance to the next one
-        s.st_W = b.stride(0) if b.dim() == 3 else 0
-        if b.dim() == 3 and n == 1:
-            s.st_W = 0
-    with _On(torch, dev, stream) as on:
-        need = c_int64()
-        st = lib.dbw_group_workspace(ctypes.byref(s), ctypes.byref(need))
-        if st != DBW_OK:
-            raise DBWError(st, lib.dbw_last_error(None).decode())
-        ws = _workspace(torch, need.value, dev, workspace)
-        st = lib.dbw_group_product(ctypes.byref(s), po, pa, pb, pc, ws.data_ptr() if ws is not None else None,
-                                   ws.numel() * ws.element_size() if ws is not None else 0, on.cuda_stream)
+        st_W = b.stride(0) if b.dim() == 3 and n > 1 else 0
+    shape = GroupShape(form, codes[0], codes[1], n, d, C, T, ld_d, ld_C, ld_W, st_W)
+    ref = ctypes.byref(shape)
+    need = c_int64()
+    st = lib.dbw_group_workspace(ref, ctypes.byref(need))
     if st != DBW_OK:
         raise DBWError(st, lib.dbw_last_error(None).decode())
+    pw, nbytes, keep = _workspace(torch, need.value, dev, workspace)
+    _call(torch, lib, dev, lib.dbw_group_product, ref, po, pa, pb, pc, pw, nbytes, raw)
     return out
 
 
@@ -437,7 +444,8 @@ def group_matmul(X, W, offsets, out=None, out_dtype=None, workspace=None, stream
     what ``out`` held."""
     if W.dim() not in (2, 3):
         raise ValueError("W must be [n][d][C] or [d][C]")
-    return _group(DBW_GROUP_FORWARD, X, W, offsets, out, out_dtype, tuple(W.shape[-2:]), workspace, stream)
+    d, C = W.shape[-2:]
+    return _group(DBW_GROUP_FORWARD, X, W, offsets, out, out_dtype, d, C, workspace, stream)
 
 
 def group_input_grad(dY, W, offsets, out=None, out_dtype=None, workspace=None, stream=None):
@@ -445,7 +453,8 @@ def group_input_grad(dY, W, offsets, out=None, out_dtype=None, workspace=None, s
     (dbw_group_product, INPUT_GRAD).  Returns dX [T][d]."""
     if W.dim() not in (2, 3):
         raise ValueError("W must be [n][d][C] or [d][C]")
-    return _group(DBW_GROUP_INPUT_GRAD, dY, W, offsets, out, out_dtype, tuple(W.shape[-2:]), workspace, stream)
+    d, C = W.shape[-2:]
+    return _group(DBW_GROUP_INPUT_GRAD, dY, W, offsets, out, out_dtype, d, C, workspace, stream)
 
 
 def group_weight_grad(X, dY, offsets, out=None, out_dtype=None, workspace=None, stream=None):
@@ -455,10 +464,9 @@ def group_weight_grad(X, dY, offsets, out=None, out_dtype=None, workspace=None, 
     in ``out_dtype`` (float32 unless given)."""
     if dY.dim() != 2 or X.dim() != 2:
         raise ValueError("X must be [T][d] and dY [T][C]")
-    torch = _torch()
     if out_dtype is None:
-        out_dtype = torch.float32 if out is None else out.dtype
-    return _group(DBW_GROUP_WEIGHT_GRAD, X, dY, offsets, out, out_dtype, (X.shape[1], dY.shape[1]), workspace, stream)
+        out_dtype = _torch().float32 if out is None else out.dtype
+    return _group(DBW_GROUP_WEIGHT_GRAD, X, dY, offsets, out, out_dtype, X.shape[1], dY.shape[1], workspace, stream)
 
 
 def token_loss(Z, y, offsets, scale=1.0, dZ=None, loss=None, grad=True, workspace=None, stream=None):
@@ -469,28 +477,24 @@ def token_loss(Z, y, offsets, scale=1.0, dZ=None, loss=None, grad=True, workspac
     Z, to write the gradient in its place; ``grad`` False: no gradient (None)."""
     torch = _torch()
     lib = load_library()
-    dev = Z.device
+    dev, dtype = Z.device, Z.dtype
     if Z.dim() != 2 or offsets.dim() != 1 or offsets.numel() < 2:
         raise ValueError("Z must be [T][C] and offsets [n + 1]")
     T, C = Z.shape
     n = offsets.numel() - 1
-    code = _dtype_code(torch, Z.dtype, "Z", (DBW_F32, DBW_BF16, DBW_F16))
+    code = _dtype_code(torch, dtype, "Z", _FLOATS)
+    raw = _stream_of(torch, dev, stream)
     po = _flat(offsets, (n + 1,), torch.int32, dev, "offsets")
     py = _flat(y, (T,), torch.int32, dev, "y")
-    pz, ld_Z = _rows_of(Z, (T, C), Z.dtype, dev, "Z")
+    pz, ld_Z = _rows_of(Z, (T, C), dtype, dev, "Z")
     if dZ is None and grad:
-        dZ = torch.empty((T, C), dtype=Z.dtype, device=dev)
-    pd, ld_dZ = _rows_of(dZ, (T, C), Z.dtype, dev, "dZ") if dZ is not None else (None, 0)
-    loss = torch.empty(n, dtype=torch.float32, device=dev) if loss is None else loss
+        dZ = torch.empty((T, C), dtype=dtype, device=dev)
+    pd, ld_dZ = _rows_of(dZ, (T, C), dtype, dev, "dZ") if dZ is not None else (None, 0)
+    if loss is None:
+        loss = torch.empty(n, dtype=torch.float32, device=dev)
     pl = _flat(loss, (n,), torch.float32, dev, "loss")
-    with _On(torch, dev, stream) as on:
-        need = lib.dbw_token_workspace(n, T)
-        ws = _workspace(torch, max(need, 0), dev, workspace)
-        st = lib.dbw_token_loss(n, T, C, code, po, pz, ld_Z, py, float(scale), pd, ld_dZ, pl,
-                                ws.data_ptr() if ws is not None else None,
-                                ws.numel() * ws.element_size() if ws is not None else 0, on.cuda_stream)
-    if st != DBW_OK:
-        raise DBWError(st, lib.dbw_last_error(None).decode())
+    pw, nbytes, keep = _workspace(torch, lib.dbw_token_workspace(n, T), dev, workspace)
+    _call(torch, lib, dev, lib.dbw_token_loss, n, T, C, code, po, pz, ld_Z, py, scale, pd, ld_dZ, pl, pw, nbytes, raw)
     return loss, dZ
 
 
@@ -565,11 +569,9 @@ class AdamW:
             t.lr_scale, t.weight_decay = float(scale[i]), float(decay[i])
         self.device = dev
         self._keep = (w, lists)      # the plan holds their addresses
+        _stream_of(torch, dev, None)
         handle = c_void_p()
-        with _On(torch, dev, None):
-            st = self.lib.dbw_adamw_create(ctypes.byref(cfg), table, ctypes.byref(handle))
-        if st != DBW_OK:
-            raise DBWError(st, self.lib.dbw_last_error(None).decode())
+        _call(torch, self.lib, dev, self.lib.dbw_adamw_create, ctypes.byref(cfg), table, ctypes.byref(handle))
         self.h = handle
 
     def step(self, lr, beta1=0.9, beta2=0.999, eps=1e-8, max_norm=0.0, grad_scale=1.0, seed=0, norm=None, stream=None):
@@ -583,10 +585,8 @@ class AdamW:
         pn = _flat(norm, norm.shape, torch.float32, self.device, "norm") if norm is not None else None
         if norm is not None and norm.numel() != 1:
             raise ValueError("norm must have one element")
-        hyper = AdamWHyper(lr=lr, beta1=beta1, beta2=beta2, eps=eps, grad_scale=grad_scale, max_norm=max_norm,
-                           seed=int(seed) & 0xFFFFFFFF)
-        with _On(torch, self.device, stream) as on:
-            st = self.lib.dbw_adamw_step(self.h, ctypes.byref(hyper), pn, on.cuda_stream)
+        hyper = AdamWHyper(lr, beta1, beta2, eps, grad_scale, max_norm, int(seed) & 0xFFFFFFFF)
+        st = self.lib.dbw_adamw_step(self.h, ctypes.byref(hyper), pn, _stream_of(torch, self.device, stream))
         if st != DBW_OK:
             raise DBWError(st, self.lib.dbw_last_error(None).decode())
         return norm
