@@ -514,6 +514,16 @@ dbw_status dbw_adamw_step(dbw_adamw* opt, const dbw_adamw_hyper* hyper, float* n
 dbw_status dbw_adamw_export(dbw_adamw* opt, int64_t* t);
 dbw_status dbw_adamw_import(dbw_adamw* opt, int64_t t);
 
+/* AdamW as the server's update of dbw_step: from now on, and until another
+ * call, each dbw_step on ctx ends with one step of opt (with hyper, copied) on
+ * the context's stream instead of w <- w - eta g_t; opt NULL brings that back.
+ * The gradients of opt's tensors must lie in the context's g_t
+ * (dbw_step_outputs, a buffer that stays where it is), each at the place that
+ * its w has in the w passed to dbw_step (DBW_EINVAL there otherwise); what no
+ * tensor covers is not updated.  opt must be on the context's device and
+ * outlive this use.  The estimator's formulas keep cfg.eta. */
+dbw_status dbw_set_adamw(dbw_ctx* ctx, dbw_adamw* opt, const dbw_adamw_hyper* hyper);
+
 /* The 32 random bits of value `index` of tensor `tensor` at step t (HOST; the
  * low 16 round m, the high 16 round r).  With mix(x): x ^= x >> 16, x *=
  * 0x9E3779B1, x ^= x >> 15, x *= 0xB7E15163, x ^= x >> 16 in 32 bits, they are

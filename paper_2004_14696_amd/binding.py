@@ -43,7 +43,7 @@ EXPORTED = (
     "dbw_grad_stats_static", "dbw_grads_route",
     "dbw_group_workspace", "dbw_group_product", "dbw_token_workspace", "dbw_token_loss",
     "dbw_adamw_create", "dbw_adamw_destroy", "dbw_adamw_step", "dbw_adamw_export", "dbw_adamw_import",
-    "dbw_adamw_bits",
+    "dbw_adamw_bits", "dbw_set_adamw",
 )
 DBW_STATIC_SCRATCH_BYTES = 8 * 1024 * 1024
 
@@ -193,6 +193,8 @@ def load_library(path: str = LIB_PATH):
     lib.dbw_adamw_export.restype = st
     lib.dbw_adamw_import.argtypes = [P, c_int64]
     lib.dbw_adamw_import.restype = st
+    lib.dbw_set_adamw.argtypes = [P, P, POINTER(AdamWHyper)]
+    lib.dbw_set_adamw.restype = st
     lib.dbw_adamw_bits.argtypes = [c_uint32, c_int64, c_int32, c_int64]
     lib.dbw_adamw_bits.restype = c_uint32
     _lib = lib
@@ -640,6 +642,14 @@ def _torch():
     return torch
 
 
+class _DeviceArray:
+    """float32 [n] device memory of a context, for torch.as_tensor."""
+
+    def __init__(self, owner, ptr, n):
+        self.owner = owner
+        self.__cuda_array_interface__ = {"shape": (n,), "typestr": "<f4", "data": (ptr, False), "version": 2}
+
+
 class Context:
     """One DBW parameter-server simulation bound to a torch CUDA (HIP) stream."""
 
@@ -765,6 +775,22 @@ class Context:
                                       ticks.ctypes.data_as(POINTER(c_int64)),
                                       ctypes.byref(kout) if wait else None), "dbw_step")
         return int(kout.value) if wait else None
+
+    def gradient(self):
+        """The context's g_t [P], which every step writes (a view, valid while
+        the context is open): the gradients of a plan for use_adamw."""
+        bufs = StepBuffers()
+        self._check(self.lib.dbw_step_outputs(self.h, ctypes.byref(bufs)), "dbw_step_outputs")
+        return _torch().as_tensor(_DeviceArray(self, bufs.g, self.P), device=self.device)
+
+    def use_adamw(self, opt, lr=0.0, beta1=0.9, beta2=0.999, eps=1e-8, max_norm=0.0, grad_scale=1.0, seed=0):
+        """From now on every step updates w by one step of ``opt`` (an AdamW
+        whose gradients are slices of gradient(), in the places that its w have
+        in the w of step) instead of by SGD; None: by SGD again."""
+        hyper = AdamWHyper(lr, beta1, beta2, eps, grad_scale, max_norm, int(seed) & 0xFFFFFFFF)
+        self._check(self.lib.dbw_set_adamw(self.h, opt.h if opt is not None else None, ctypes.byref(hyper)),
+                    "dbw_set_adamw")
+        self._adamw = opt            # the plan outlives its use
 
     def step_outputs(self):
         """Copies of the buffers the last step wrote (torch tensors)."""

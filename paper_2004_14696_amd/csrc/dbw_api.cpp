@@ -24,6 +24,7 @@
 #include "dbw.h"
 #include "dbw_buffer.h"
 #include "dbw_internal.h"
+#include "lm_ops.h"
 
 #define DBW_API extern "C" __attribute__((visibility("default")))
 
@@ -147,6 +148,11 @@ struct dbw_ctx {
   std::atomic<int> job_state{0};    // 0 none, 1 posted, 2 finished
   dbw_status job_status = DBW_OK;
   std::string job_error;
+
+  // dbw_set_adamw: the server's update, and the w that its plan updates
+  dbw_adamw* adamw = nullptr;
+  dbw_adamw_hyper adamw_hyper{};
+  const float* adamw_w = nullptr;
 
   bool profiling = false;      // host timers
   bool prof_events = false;    // device events
@@ -829,6 +835,8 @@ DBW_API dbw_status dbw_step(dbw_ctx* c, float* w, const float* X, const int32_t*
   if (!aligned16(w)) return fail(c, DBW_EINVAL, "w must be 16-byte aligned");
   if (dbw_status s = check_batch(c, X, y, rows); s != DBW_OK) return s;
   if (!ticks_host) return fail(c, DBW_EINVAL, "ticks_host is NULL");
+  if (c->adamw && c->adamw_w && w != c->adamw_w)
+    return fail(c, DBW_EINVAL, "w is not the one that the plan of dbw_set_adamw updates");
   const int n = c->cfg.n;
   for (int i = 0; i < n; ++i)
     if (ticks_host[i] < 0) return fail(c, DBW_EINVAL, "tick of worker %d is negative", i);
@@ -908,7 +916,7 @@ DBW_API dbw_status dbw_step(dbw_ctx* c, float* w, const float* X, const int32_t*
     ca.do_choose = 1; ca.do_select = 1; ca.k_out = c->k; ca.b_out = c->b;
     ca.objective = c->objective; ca.sel = c->sel; ca.mask = c->mask; ca.err = c->err;
     dbw::AggArgs aa{};
-    aa.G = c->Ga; aa.P = c->P; aa.n = n; aa.sel = c->sel; aa.k_dev = c->k; aa.g_out = c->g; aa.w = w;
+    aa.G = c->Ga; aa.P = c->P; aa.n = n; aa.sel = c->sel; aa.k_dev = c->k; aa.g_out = c->g; aa.w = c->adamw ? nullptr : w;
     aa.eta = static_cast<float>(c->cfg.eta); aa.sqpart = c->sqpart; aa.part = c->part; aa.mode = dbw::AGG_FUSED;
     if (c->copy_rows) aa.G_rows = c->G;
     if (slab) {
@@ -943,6 +951,9 @@ DBW_API dbw_status dbw_step(dbw_ctx* c, float* w, const float* X, const int32_t*
       ps.emplace(c, DBW_KT_AGGREGATE);
     }
     if (!fused) HIP_TRY(c, dbw::launch_aggregate(aa, c->stream));
+    if (c->adamw)
+      if (dbw_status s = dbw_adamw_step(c->adamw, &c->adamw_hyper, nullptr, c->stream); s != DBW_OK)
+        return fail(c, s, "%s", dbw_last_error(nullptr));
     // T_hat_{t+1} on the worker now (it needs this iteration's ticks, stored
     // above, and k_{t-1}); the rest of the queueing overlaps its solve
     c->t = t + 1;
@@ -960,6 +971,24 @@ DBW_API dbw_status dbw_step(dbw_ctx* c, float* w, const float* X, const int32_t*
     HIP_TRY(c, hipEventSynchronize(c->ev_fin));
     *k_host = c->h_k[slot];
   }
+  return DBW_OK;
+}
+
+DBW_API dbw_status dbw_set_adamw(dbw_ctx* c, dbw_adamw* opt, const dbw_adamw_hyper* hyper) {
+  if (!c) return DBW_EINVAL;
+  if (!opt) {
+    c->adamw = nullptr;
+    return DBW_OK;
+  }
+  if (!hyper) return fail(c, DBW_EINVAL, "hyper is NULL");
+  std::string why;
+  const float* w = nullptr;
+  if (dbw_status s = dbw::adamw_check(*hyper, &why); s != DBW_OK) return fail(c, s, "%s", why.c_str());
+  if (dbw_status s = dbw::adamw_place(opt, c->device, c->g, c->P, &w, &why); s != DBW_OK)
+    return fail(c, s, "%s", why.c_str());
+  c->adamw = opt;
+  c->adamw_hyper = *hyper;
+  c->adamw_w = w;
   return DBW_OK;
 }
 

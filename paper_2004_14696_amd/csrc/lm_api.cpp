@@ -159,7 +159,45 @@ struct dbw_adamw {
   double* parts = nullptr;
   dbw::AdamTensor* tensors = nullptr;
   dbw::AdamChunk* chunks = nullptr;
+  std::vector<dbw_adamw_tensor> list;   // the caller's description
 };
+
+dbw_status dbw::adamw_place(const dbw_adamw* o, int device, const float* g, int64_t P, const float** w,
+                            std::string* why) {
+  if (o->device != device) {
+    *why = "the plan is on another device";
+    return DBW_EINVAL;
+  }
+  if (o->cfg.g_dtype != DBW_F32) {
+    *why = "the context's gradient is fp32, the plan's are not";
+    return DBW_EINVAL;
+  }
+  *w = nullptr;
+  for (size_t i = 0; i < o->list.size(); ++i) {
+    const dbw_adamw_tensor& t = o->list[i];
+    if (!t.count) continue;
+    const float* tg = static_cast<const float*>(t.g);
+    const bool inside = tg >= g && t.count <= P && tg - g <= P - t.count;
+    const float* base = inside ? t.w - (tg - g) : nullptr;
+    if (!inside || (*w && base != *w)) {
+      *why = "tensor " + std::to_string(i) + (inside ? ": its w has another place than its gradient in g"
+                                                     : ": its gradient is not in the context's g");
+      return DBW_EINVAL;
+    }
+    *w = base;
+  }
+  return DBW_OK;
+}
+
+dbw_status dbw::adamw_check(const dbw_adamw_hyper& h, std::string* why) {
+  if (!(h.lr >= 0.0) || !std::isfinite(h.lr)) *why = "lr is finite and >= 0";
+  else if (!(h.beta1 >= 0.0 && h.beta1 < 1.0 && h.beta2 >= 0.0 && h.beta2 < 1.0)) *why = "beta1 and beta2 lie in [0, 1)";
+  else if (!(h.eps >= 1e-30) || !std::isfinite(h.eps)) *why = "eps is at least 1e-30";
+  else if (!std::isfinite(h.grad_scale)) *why = "grad_scale is not finite";
+  else if (!(h.max_norm >= 0.0) || !std::isfinite(h.max_norm)) *why = "max_norm is finite and >= 0";
+  else return DBW_OK;
+  return DBW_EINVAL;
+}
 
 DBW_API dbw_status dbw_adamw_create(const dbw_adamw_config* cfg, const dbw_adamw_tensor* tensors, dbw_adamw** out) {
   const char* call = "dbw_adamw_create";
@@ -207,6 +245,7 @@ DBW_API dbw_status dbw_adamw_create(const dbw_adamw_config* cfg, const dbw_adamw
   std::vector<char> host;
   try {
     host.resize(all);
+    o->list.assign(tensors, tensors + cfg->tensors);
   } catch (const std::exception&) {
     delete o;
     return set_free_error(DBW_EHIP, "%s: out of host memory", call);
@@ -248,13 +287,9 @@ DBW_API void dbw_adamw_destroy(dbw_adamw* o) {
 DBW_API dbw_status dbw_adamw_step(dbw_adamw* o, const dbw_adamw_hyper* h, float* norm, void* stream) {
   const char* call = "dbw_adamw_step";
   if (!o || !h) return set_free_error(DBW_EINVAL, "%s: a pointer is NULL", call);
-  if (!(h->lr >= 0.0) || !std::isfinite(h->lr)) return set_free_error(DBW_EINVAL, "%s: lr is finite and >= 0", call);
-  if (!(h->beta1 >= 0.0 && h->beta1 < 1.0 && h->beta2 >= 0.0 && h->beta2 < 1.0))
-    return set_free_error(DBW_EINVAL, "%s: beta1 and beta2 lie in [0, 1)", call);
-  if (!(h->eps >= 1e-30) || !std::isfinite(h->eps)) return set_free_error(DBW_EINVAL, "%s: eps is at least 1e-30", call);
-  if (!std::isfinite(h->grad_scale)) return set_free_error(DBW_EINVAL, "%s: grad_scale is not finite", call);
-  if (!(h->max_norm >= 0.0) || !std::isfinite(h->max_norm))
-    return set_free_error(DBW_EINVAL, "%s: max_norm is finite and >= 0", call);
+  std::string why;
+  if (dbw_status st = dbw::adamw_check(*h, &why); st != DBW_OK)
+    return set_free_error(st, "%s: %s", call, why.c_str());
   if (!aligned(norm, 4)) return set_free_error(DBW_EINVAL, "%s: norm is not aligned", call);
   OnDevice on(o->device);
   dbw::AdamArgs a{};

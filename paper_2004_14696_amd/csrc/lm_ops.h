@@ -5,6 +5,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
+#include <string>
 
 #include "dbw.h"
 
@@ -105,6 +106,11 @@ struct AdamArgs {
   float* norm;      // nullable
 };
 hipError_t launch_adamw(const AdamArgs& a, hipStream_t s);
+
+// For dbw_set_adamw: the w at whose place the gradient buffer g [P] stands for
+// all tensors of a plan; the failing tensor's number and reason in *why.
+dbw_status adamw_place(const dbw_adamw* o, int device, const float* g, int64_t P, const float** w, std::string* why);
+dbw_status adamw_check(const dbw_adamw_hyper& h, std::string* why);
 
 // Rounding bits (see dbw_adamw_bits).
 __host__ __device__ inline uint32_t adam_mix(uint32_t x) {

@@ -710,6 +710,72 @@ def test_a_heads_training_steps_captured(bits):
         assert all(torch.equal(x, z) for x, z in zip(a, b))
 
 
+STEP_MODELS = [("softmax", dict(n=5, B=32, d=60, C=7), "none"), ("softmax", dict(n=64, B=256, d=200, C=10), "none"),
+               ("softmax", dict(n=4, B=64, d=2048, C=120), "selected"), ("mlp", dict(n=6, B=32, d=50, H=40, C=5), "all")]
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("model,kw,g_rows", STEP_MODELS)
+def test_dbw_step_with_adamw_as_the_servers_update(model, kw, g_rows, bits):
+    # every step of the simulation, with AdamW on parts of w, against an AdamW
+    # step by hand on the g that the simulation made; the choice and the
+    # statistics are those of SGD
+    n, d, C = kw["n"], kw["d"], kw["C"]
+    g = gen(41)
+    X = torch.rand((n, kw["B"], d), generator=g, device="cuda")
+    y = torch.randint(0, C, (n, kw["B"]), generator=g, device="cuda", dtype=torch.int32)
+    ctx = pb.Context(pb.make_config(model, g_rows=g_rows, **kw))
+    other = pb.Context(pb.make_config(model, g_rows=g_rows, **kw))
+    P = ctx.P
+    cut = P // 3 + 1
+    w = normal(g, (P,), torch.float32, 0.05)
+    frozen = w[-5:].clone()
+
+    def parts(x):
+        return [x[:cut], x[cut:P - 5]]
+    st = pb.adamw_states(parts(w), bits)
+    opt = pb.AdamW(parts(w), parts(ctx.gradient()), **st, weight_decay=[0.0, 0.1])
+    hand_w, hand_g = w.clone(), torch.empty_like(w)
+    hand_st = pb.adamw_states(parts(hand_w), bits)
+    hand = pb.AdamW(parts(hand_w), parts(hand_g), **hand_st, weight_decay=[0.0, 0.1])
+    hyper = dict(lr=0.01, max_norm=0.5, seed=9)
+    ctx.use_adamw(opt, **hyper)
+    for t in range(4):
+        ticks = np.random.default_rng(t).integers(1, 1000, n)
+        w_sgd = w.clone()
+        k = ctx.step(w, X, y, ticks, wait=True)
+        out = ctx.step_outputs()
+        ctx.sync()
+        hand_g.copy_(out["g"])
+        hand.step(**hyper)
+        assert torch.equal(w, hand_w) and bool(torch.isfinite(w).all()) and not torch.equal(w, w_sgd)
+        assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for m in st for a, b in zip(st[m], hand_st[m]))
+        if t == 0:   # the first iteration of a context that updates by SGD has the same k and g
+            assert other.step(w_sgd, X, y, ticks, wait=True) == k
+            other.sync()
+            assert torch.equal(other.step_outputs()["g"], out["g"])
+    assert torch.equal(w[-5:], frozen) and opt.t == 4
+    # a w that the plan does not update, and a plan that does not fit
+    with pytest.raises(pb.DBWError):
+        ctx.step(hand_w, X, y, ticks)
+    four = pb.adamw_states([w[:4], w[4:8]])
+    for bad in (pb.AdamW(parts(w), parts(hand_g), **st),
+                pb.AdamW([w[:4], w[4:8]], [ctx.gradient()[:4], ctx.gradient()[5:9]], **four),
+                pb.AdamW([w[:4], w[4:8]], [w[:4].half(), w[4:8].half()], **four)):
+        with pytest.raises(pb.DBWError):
+            ctx.use_adamw(bad, lr=0.1)
+    with pytest.raises(pb.DBWError):
+        ctx.use_adamw(opt, lr=-1.0)
+    # and back to SGD
+    ctx.use_adamw(None)
+    before = hand_w.clone()
+    ctx.step(hand_w, X, y, ticks)
+    ctx.sync()
+    step = before.double() - 0.1 * ctx.step_outputs()["g"].double()
+    assert bool(((hand_w.double() - step).abs() <= 4 * u * (before.double().abs() + step.abs() + 1e-3)).all())
+    assert opt.t == 4
+
+
 def test_calls_on_another_stream_and_twice_give_the_same_bits():
     g = gen(33)
     T, d, C, n = 900, 256, 520, 7
