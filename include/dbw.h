@@ -480,7 +480,7 @@ typedef struct {
   void *m, *v;      /* DEVICE [count]                                        */
   uint8_t *m_scale, *v_scale; /* DEVICE; NULL with 32-bit states             */
   void* w_low;      /* DEVICE [count] of low_dtype, or NULL                  */
-  int64_t count;    /* >= 0                                                  */
+  int64_t count;    /* >= 0; of all tensors together at most 2^36              */
   double lr_scale, weight_decay; /* finite, >= 0                             */
 } dbw_adamw_tensor;
 typedef struct {

@@ -1,7 +1,7 @@
 // AdamW over many tensors: one step is
 //   k_adamw_norm   (only where a norm is asked for) sums of squares of g,
 //   k_adamw_prep   one workgroup: t, the norm, the clip factor, 1 - beta^t,
-//   k_adamw_update every tensor, a workgroup to a chunk of 4096 values.
+//   k_adamw_update every tensor, a workgroup to a chunk of 1024 values.
 //
 // The update is bound by memory: 8 bytes of w, 16 (32-bit states) or 4 + 1/64
 // (8-bit) of states, and the gradient, each moved once; some 60 vector
@@ -24,6 +24,7 @@ namespace dbw {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kNormChunks = 4;   // chunks that a workgroup of the norm has in flight
 
 template <typename G>
 struct Vec4;   // four gradients
@@ -159,20 +160,21 @@ __global__ __launch_bounds__(kThreads) void k_adamw_norm(const AdamTensor* __res
   // squares and their sums in 64 bits: products of two fp32 values are exact
   // there, and neither overflow nor a long sum loses the small tensors
   double sum = 0.0;
-  for (int64_t c = blockIdx.x; c < nchunks; c += gridDim.x) {
-    const AdamChunk ch = chunks[c];
-    const G* g = static_cast<const G*>(tensors[ch.tensor].g);
-    const int64_t first = static_cast<int64_t>(ch.index) * kAdamChunk;
-    const int64_t left = tensors[ch.tensor].count - first;
+  for (int64_t c = static_cast<int64_t>(blockIdx.x) * kNormChunks; c < nchunks;
+       c += static_cast<int64_t>(gridDim.x) * kNormChunks) {
+    float x[kNormChunks][4];
 #pragma unroll
-    for (int it = 0; it < kAdamChunk / (kThreads * 4); ++it) {
-      const int at = (it * kThreads + threadIdx.x) * 4;
-      if (at >= left) continue;
-      float x[4];
-      load4(g + first + at, static_cast<int>(left - at < 4 ? left - at : 4), x);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) sum += static_cast<double>(x[j]) * static_cast<double>(x[j]);
+    for (int q = 0; q < kNormChunks; ++q) {
+      // (behind the last chunk: that one again, with nothing left of it)
+      const AdamChunk ch = chunks[c + q < nchunks ? c + q : nchunks - 1];
+      const int64_t at = static_cast<int64_t>(ch.index) * kAdamChunk + threadIdx.x * 4;
+      const int64_t left = c + q < nchunks ? tensors[ch.tensor].count - at : 0;
+      load4(static_cast<const G*>(tensors[ch.tensor].g) + at, static_cast<int>(left < 4 ? left : 4), x[q]);
     }
+#pragma unroll
+    for (int q = 0; q < kNormChunks; ++q)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) sum += static_cast<double>(x[q][j]) * static_cast<double>(x[q][j]);
   }
 #pragma unroll
   for (int d = 32; d; d /= 2) sum += __shfl_xor(sum, d);
@@ -228,63 +230,61 @@ __global__ __launch_bounds__(kThreads) void k_adamw_update(const AdamTensor* __r
   const float b1 = static_cast<float>(h.beta1), c1 = static_cast<float>(1.0 - h.beta1);
   const float b2 = static_cast<float>(h.beta2), c2 = static_cast<float>(1.0 - h.beta2);
   const uint32_t key = BITS == 8 ? adam_mix(step->key + static_cast<uint32_t>(ch.tensor)) : 0;
+  static_assert(kAdamChunk == kThreads * 4, "four values a thread");
+  const int at = static_cast<int>(threadIdx.x) * 4;
+  // whole waves leave together: encode() reduces over a wave
+  if ((at & ~(kAdamBlock - 1)) >= left) return;
+  const int64_t i = first + at;
+  const int n = left - at >= 4 ? 4 : left - at > 0 ? static_cast<int>(left - at) : 0;
+  float w[4], g[4], m[4], v[4];
+  load4(t.w + i, n, w);
+  load4(static_cast<const G*>(t.g) + i, n, g);
+  if (BITS == 32) {
+    load4(static_cast<const float*>(t.m) + i, n, m);
+    load4(static_cast<const float*>(t.v) + i, n, v);
+  } else {
+    const int64_t b = i / kAdamBlock;
+    decode(load_codes(static_cast<const uint8_t*>(t.m) + i, n), t.m_scale[b], m);
+    decode(load_codes(static_cast<const uint8_t*>(t.v) + i, n), t.v_scale[b], v);
 #pragma unroll
-  for (int it = 0; it < kAdamChunk / (kThreads * 4); ++it) {
-    const int at = (it * kThreads + static_cast<int>(threadIdx.x)) * 4;
-    // whole waves leave together: encode() reduces over a wave
-    if ((at & ~(kAdamBlock - 1)) >= left) continue;
-    const int64_t i = first + at;
-    const int n = left - at >= 4 ? 4 : left - at > 0 ? static_cast<int>(left - at) : 0;
-    float w[4], g[4], m[4], v[4];
-    load4(t.w + i, n, w);
-    load4(static_cast<const G*>(t.g) + i, n, g);
-    if (BITS == 32) {
-      load4(static_cast<const float*>(t.m) + i, n, m);
-      load4(static_cast<const float*>(t.v) + i, n, v);
-    } else {
-      const int64_t b = i / kAdamBlock;
-      decode(load_codes(static_cast<const uint8_t*>(t.m) + i, n), t.m_scale[b], m);
-      decode(load_codes(static_cast<const uint8_t*>(t.v) + i, n), t.v_scale[b], v);
+    for (int j = 0; j < 4; ++j) v[j] = v[j] * v[j];
+  }
+  float r[4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) v[j] = v[j] * v[j];
-    }
-    float r[4];
+  for (int j = 0; j < 4; ++j) {
+    const float x = g[j] * f;
+    m[j] = m[j] * b1 + x * c1;
+    v[j] = v[j] * b2 + x * x * c2;
+    r[j] = sqrtf(v[j]);
+    w[j] = w[j] * keep - m[j] / (r[j] * ibc2 + eps) * rate;
+  }
+  store4(t.w + i, n, w);
+  if (t.low) {
+    if (low_dtype == DBW_BF16)
+      store4_half(static_cast<__bf16*>(t.low) + i, n, w);
+    else
+      store4_half(static_cast<_Float16*>(t.low) + i, n, w);
+  }
+  if (BITS == 32) {
+    store4(static_cast<float*>(t.m) + i, n, m);
+    store4(static_cast<float*>(t.v) + i, n, v);
+  } else {
+    uint32_t lo[4], hi[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const float x = g[j] * f;
-      m[j] = m[j] * b1 + x * c1;
-      v[j] = v[j] * b2 + x * x * c2;
-      r[j] = sqrtf(v[j]);
-      w[j] = w[j] * keep - m[j] / (r[j] * ibc2 + eps) * rate;
+      const uint32_t u = adam_mix(adam_index(i + j) + key);
+      lo[j] = u & 0xffffu;
+      hi[j] = u >> 16;
+      if (j >= n) m[j] = r[j] = 0.f;   // beyond the tensor: no part in the scale
     }
-    store4(t.w + i, n, w);
-    if (t.low) {
-      if (low_dtype == DBW_BF16)
-        store4_half(static_cast<__bf16*>(t.low) + i, n, w);
-      else
-        store4_half(static_cast<_Float16*>(t.low) + i, n, w);
-    }
-    if (BITS == 32) {
-      store4(static_cast<float*>(t.m) + i, n, m);
-      store4(static_cast<float*>(t.v) + i, n, v);
-    } else {
-      uint32_t lo[4], hi[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const uint32_t u = adam_mix(adam_index(i + j) + key);
-        lo[j] = u & 0xffffu;
-        hi[j] = u >> 16;
-        if (j >= n) m[j] = r[j] = 0.f;   // beyond the tensor: no part in the scale
-      }
-      uint32_t em, ev;
-      const uint32_t cm = encode<false>(m, lo, &em), cv = encode<true>(r, hi, &ev);
-      store_codes(static_cast<uint8_t*>(t.m) + i, n, cm);
-      store_codes(static_cast<uint8_t*>(t.v) + i, n, cv);
-      if (threadIdx.x % 64 == 0) {
-        const int64_t b = i / kAdamBlock;
-        t.m_scale[b] = static_cast<uint8_t>(em);
-        t.v_scale[b] = static_cast<uint8_t>(ev);
-      }
+    uint32_t em, ev;
+    const uint32_t cm = encode<false>(m, lo, &em), cv = encode<true>(r, hi, &ev);
+    store_codes(static_cast<uint8_t*>(t.m) + i, n, cm);
+    store_codes(static_cast<uint8_t*>(t.v) + i, n, cv);
+    if (threadIdx.x % 64 == 0) {
+      const int64_t b = i / kAdamBlock;
+      t.m_scale[b] = static_cast<uint8_t>(em);
+      t.v_scale[b] = static_cast<uint8_t>(ev);
     }
   }
 }
@@ -292,15 +292,18 @@ __global__ __launch_bounds__(kThreads) void k_adamw_update(const AdamTensor* __r
 template <typename G>
 hipError_t launch(const AdamArgs& a, hipStream_t s) {
   const bool norm = a.norm || a.h.max_norm > 0.0;
-  const int parts = norm ? static_cast<int>(a.nchunks < kAdamNormParts ? a.nchunks : kAdamNormParts) : 0;
+  const int64_t groups = (a.nchunks + kNormChunks - 1) / kNormChunks;
+  const int parts = norm ? static_cast<int>(groups < kAdamNormParts ? groups : kAdamNormParts) : 0;
   if (parts) k_adamw_norm<G><<<parts, kThreads, 0, s>>>(a.tensors, a.chunks, a.nchunks, a.parts);
   k_adamw_prep<<<1, kThreads, 0, s>>>(a.step, a.parts, parts, a.h, a.norm);
-  if (a.nchunks) {
-    const uint32_t grid = static_cast<uint32_t>(a.nchunks);
+  // (a launch holds fewer than 2^32 threads)
+  constexpr int64_t kMost = int64_t{1} << 23;
+  for (int64_t first = 0; first < a.nchunks; first += kMost) {
+    const uint32_t grid = static_cast<uint32_t>(a.nchunks - first < kMost ? a.nchunks - first : kMost);
     if (a.bits == 8)
-      k_adamw_update<G, 8><<<grid, kThreads, 0, s>>>(a.tensors, a.chunks, a.step, a.h, a.low_dtype);
+      k_adamw_update<G, 8><<<grid, kThreads, 0, s>>>(a.tensors, a.chunks + first, a.step, a.h, a.low_dtype);
     else
-      k_adamw_update<G, 32><<<grid, kThreads, 0, s>>>(a.tensors, a.chunks, a.step, a.h, a.low_dtype);
+      k_adamw_update<G, 32><<<grid, kThreads, 0, s>>>(a.tensors, a.chunks + first, a.step, a.h, a.low_dtype);
   }
   return hipGetLastError();
 }

@@ -552,7 +552,7 @@ __global__ __launch_bounds__(256) void k_group_sum(GroupArgs g, const float* __r
     const int left = N - n < 4 ? static_cast<int>(N - n) : 4;
     f32x4 x = {0.f, 0.f, 0.f, 0.f};
     if (left == 4) {
-#pragma unroll 4
+#pragma unroll 8
       for (int s = 0; s < g.splits; ++s) x += *reinterpret_cast<const lm_f32x4_any*>(p + s * g.part);
     } else {
       for (int s = 0; s < g.splits; ++s)

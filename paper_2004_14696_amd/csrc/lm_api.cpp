@@ -229,10 +229,8 @@ DBW_API dbw_status dbw_adamw_create(const dbw_adamw_config* cfg, const dbw_adamw
       return set_free_error(DBW_EUNSUPPORTED, "%s: tensor %d: count above 2^40", call, i);
     nchunks += (t.count + dbw::kAdamChunk - 1) / dbw::kAdamChunk;
   }
-  // (a launch holds fewer than 2^32 threads)
-  if (nchunks >= (int64_t{1} << 24))
-    return set_free_error(DBW_EUNSUPPORTED, "%s: %lld chunks of %d values: 2^24 or more", call, (long long)nchunks,
-                          dbw::kAdamChunk);
+  if (nchunks > (int64_t{1} << 26))
+    return set_free_error(DBW_EUNSUPPORTED, "%s: more than 2^26 chunks of %d values", call, dbw::kAdamChunk);
   dbw_adamw* o = new (std::nothrow) dbw_adamw;
   if (!o) return set_free_error(DBW_EHIP, "%s: out of host memory", call);
   o->cfg = *cfg;

@@ -68,7 +68,7 @@ hipError_t launch_token_loss(const TokenArgs& a, hipStream_t s);
 // ---------------------------------------------------------------------------
 // AdamW.
 constexpr int kAdamBlock = 256;    // values of one scale (8-bit states): a wave, four values a lane
-constexpr int kAdamChunk = 4096;   // values of one tensor that a workgroup updates
+constexpr int kAdamChunk = 1024;   // values of one tensor that a workgroup updates
 constexpr int kAdamNormParts = 2048;
 
 struct AdamTensor {

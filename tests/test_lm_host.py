@@ -100,7 +100,7 @@ def test_adamw_refusals(lib):
         assert create(**kw) == pb.DBW_EINVAL, kw
         assert lib.dbw_last_error(None).startswith(b"dbw_adamw_create")
     assert create(count=(1 << 40) + 1) == pb.DBW_EUNSUPPORTED
-    assert create(count=1 << 37) == pb.DBW_EUNSUPPORTED      # 2^25 chunks
+    assert create(count=1 << 37) == pb.DBW_EUNSUPPORTED      # 2^27 chunks of 1024
     assert lib.dbw_adamw_create(None, None, None) == pb.DBW_EINVAL
     h = pb.AdamWHyper(lr=1e-3, beta1=0.9, beta2=0.99, eps=1e-8, grad_scale=1.0)
     assert lib.dbw_adamw_step(None, ctypes.byref(h), None, None) == pb.DBW_EINVAL
