@@ -9,6 +9,7 @@ fallback implementation.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from ctypes import POINTER, c_double, c_int32, c_int64, c_size_t, c_uint8, c_uint32, c_void_p
 
@@ -362,11 +363,18 @@ def _flat(t, shape, dtype, dev, name):
     return t.data_ptr()
 
 
-def _stream_of(torch, dev, stream):
-    """The raw handle of `stream`, or of the current stream of `dev`."""
+def _stream_of(torch, dev):
+    """The raw handle of the current stream of `dev`."""
     if dev.type != "cuda":
         raise ValueError(f"tensors must live on a GPU, not {dev}")
-    return torch._C._cuda_getCurrentRawStream(dev.index) if stream is None else stream.cuda_stream
+    return torch._C._cuda_getCurrentRawStream(dev.index)
+
+
+def _on(stream, function, *args, **kw):
+    """function with `stream` as the current one, so that what it allocates
+    belongs to that stream."""
+    with _torch().cuda.stream(stream):
+        return function(*args, **kw)
 
 
 def _call(torch, lib, dev, function, *args):
@@ -395,7 +403,21 @@ _HALVES = (DBW_BF16, DBW_F16)
 _FLOATS = (DBW_F32, DBW_BF16, DBW_F16)
 
 
-def _group(form, a, b, offsets, out, out_dtype, d, C, workspace, stream):
+@functools.lru_cache(maxsize=512)
+def _group_shape(*sizes):
+    """A dbw_group_shape, by reference, and its bytes of workspace."""
+    lib = load_library()
+    ref = ctypes.byref(GroupShape(*sizes))
+    need = c_int64()
+    st = lib.dbw_group_workspace(ref, ctypes.byref(need))
+    if st != DBW_OK:
+        raise DBWError(st, lib.dbw_last_error(None).decode())
+    return ref, need.value
+
+
+def _group(form, a, b, offsets, out, out_dtype, d, C, workspace, stream=None):
+    if stream is not None:
+        return _on(stream, _group, form, a, b, offsets, out, out_dtype, d, C, workspace)
     torch = _torch()
     lib = load_library()
     dev, dtype = a.device, a.dtype
@@ -408,7 +430,7 @@ def _group(form, a, b, offsets, out, out_dtype, d, C, workspace, stream):
     if out_dtype is None:
         out_dtype = dtype if out is None else out.dtype
     codes = _dtype_code(torch, dtype, "the inputs", _HALVES), _dtype_code(torch, out_dtype, "the output", _FLOATS)
-    raw = _stream_of(torch, dev, stream)
+    raw = _stream_of(torch, dev)
     if form == DBW_GROUP_WEIGHT_GRAD:
         if out is None:
             out = torch.empty((n, d, C), dtype=out_dtype, device=dev)
@@ -427,13 +449,8 @@ def _group(form, a, b, offsets, out, out_dtype, d, C, workspace, stream):
         ld_d, ld_C = (lda, ldo) if forward else (ldo, lda)
         # one matrix for all groups has no distance to the next one
         st_W = b.stride(0) if b.dim() == 3 and n > 1 else 0
-    shape = GroupShape(form, codes[0], codes[1], n, d, C, T, ld_d, ld_C, ld_W, st_W)
-    ref = ctypes.byref(shape)
-    need = c_int64()
-    st = lib.dbw_group_workspace(ref, ctypes.byref(need))
-    if st != DBW_OK:
-        raise DBWError(st, lib.dbw_last_error(None).decode())
-    pw, nbytes, keep = _workspace(torch, need.value, dev, workspace)
+    ref, need = _group_shape(form, codes[0], codes[1], n, d, C, T, ld_d, ld_C, ld_W, st_W)
+    pw, nbytes, keep = _workspace(torch, need, dev, workspace)
     _call(torch, lib, dev, lib.dbw_group_product, ref, po, pa, pb, pc, pw, nbytes, raw)
     return out
 
@@ -477,6 +494,8 @@ def token_loss(Z, y, offsets, scale=1.0, dZ=None, loss=None, grad=True, workspac
     labels (negative: the row is masked), offsets [n+1] int32.  Returns
     (loss [n] float32, dZ [T][C] of the type of Z, times ``scale``); dZ may be
     Z, to write the gradient in its place; ``grad`` False: no gradient (None)."""
+    if stream is not None:
+        return _on(stream, token_loss, Z, y, offsets, scale, dZ, loss, grad, workspace)
     torch = _torch()
     lib = load_library()
     dev, dtype = Z.device, Z.dtype
@@ -485,7 +504,7 @@ def token_loss(Z, y, offsets, scale=1.0, dZ=None, loss=None, grad=True, workspac
     T, C = Z.shape
     n = offsets.numel() - 1
     code = _dtype_code(torch, dtype, "Z", _FLOATS)
-    raw = _stream_of(torch, dev, stream)
+    raw = _stream_of(torch, dev)
     po = _flat(offsets, (n + 1,), torch.int32, dev, "offsets")
     py = _flat(y, (T,), torch.int32, dev, "y")
     pz, ld_Z = _rows_of(Z, (T, C), dtype, dev, "Z")
@@ -571,7 +590,7 @@ class AdamW:
             t.lr_scale, t.weight_decay = float(scale[i]), float(decay[i])
         self.device = dev
         self._keep = (w, lists)      # the plan holds their addresses
-        _stream_of(torch, dev, None)
+        _stream_of(torch, dev)
         handle = c_void_p()
         _call(torch, self.lib, dev, self.lib.dbw_adamw_create, ctypes.byref(cfg), table, ctypes.byref(handle))
         self.h = handle
@@ -581,6 +600,8 @@ class AdamW:
         their norm (over all tensors).  Returns the norm before clipping, a
         float32 scalar tensor, where max_norm or ``norm`` (a tensor to write
         it to) is given, else None."""
+        if stream is not None:
+            return _on(stream, self.step, lr, beta1, beta2, eps, max_norm, grad_scale, seed, norm)
         torch = _torch()
         if norm is None and max_norm:
             norm = torch.empty((), dtype=torch.float32, device=self.device)
@@ -588,7 +609,7 @@ class AdamW:
         if norm is not None and norm.numel() != 1:
             raise ValueError("norm must have one element")
         hyper = AdamWHyper(lr, beta1, beta2, eps, grad_scale, max_norm, int(seed) & 0xFFFFFFFF)
-        st = self.lib.dbw_adamw_step(self.h, ctypes.byref(hyper), pn, _stream_of(torch, self.device, stream))
+        st = self.lib.dbw_adamw_step(self.h, ctypes.byref(hyper), pn, _stream_of(torch, self.device))
         if st != DBW_OK:
             raise DBWError(st, self.lib.dbw_last_error(None).decode())
         return norm

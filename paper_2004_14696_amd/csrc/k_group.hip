@@ -50,6 +50,7 @@ struct Tile {
   int64_t lda, ldb, ldo;
   int k0, k1;
   int rows, cols;
+  int line_a, line_b;   // values of a line of either matrix
 };
 
 // One operand's part of a step: L outputs x BK terms, by THREADS threads.
@@ -192,46 +193,91 @@ struct Direct {
   }
 };
 
-// Loads of a step through registers, for lines at any address and of any
-// length.
-template <typename Op, typename E, int BK>
+// v >> 16 s, for s in 1 .. 7.
+__device__ __forceinline__ lm_u32x4 shift_halves(const lm_u32x4& v, int s) {
+  uint64_t lo = v[0] | static_cast<uint64_t>(v[1]) << 32, hi = v[2] | static_cast<uint64_t>(v[3]) << 32;
+  if (s >= 4) {
+    lo = hi;
+    hi = 0;
+  }
+  const int r = 16 * (s & 3);
+  if (r) {
+    lo = lo >> r | hi << (64 - r);
+    hi >>= r;
+  }
+  return lm_u32x4{static_cast<uint32_t>(lo), static_cast<uint32_t>(lo >> 32), static_cast<uint32_t>(hi),
+                  static_cast<uint32_t>(hi >> 32)};
+}
+
+// Loads of one step after the other through registers, for lines at any
+// address and of any length.  A chunk that a line ends in is the line's last
+// eight values, shifted when it goes to LDS: as many loads as whole chunks
+// take, and no branch around any.  `total` values make a line of the matrix.
+template <typename Op, typename E, int BK, bool SWAP>
 struct Staged {
+  const E* p;                  // eight values before the next step's first term
+  int64_t ld, step;
+  int length, total;
+  int shift, end;              // of the step held: values that the last chunk lacks, its first place
+  uint32_t off[Op::CHUNKS];
   lm_u32x4 held[Op::CHUNKS];
-  template <bool SWAP>
-  __device__ __forceinline__ void load(const E* p, int64_t ld, int k, int k1, int length, int tid) {
-    const E* base = SWAP ? p + k * ld : p + k;
-    const int left = k1 - k;
-    const __amdgpu_buffer_rsrc_t r = make_rsrc(base, static_cast<uint32_t>(kMaxBufferBytes));
-    // whole chunks in one load each, at any alignment, without a branch
+  __device__ __forceinline__ uint32_t offset(int left, int tid, int i) const {
+    const int at = Op::line(tid, i), first = Op::chunk(tid, i) * 8, in_line = SWAP ? length : left;
+    if (at >= (SWAP ? left : length) || first >= in_line) return kOutOfRange;
+    return static_cast<uint32_t>((at * ld + 8 + (first + 8 <= in_line ? first : in_line - 8)) * 2);
+  }
+  __device__ __forceinline__ Staged(const E* first, int64_t ld_, int length_, int total_, int k0, int tid)
+      : p((SWAP ? first + k0 * ld_ : first + k0) - 8), ld(ld_), step(SWAP ? BK * ld_ : BK), length(length_),
+        total(total_) {
 #pragma unroll
-    for (int i = 0; i < Op::CHUNKS; ++i) {
-      const int at = Op::line(tid, i), first = Op::chunk(tid, i) * 8;
-      const bool whole = at < (SWAP ? left : length) && first + 8 <= (SWAP ? length : left);
-      held[i] = __builtin_bit_cast(lm_u32x4, __builtin_amdgcn_raw_buffer_load_b128(
-                                                 r, whole ? static_cast<uint32_t>((at * ld + first) * 2) : kOutOfRange, 0, 0));
-    }
-    // and those that a line ends in, value by value
-    if ((SWAP ? length : left) < (SWAP ? Op::LINE * 8 : BK)) {
+    for (int i = 0; i < Op::CHUNKS; ++i) off[i] = offset(BK, tid, i);
+  }
+  __device__ __forceinline__ void load(int left, int tid) {
+    const __amdgpu_buffer_rsrc_t r = make_rsrc(p, static_cast<uint32_t>(kMaxBufferBytes));
+    const int in_line = SWAP ? length : left;
+    shift = 0;
+    if (total >= 8) {
+      if (in_line < Op::LINE * 8) {
+        shift = -in_line & 7;
+        end = in_line & ~7;
+      }
+      if (left >= BK) {
+#pragma unroll
+        for (int i = 0; i < Op::CHUNKS; ++i)
+          held[i] = __builtin_bit_cast(lm_u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, off[i], 0, 0));
+      } else {
+#pragma unroll
+        for (int i = 0; i < Op::CHUNKS; ++i)
+          held[i] = __builtin_bit_cast(lm_u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, offset(left, tid, i), 0, 0));
+      }
+    } else {
+      // a matrix of fewer than eight columns: value by value
 #pragma unroll
       for (int i = 0; i < Op::CHUNKS; ++i) {
         const int at = Op::line(tid, i), first = Op::chunk(tid, i) * 8;
-        const int in_line = (SWAP ? length : left) - first;
-        if (at < (SWAP ? left : length) && in_line > 0 && in_line < 8) {
-          const E* q = base + at * ld + first;
-          typedef E V __attribute__((ext_vector_type(8)));
-          V x = __builtin_bit_cast(V, lm_u32x4{0, 0, 0, 0});
 #pragma unroll
-          for (int j = 0; j < 7; ++j)
-            if (j < in_line) x[j] = q[j];
-          held[i] = __builtin_bit_cast(lm_u32x4, x);
+        for (int j = 0; j < 4; ++j) held[i][j] = 0;
+#pragma unroll
+        for (int j = 0; j < 7; ++j) {
+          const bool in = at < (SWAP ? left : length) && first + j < in_line;
+          const uint32_t x = __builtin_amdgcn_raw_buffer_load_b16(
+              r, in ? static_cast<uint32_t>((at * ld + 8 + first + j) * 2) : kOutOfRange, 0, 0);
+          held[i][j / 2] |= (x & 0xffffu) << (16 * (j % 2));
         }
       }
     }
+    p += step;
   }
   __device__ __forceinline__ void store(char* lds, int tid) const {
 #pragma unroll
-    for (int i = 0; i < Op::CHUNKS; ++i)
-      *reinterpret_cast<lm_u32x4*>(lds + (i * Op::STEP * Op::LINE + tid) * 16) = held[i];
+    for (int i = 0; i < Op::CHUNKS; ++i) {
+      lm_u32x4 v = held[i];
+      if (shift) {
+        const lm_u32x4 w = shift_halves(v, shift);
+        v = Op::chunk(tid, i) * 8 == end ? w : v;
+      }
+      *reinterpret_cast<lm_u32x4*>(lds + (i * Op::STEP * Op::LINE + tid) * 16) = v;
+    }
   }
 };
 
@@ -381,12 +427,12 @@ __device__ __forceinline__ void product(const Tile& t, bool out_f32, char* lds) 
       wait_step<0>();
     }
   } else {
-    Staged<OpA, E, BK> A;
-    Staged<OpB, E, BK> B;
-    int k = t.k0, left = t.k1 - t.k0;
-    const auto load = [&](int from) {
-      A.template load<A_SWAP>(a, t.lda, from, t.k1, t.rows, tid);
-      B.template load<B_SWAP>(b, t.ldb, from, t.k1, t.cols, tid);
+    Staged<OpA, E, BK, A_SWAP> A(a, t.lda, t.rows, t.line_a, t.k0, tid);
+    Staged<OpB, E, BK, B_SWAP> B(b, t.ldb, t.cols, t.line_b, t.k0, tid);
+    int left = t.k1 - t.k0;
+    const auto load = [&](int of) {
+      A.load(of, tid);
+      B.load(of, tid);
     };
     const auto store = [&](int slot) {
       A.store(lds + slot * STAGE, tid);
@@ -394,10 +440,10 @@ __device__ __forceinline__ void product(const Tile& t, bool out_f32, char* lds) 
       __syncthreads();
     };
     if (left > 0) {
-      load(k);
+      load(left);
       store(0);
       for (int slot = 0; left > 0; slot ^= 1, left -= BK) {
-        if (left > BK) load(k += BK);
+        if (left > BK) load(left - BK);
         multiply(lds + slot * STAGE, std::integral_constant<int, 0>{});
         if (left > BK) store(slot ^ 1);
       }
@@ -458,6 +504,8 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64, 2) void k_group(GroupAr
     t.b = static_cast<const E*>(g.b) + n;
     t.lda = g.ld_d;
     t.ldb = g.ld_C;
+    t.line_a = g.d;
+    t.line_b = g.C;
     t.k0 = static_cast<int>(first + std::min<int64_t>(length, split * step));
     t.k1 = static_cast<int>(first + std::min<int64_t>(length, (split + 1) * step));
     t.rows = std::min(BM, g.d - m);
@@ -517,6 +565,8 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64, 2) void k_group(GroupAr
     const int64_t step = split_of(K, g.splits);
     t.lda = FORM == DBW_GROUP_FORWARD ? g.ld_d : g.ld_C;
     t.ldb = g.ld_W;
+    t.line_a = K;
+    t.line_b = g.C;
     t.a = static_cast<const E*>(g.a) + row * t.lda;
     t.b = static_cast<const E*>(g.b) + group * g.st_W + (FORM == DBW_GROUP_FORWARD ? n : n * g.ld_W);
     t.k0 = static_cast<int>(std::min<int64_t>(K, split * step));

@@ -103,6 +103,7 @@ SIZES = [
     # d, C, lengths: one token, empty groups, odd widths, tiles that end inside
     (64, 64, [1]), (8, 8, [1, 0, 2]), (64, 128, [3, 0, 0, 5]), (40, 72, [33, 31, 1]),
     (1, 1, [5, 2]), (7, 3, [1, 9]), (65, 129, [130, 1, 63]), (130, 255, [64, 65]),
+    (9, 15, [70, 3]), (136, 201, [129, 1]), (71, 66, [300]), (8, 9, [1, 2]), (77, 8, [64, 65]), (2, 260, [40]),
     (264, 520, [300, 17]), (512, 256, [700, 100, 513]), (200, 1000, [0, 0, 0]), (96, 40, [2000]),
 ]
 
@@ -795,9 +796,14 @@ def test_calls_on_another_stream_and_twice_give_the_same_bits():
     other.wait_stream(torch.cuda.current_stream())
     with torch.cuda.stream(other):
         there = all_of()
+    # a stream given to the calls: their memory is that stream's, and what the
+    # current stream allocates and fills meanwhile is not it
+    given = all_of(stream=other)
+    noise = [torch.full((T, C), 7.0, device="cuda") for _ in range(8)]
     torch.cuda.synchronize()
-    for a, b, c in zip(first, again, there):
-        assert torch.equal(a, b) and torch.equal(a, c)
+    assert all(float(x[0, 0]) == 7.0 for x in noise)
+    for a, b, c, e in zip(first, again, there, given):
+        assert torch.equal(a, b) and torch.equal(a, c) and torch.equal(a, e)
 
 
 def test_offsets_that_break_the_rules_stay_inside():
