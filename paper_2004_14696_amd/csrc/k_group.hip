@@ -20,6 +20,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include "dbw_buffer.h"
@@ -627,7 +628,6 @@ __global__ __launch_bounds__(256) void k_group_sum(GroupArgs g, const float* __r
   }
 }
 
-constexpr int64_t kTarget = 512;
 enum GroupVariant { SMALL = 0, MIDDLE = 1, LARGE = 2 };
 struct VariantSize {
   int bm, bn;
@@ -673,7 +673,7 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 namespace {
 
-// The plan with a given variant; splits = 0: as many as fill the GPU.
+// The plan with a given variant and number of parts of the sum.
 GroupPlan plan_of(const dbw_group_shape& p, int variant, int splits) {
   GroupPlan plan;
   const bool grad = p.form == DBW_GROUP_WEIGHT_GRAD;
@@ -687,26 +687,82 @@ GroupPlan plan_of(const dbw_group_shape& p, int variant, int splits) {
                         : std::min<int64_t>(p.T, p.T / size.bm + std::min<int64_t>(groups, p.T));
   plan.col_tiles = ceil_div(N, size.bn);
   plan.tiles = std::max<int64_t>(1, ceil_div(rows, size.bm) * plan.col_tiles * groups);
-  const int64_t K = grad ? p.T / p.n : p.form == DBW_GROUP_FORWARD ? p.d : p.C;
-  plan.splits = splits ? splits
-                       : static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({kTarget / plan.tiles, K / 256, 64})));
+  plan.splits = splits;
   plan.part = grad ? static_cast<int64_t>(p.n) * p.d * p.C : p.T * N;
   plan.blocks = plan.row_tiles * plan.col_tiles * plan.splits * (grad ? p.n : 1);
   return plan;
 }
 
+// Terms of the sum, on average.
+int64_t terms(const dbw_group_shape& p) {
+  return p.form == DBW_GROUP_WEIGHT_GRAD ? p.T / p.n : p.form == DBW_GROUP_FORWARD ? p.d : p.C;
+}
+
+// The best plan of a variant for Y and dX, by an estimate of its time in us:
+//   steps of 64 terms, whose time was measured with one workgroup on a CU and
+//   with two (1 x 1024 x 1024 x 1024 and 1 x 2048 x 1024 x 1024 with 32 x 128, 1 x 4096 x
+//   1024 x 4096 and x 8192 with 128 x 128), for as many rounds as the tiles of
+//   ragged groups take;
+//   or the weights' way from memory, once for every row tile, where they are
+//   larger than caches hold beside the rest (16 groups of 16 and 64 rows 2048 x 2048: 27 us with
+//   32 x 128 and 50 against 39 us with 128 x 128);
+//   and the sum of the parts: a launch, and the parts written and read.
+struct Estimate {
+  GroupPlan plan;
+  double us;
+};
+Estimate best_plan(const dbw_group_shape& p, int variant) {
+  const bool small = variant == SMALL;
+  const double one = small ? 0.33 : 0.75, two = small ? 0.53 : 1.05;   // us a step
+  Estimate best{plan_of(p, variant, 1), 0.0};
+  const double groups = p.st_W == 0 ? 1 : p.n, rows = p.T / groups;
+  // a group ends, on average, in the middle of a tile
+  const double row_tiles = groups > 1 ? std::max(1.0, rows / kSize[variant].bm + 0.5)
+                                      : static_cast<double>(ceil_div(p.T, kSize[variant].bm));
+  const double tiles = groups * row_tiles * best.plan.col_tiles, K = static_cast<double>(terms(p));
+  const double weights = 2.0 * groups * p.d * p.C, traffic = weights > 64e6 ? weights * row_tiles : 0.0;
+  const int most = static_cast<int>(std::max(1.0, std::min({512 / tiles, K / 256, 64.0})));
+  for (int s = 1; s <= most; ++s) {
+    const double blocks = tiles * s, rounds = blocks <= 512 ? 1.0 : std::ceil(blocks / 512);
+    const double step = blocks <= 256 ? one : two * rounds;
+    const double rate = small ? 5.0e6 * std::min(1.0, blocks / 192) : blocks <= 256 ? 3.0e6 : 4.5e6;   // bytes a us
+    const double sum = s > 1 ? 5.0 + 0.2 * s + 1e-6 * s * best.plan.part : 0.0;
+    const double us = std::max(K / 64 / s * step, traffic / rate) + sum;
+    if (s == 1 || us < best.us) best = Estimate{plan_of(p, variant, s), us};
+  }
+  return best;
+}
+
 }  // namespace
 
 GroupPlan group_plan(const dbw_group_shape& p) {
-  const bool grad = p.form == DBW_GROUP_WEIGHT_GRAD;
-  const int64_t groups = p.st_W == 0 && !grad ? 1 : p.n;
-  const GroupPlan middle = plan_of(p, MIDDLE, 0);
-  if (!grad && (p.T / groups <= 32 || middle.tiles <= 128)) return plan_of(p, SMALL, 0);
-  if (p.form != DBW_GROUP_INPUT_GRAD) {
-    const GroupPlan large = plan_of(p, LARGE, 1);
-    if (large.tiles >= 384) return large;
+  if (p.form == DBW_GROUP_WEIGHT_GRAD) {
+    // 128 x 256: more products a value read, from one and a half tiles a CU on
+    // (1 x 4096 x 1024 x 8192: 81 us either way; 32 groups 8192 x 2048 x 1536: 104
+    // against 121 us).  Below, parts of the sum for one workgroup a CU, each
+    // with 256 terms at least; a second one a CU is lost again to the sum of
+    // the parts (1 x 4096 x 1024 x 4096: 56 against 48 us) but with very few tiles
+    // (2 x 15000 x 512 x 512, 32 tiles: 38 against 46 us).
+    if (const GroupPlan large = plan_of(p, LARGE, 1); large.tiles >= 384) return large;
+    const GroupPlan middle = plan_of(p, MIDDLE, 1);
+    const int64_t target = middle.tiles <= 32 ? 512 : 256;
+    return plan_of(p, MIDDLE,
+                   static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({target / middle.tiles, terms(p) / 256, 64}))));
   }
-  return middle;
+  // Y in tiles of 128 x 256 from one and a half a CU on (1 x 4096 x 1024 x 4096, 512
+  // tiles: 37 against 47 us; 1 x 2560 x 1024 x 4096, 320 tiles: 32 against 33 us; 1 x
+  // 4096 x 1024 x 2048, 256 tiles: 25 against 23 us).  Not dX: both operands are
+  // read in lines of the sum there, which 32 terms a step cut in halves (32
+  // groups 8192 x 2048 x 1536: 85 against 75 us).
+  const int64_t groups = p.st_W == 0 ? 1 : p.n;
+  if (const GroupPlan large = plan_of(p, LARGE, 1);
+      p.form == DBW_GROUP_FORWARD && large.tiles >= 384 && p.T / groups > 32)
+    return large;
+  // 32 x 128 for groups of few rows, which a taller tile would mostly leave
+  // empty (16 groups of 2 rows 2048 x 1408: 19 against 22 us), and where it is
+  // estimated to take less time.
+  const Estimate small = best_plan(p, SMALL), middle = best_plan(p, MIDDLE);
+  return p.T / groups <= 32 || small.us <= middle.us ? small.plan : middle.plan;
 }
 
 hipError_t launch_group(const dbw_group_shape& p, GroupPlan plan, const int32_t* offsets, const void* a,
