@@ -10,7 +10,19 @@
 // are zeros in LDS, in both operands: NaN and infinities there reach no sum.
 //
 // Steps are pipelined: while one is multiplied, the loads of the next STAGES -
-// 1 are in flight, straight into LDS, with one barrier a step.
+// 1 are in flight, straight into LDS, with one barrier a step.  Two workgroups
+// share a CU, so that one multiplies while the other waits, loads its first
+// steps or stores (256 x 256 tiles, one workgroup a CU: 319 us where 128 x 256
+// take 258, head 4096 x 1024 x 32000).
+//
+// What bounds it: long sums, the matrix cores, busy 64% of the cycles at 8192
+// terms (1200 TFLOP/s; a library product of 8192^3 reaches 1210), the rest LDS
+// reads and barriers; head 4096 x 1024 x 32000 258 us, 1040 TFLOP/s.  Ragged
+// groups, how evenly their tiles fall on the CUs: 32 groups 8192 x 2048 x 1536 80
+// us, 650 TFLOP/s and 3.3 TB/s.  G of short minibatches, its stores: 16 workers
+// 8000 x 784 x 4000 78 us (200 MB; streamed past the caches 123 us became 107 for
+// 32 groups, in pieces of 16 bytes instead of lines they had taken 163).  Few
+// rows, the weights from memory: 16 groups 37 x 2048 x 1408 16.6 us, 5.6 TB/s.
 //
 // v_mfma_f32_16x16x32 takes, in lane l = 16 g + c, row c and terms 8 g .. 8 g
 // + 7 of each operand; its result r of a lane is row 4 g + r of the first

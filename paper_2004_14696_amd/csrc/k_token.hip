@@ -12,6 +12,13 @@
 // operations a value, against a second read of the row).  Rows beyond what a
 // workgroup's registers hold are read a second time.
 //
+// A row takes as few threads as hold it in 16 packs each, so that two or more
+// workgroups share a CU and one's exponentials run beside another's loads and
+// stores: 8192 x 50257 bf16 330 us, 5.0 TB/s (a large copy reaches 4.9), where 1024
+// threads of 8 packs, alone on a CU, took 542.  Rows of up to 131072 16-bit
+// values fill a CU by themselves (2048 x 128000 fp16 233 us, 4.5 TB/s), longer ones
+// are read twice (1024 x 200000 bf16 239 us, 3.4 TB/s by their size).
+//
 // softmax(z)_c = 2^(b z_c - b max) / sum 2^(b z - b max) with b = log2(e), in
 // fp32: one fused multiply-add and one exponential a value.  b max is rounded;
 // that factor is the same above and below, and is taken out of the loss.
