@@ -347,11 +347,18 @@ void launch_rows(const TokenArgs& a, hipStream_t s) {
 
 hipError_t launch_token_loss(const TokenArgs& args, hipStream_t s) {
   TokenArgs a = args;
-  // One workgroup goes over 16384 rows in some 10 us; more rows to a worker
-  // are taken in parts.  Up to 1024 rows in all, a row's wave counts its
+  // Parts by all rows, not by a worker's even share, as one may have them all:
+  // 65536 x 100 bf16, 16 workers, all rows to one, 145 us in one part and 58 in
+  // several (evenly shared 49 and 45).  At most 4096 parts in all: 900 workers pay
+  // 4 to 7 us for four parts when they share evenly (65536 rows 64 and 70) and
+  // save 67 when one has all (166 and 99).  A second part costs a launch: 16384
+  // rows of 16 workers 21 us for 19 evenly shared, 31 for 40 all to one; hence
+  // none up to 8192 rows, but for a worker that has them all for certain (8192
+  // rows 21 us for 25).  Up to 1024 rows in all, a row's wave counts its
   // worker's labels itself (16 loads a lane) and saves a launch.
-  const int64_t rows = a.T / a.n;
-  a.parts = a.T <= 1024 ? 0 : static_cast<int>(std::min<int64_t>(kTokenParts, 1 + rows / 8192));
+  const int64_t most = std::min<int64_t>(kTokenParts, std::max(1, 4096 / a.n));
+  const int64_t parts = 1 + (a.n == 1 ? a.T : a.T - 1) / 8192;
+  a.parts = a.T <= 1024 ? 0 : static_cast<int>(std::min<int64_t>(most, parts));
   if (a.dZ && a.parts) k_token_count<<<a.n * a.parts, 256, 0, s>>>(a);
   if (a.T) {
     if (a.dtype == DBW_F32)

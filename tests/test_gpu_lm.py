@@ -319,6 +319,16 @@ def test_token_loss_strides_many_workers_and_one_token():
     assert host(loss).tolist() == [0.0, 0.0] and dZ.shape == (0, C)
 
 
+def test_token_loss_of_more_rows_than_one_launch_starts():
+    # 2^20 + 5 rows, and workers that have nearly all of them or none
+    g = gen(10)
+    T, C = (1 << 20) + 5, 9
+    Z = normal(g, (T, C), torch.bfloat16, 2.0)
+    y = torch.randint(-1, C, (T,), generator=g, device="cuda", dtype=torch.int32)
+    check_loss(Z, y, [3, T - 7, 0, 4])
+    check_loss(Z[:70001].float(), y[:70001], [0] * 500 + [70001] + [0] * 400)
+
+
 @pytest.mark.parametrize("C", [9, 3000, 20000, 150000])
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
 def test_token_loss_of_masked_and_broken_logits(C, dtype):
