@@ -15,9 +15,11 @@
 // steps or stores (256 x 256 tiles, one workgroup a CU: 319 us where 128 x 256
 // take 258, head 4096 x 1024 x 32000).
 //
-// What bounds it: long sums, the matrix cores, busy 64% of the cycles at 8192
-// terms (1200 TFLOP/s; a library product of 8192^3 reaches 1210), the rest LDS
-// reads and barriers; head 4096 x 1024 x 32000 258 us, 1040 TFLOP/s.  Ragged
+// What bounds it: long sums, the matrix cores at the clock they hold, busy 62%
+// of the cycles, the rest LDS reads and barriers.  4096 rows, 16384 columns, bf16,
+// TFLOP/s of Y, G and dX (a library product): 256 terms 670, 600, 540 (570); 1024
+// 1030, 1050, 845 (1070); 4096 1310, 1370, 1155 (1370); 8192 1215, 1315, 1035
+// (1390).  Head 4096 x 1024 x 32000 258 us, 1040 TFLOP/s.  Ragged
 // groups, how evenly their tiles fall on the CUs: 32 groups 8192 x 2048 x 1536 80
 // us, 650 TFLOP/s and 3.3 TB/s.  G of short minibatches, its stores: 16 workers
 // 8000 x 784 x 4000 78 us (200 MB; streamed past the caches 123 us became 107 for
