@@ -59,8 +59,10 @@ dbw_status check_shape(const dbw_group_shape* p, const char* call) {
     return set_free_error(DBW_EINVAL, "%s: W_%d would overlap W_0 (st_W=%lld)", call, 1, (long long)p->st_W);
   if (p->st_W >= (int64_t{1} << 40))
     return set_free_error(DBW_EUNSUPPORTED, "%s: st_W reaches 2^40", call);
-  // (a launch holds fewer than 2^32 threads, 512 at most to a workgroup)
-  if (dbw::group_plan(*p).blocks >= (int64_t{1} << 23) - 8)
+  // (a launch holds fewer than 2^32 threads: fewer than 2^24 workgroups, which
+  // are twice the plan's where lines at odd addresses take the smaller tile, and
+  // up to 255 more for whole runs)
+  if (dbw::group_plan(*p).blocks > (int64_t{1} << 23) - 128 - 1)
     return set_free_error(DBW_EUNSUPPORTED, "%s: 2^23 output tiles or more", call);
   return DBW_OK;
 }

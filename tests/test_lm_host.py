@@ -157,3 +157,16 @@ def test_binding_refuses_what_the_library_cannot_see():
     assert s["m"][0].dtype == torch.float8_e4m3fn and s["m"][0].shape == (3, 100) and s["v_scale"][0].shape == (2,)
     assert float(s["m_scale"][0].float()[0]) == 2.0 ** -126
     assert pb.adamw_states([torch.zeros(5)])["v"][0].dtype == torch.float32
+
+
+def test_unaligned_products_near_the_most_tiles_are_refused(lib):
+    # 2053 x 4086 tiles of 128 x 256 are below 2^23, but lines of an odd length
+    # take 128 x 128: in whole runs 2^24 workgroups of 256 threads, and a launch
+    # holds fewer than 2^32 threads
+    C = 4085 * 256 + 1
+    s = _shape(n=1, T=2052 * 128, C=C, ld_C=C, ld_W=C, st_W=0)
+    need = ctypes.c_int64(-5)
+    assert lib.dbw_group_workspace(ctypes.byref(s), ctypes.byref(need)) == pb.DBW_EUNSUPPORTED
+    assert lib.dbw_group_product(ctypes.byref(s), P, P, P, P, P, 1 << 40, NULL) == pb.DBW_EUNSUPPORTED
+    s = _shape(n=1, T=2051 * 128, C=C, ld_C=C, ld_W=C, st_W=0)
+    assert lib.dbw_group_workspace(ctypes.byref(s), ctypes.byref(need)) == pb.DBW_OK and need.value == 0
