@@ -500,8 +500,9 @@ typedef struct {
 typedef struct dbw_adamw dbw_adamw;
 
 /* A plan for these tensors on the current device: their addresses and t are
- * kept on the device until dbw_adamw_destroy.  Tensors must not overlap each
- * other; each pointer is aligned to its elements. */
+ * kept on the device until dbw_adamw_destroy.  An array that a step writes
+ * (all but g) must overlap no other of the plan (DBW_EINVAL); two tensors may
+ * read the same g.  Each pointer is aligned to its elements. */
 dbw_status dbw_adamw_create(const dbw_adamw_config* cfg, const dbw_adamw_tensor* tensors, dbw_adamw** out);
 void dbw_adamw_destroy(dbw_adamw* opt);
 

@@ -2,6 +2,7 @@
 // launches.  The kernels are in k_group.hip, k_token.hip and k_adamw.hip.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstdint>
 #include <new>
@@ -201,6 +202,48 @@ dbw_status dbw::adamw_check(const dbw_adamw_hyper& h, std::string* why) {
   return DBW_EINVAL;
 }
 
+namespace {
+// A tensor one of whose arrays overlaps another that a step writes (a tensor
+// listed twice, a state of two tensors), or -1.  In the order of their starts,
+// an array is compared with the farthest ends before it, of all and of the
+// written ones.
+int32_t overlapping(const dbw_adamw_config& cfg, const dbw_adamw_tensor* tensors, size_t state) {
+  struct Array {
+    uintptr_t first, end;
+    int32_t tensor;
+    bool written;
+  };
+  std::vector<Array> all;
+  all.reserve(static_cast<size_t>(cfg.tensors) * 7);
+  for (int32_t i = 0; i < cfg.tensors; ++i) {
+    const dbw_adamw_tensor& t = tensors[i];
+    if (!t.count) continue;
+    const auto add = [&](const void* p, int64_t bytes, bool written) {
+      const uintptr_t first = reinterpret_cast<uintptr_t>(p);
+      all.push_back(Array{first, first + static_cast<uintptr_t>(bytes), i, written});
+    };
+    add(t.w, t.count * 4, true);
+    add(t.g, t.count * dbw::elem_bytes(cfg.g_dtype), false);
+    add(t.m, t.count * static_cast<int64_t>(state), true);
+    add(t.v, t.count * static_cast<int64_t>(state), true);
+    if (t.w_low) add(t.w_low, t.count * 2, true);
+    if (cfg.state_bits == 8) {
+      const int64_t blocks = (t.count + dbw::kAdamBlock - 1) / dbw::kAdamBlock;
+      add(t.m_scale, blocks, true);
+      add(t.v_scale, blocks, true);
+    }
+  }
+  std::sort(all.begin(), all.end(), [](const Array& a, const Array& b) { return a.first < b.first; });
+  uintptr_t end = 0, end_written = 0;
+  for (const Array& a : all) {
+    if (a.first < (a.written ? end : end_written)) return a.tensor;
+    end = std::max(end, a.end);
+    if (a.written) end_written = std::max(end_written, a.end);
+  }
+  return -1;
+}
+}  // namespace
+
 DBW_API dbw_status dbw_adamw_create(const dbw_adamw_config* cfg, const dbw_adamw_tensor* tensors, dbw_adamw** out) {
   const char* call = "dbw_adamw_create";
   if (!cfg || !tensors || !out) return set_free_error(DBW_EINVAL, "%s: a pointer is NULL", call);
@@ -233,6 +276,12 @@ DBW_API dbw_status dbw_adamw_create(const dbw_adamw_config* cfg, const dbw_adamw
   }
   if (nchunks > (int64_t{1} << 26))
     return set_free_error(DBW_EUNSUPPORTED, "%s: more than 2^26 chunks of %d values", call, dbw::kAdamChunk);
+  try {
+    if (const int32_t i = overlapping(*cfg, tensors, state); i >= 0)
+      return set_free_error(DBW_EINVAL, "%s: tensor %d: an array overlaps another, and a step writes one of them", call, i);
+  } catch (const std::exception&) {
+    return set_free_error(DBW_EHIP, "%s: out of host memory", call);
+  }
   dbw_adamw* o = new (std::nothrow) dbw_adamw;
   if (!o) return set_free_error(DBW_EHIP, "%s: out of host memory", call);
   o->cfg = *cfg;

@@ -170,3 +170,37 @@ def test_unaligned_products_near_the_most_tiles_are_refused(lib):
     assert lib.dbw_group_product(ctypes.byref(s), P, P, P, P, P, 1 << 40, NULL) == pb.DBW_EUNSUPPORTED
     s = _shape(n=1, T=2051 * 128, C=C, ld_C=C, ld_W=C, st_W=0)
     assert lib.dbw_group_workspace(ctypes.byref(s), ctypes.byref(need)) == pb.DBW_OK and need.value == 0
+
+
+def test_adamw_refuses_arrays_that_overlap(lib):
+    # two tensors of 300 values, states in 8 bits, each array at a place of its own
+    def create(edit):
+        t = (pb.AdamWTensor * 2)()
+        for i in range(2):
+            for j, k in enumerate(("w", "g", "m", "v", "m_scale", "v_scale", "w_low")):
+                setattr(t[i], k, 65536 * (1 + 7 * i + j))
+            t[i].count, t[i].lr_scale, t[i].weight_decay = 300, 1.0, 0.0
+        edit(t)
+        c = pb.AdamWConfig(state_bits=8, g_dtype=pb.DBW_F32, low_dtype=pb.DBW_BF16, tensors=2, t=0)
+        out = ctypes.c_void_p()
+        status = lib.dbw_adamw_create(ctypes.byref(c), t, ctypes.byref(out))
+        lib.dbw_adamw_destroy(out)
+        return status
+
+    def at(k, size):   # the second tensor's array at a distance of the first one's
+        return lambda t: setattr(t[1], k, getattr(t[0], k) + size)
+    edits = [at(k, 0) for k in ("w", "m", "v", "m_scale", "v_scale", "w_low")]
+    # in the last value of the first one's
+    edits += [at("w", 299 * 4), at("m", 299), at("v", 299), at("m_scale", 1), at("w_low", 299 * 2)]
+    # with another kind of array, written or read
+    edits += [lambda t: setattr(t[0], "v", t[0].m), lambda t: setattr(t[0], "w", t[1].g),
+              lambda t: setattr(t[0], "w_low", t[0].w), lambda t: setattr(t[1], "g", t[0].w + 299 * 4)]
+    # a long array over a short one in its middle, where both neighbours are apart
+    edits += [lambda t: setattr(t[1], "v_scale", t[0].w + 600)]
+    for i, edit in enumerate(edits):
+        assert create(edit) == pb.DBW_EINVAL, i
+        assert b"overlap" in lib.dbw_last_error(None), i
+    # one behind the other is allowed, and so is a gradient that two tensors read
+    # (without a device the plan then fails to find one)
+    for edit in (at("w", 300 * 4), at("m", 300), at("m_scale", 2), at("g", 0), at("g", 4)):
+        assert create(edit) in (pb.DBW_OK, pb.DBW_EHIP)
