@@ -602,6 +602,7 @@ class AdamW:
         it to) is given, else None."""
         if stream is not None:
             return _on(stream, self.step, lr, beta1, beta2, eps, max_norm, grad_scale, seed, norm)
+        self._open()
         torch = _torch()
         if norm is None and max_norm:
             norm = torch.empty((), dtype=torch.float32, device=self.device)
@@ -617,17 +618,24 @@ class AdamW:
     @property
     def t(self) -> int:
         """Steps made (waits for the device)."""
-        out = c_int64()
-        st = self.lib.dbw_adamw_export(self.h, ctypes.byref(out))
+        out, plan = c_int64(), self._open()
+        st = self.lib.dbw_adamw_export(plan, ctypes.byref(out))
         if st != DBW_OK:
             raise DBWError(st, self.lib.dbw_last_error(None).decode())
         return out.value
 
     @t.setter
     def t(self, value: int):
-        st = self.lib.dbw_adamw_import(self.h, int(value))
+        plan = self._open()
+        st = self.lib.dbw_adamw_import(plan, int(value))
         if st != DBW_OK:
             raise DBWError(st, self.lib.dbw_last_error(None).decode())
+
+    def _open(self):
+        """The plan's handle."""
+        if self.h is None:
+            raise ValueError("the AdamW plan is closed")
+        return self.h
 
     def close(self):
         if self.h is not None:
@@ -673,6 +681,8 @@ class _DeviceArray:
 
 class Context:
     """One DBW parameter-server simulation bound to a torch CUDA (HIP) stream."""
+
+    _adamw = None   # the plan of use_adamw
 
     def __init__(self, cfg: Config, stream=None, device=None):
         torch = _torch()
@@ -785,6 +795,8 @@ class Context:
 
     def step(self, w, X, y, ticks, rows=None, wait: bool = False):
         """One DBW iteration; updates w in place.  Returns k_t if ``wait``."""
+        if self._adamw is not None:
+            self._adamw._open()      # not closed since use_adamw
         torch = _torch()
         c = self.cfg
         ticks = np.ascontiguousarray(ticks, dtype=np.int64)
@@ -809,7 +821,8 @@ class Context:
         whose gradients are slices of gradient(), in the places that its w have
         in the w of step) instead of by SGD; None: by SGD again."""
         hyper = AdamWHyper(lr, beta1, beta2, eps, grad_scale, max_norm, int(seed) & 0xFFFFFFFF)
-        self._check(self.lib.dbw_set_adamw(self.h, opt.h if opt is not None else None, ctypes.byref(hyper)),
+        plan = opt._open() if opt is not None else None   # (a closed plan's NULL would mean SGD)
+        self._check(self.lib.dbw_set_adamw(self.h, plan, ctypes.byref(hyper)),
                     "dbw_set_adamw")
         self._adamw = opt            # the plan outlives its use
 

@@ -204,3 +204,21 @@ def test_adamw_refuses_arrays_that_overlap(lib):
     # (without a device the plan then fails to find one)
     for edit in (at("w", 300 * 4), at("m", 300), at("m_scale", 2), at("g", 0), at("g", 4)):
         assert create(edit) in (pb.DBW_OK, pb.DBW_EHIP)
+
+
+class _NoLibrary:
+    def __getattr__(self, name):
+        raise AssertionError(f"{name} was called")
+
+
+def test_a_closed_plan_is_refused():
+    opt, ctx = pb.AdamW.__new__(pb.AdamW), pb.Context.__new__(pb.Context)
+    opt.h, ctx.h, ctx.lib, opt.lib = None, ctypes.c_void_p(1), _NoLibrary(), _NoLibrary()
+    with pytest.raises(ValueError, match="closed"):   # not: back to SGD
+        ctx.use_adamw(opt, lr=1e-3)
+    ctx._adamw = opt                                  # closed while it was in use
+    with pytest.raises(ValueError, match="closed"):
+        ctx.step(None, None, None, [0])
+    for call in (lambda: opt.step(1e-3), lambda: opt.t, lambda: setattr(opt, "t", 3)):
+        with pytest.raises(ValueError, match="closed"):
+            call()
