@@ -370,9 +370,11 @@ def _stream_of(torch, dev):
     return torch._C._cuda_getCurrentRawStream(dev.index)
 
 
-def _on(stream, function, *args, **kw):
+def _on(stream, dev, function, *args, **kw):
     """function with `stream` as the current one, so that what it allocates
     belongs to that stream."""
+    if stream.device != dev:
+        raise ValueError(f"the stream is of {stream.device}, the tensors are on {dev}")
     with _torch().cuda.stream(stream):
         return function(*args, **kw)
 
@@ -417,7 +419,7 @@ def _group_shape(*sizes):
 
 def _group(form, a, b, offsets, out, out_dtype, d, C, workspace, stream=None):
     if stream is not None:
-        return _on(stream, _group, form, a, b, offsets, out, out_dtype, d, C, workspace)
+        return _on(stream, a.device, _group, form, a, b, offsets, out, out_dtype, d, C, workspace)
     torch = _torch()
     lib = load_library()
     dev, dtype = a.device, a.dtype
@@ -495,7 +497,7 @@ def token_loss(Z, y, offsets, scale=1.0, dZ=None, loss=None, grad=True, workspac
     (loss [n] float32, dZ [T][C] of the type of Z, times ``scale``); dZ may be
     Z, to write the gradient in its place; ``grad`` False: no gradient (None)."""
     if stream is not None:
-        return _on(stream, token_loss, Z, y, offsets, scale, dZ, loss, grad, workspace)
+        return _on(stream, Z.device, token_loss, Z, y, offsets, scale, dZ, loss, grad, workspace)
     torch = _torch()
     lib = load_library()
     dev, dtype = Z.device, Z.dtype
@@ -601,7 +603,7 @@ class AdamW:
         float32 scalar tensor, where max_norm or ``norm`` (a tensor to write
         it to) is given, else None."""
         if stream is not None:
-            return _on(stream, self.step, lr, beta1, beta2, eps, max_norm, grad_scale, seed, norm)
+            return _on(stream, self.device, self.step, lr, beta1, beta2, eps, max_norm, grad_scale, seed, norm)
         self._open()
         torch = _torch()
         if norm is None and max_norm:

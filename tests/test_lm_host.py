@@ -222,3 +222,19 @@ def test_a_closed_plan_is_refused():
     for call in (lambda: opt.step(1e-3), lambda: opt.t, lambda: setattr(opt, "t", 3)):
         with pytest.raises(ValueError, match="closed"):
             call()
+
+
+def test_a_stream_of_another_device_is_refused():
+    torch = pytest.importorskip("torch")
+
+    class Stream:
+        device = torch.device("cuda", 1)
+    X, W, y = torch.zeros(6, 8).bfloat16(), torch.zeros(2, 8, 4).bfloat16(), torch.zeros(6, dtype=torch.int32)
+    off = torch.tensor([0, 2, 6], dtype=torch.int32)
+    opt = pb.AdamW.__new__(pb.AdamW)
+    opt.h, opt.lib, opt.device = ctypes.c_void_p(1), _NoLibrary(), torch.device("cuda", 0)
+    for call in (lambda: pb.group_matmul(X, W, off, stream=Stream()), lambda: pb.token_loss(X, y, off, stream=Stream()),
+                 lambda: opt.step(1e-3, stream=Stream())):
+        with pytest.raises(ValueError, match="stream"):
+            call()
+    opt.h = None
