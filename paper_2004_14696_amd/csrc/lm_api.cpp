@@ -315,6 +315,7 @@ DBW_API dbw_status dbw_adamw_create(const dbw_adamw_config* cfg, const dbw_adamw
   if (e == hipSuccess) e = hipMemcpy(o->pool, host.data(), all, hipMemcpyHostToDevice);
   if (e != hipSuccess) {
     if (o->pool) (void)hipFree(o->pool);
+    (void)hipGetLastError();   // not the next launch's
     delete o;
     return set_free_error(DBW_EHIP, "%s: the plan's %lld bytes: %s", call, (long long)all, hipGetErrorString(e));
   }
