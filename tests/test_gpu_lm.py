@@ -834,3 +834,60 @@ def test_offsets_that_break_the_rules_stay_inside():
     Y = torch.full((T, C), 2.0, dtype=torch.bfloat16, device="cuda")
     pb.group_matmul(X, W, torch.tensor([0, 60, 70, 80], dtype=torch.int32, device="cuda"), out=Y)
     assert torch.equal(Y, pb.group_matmul(X, W, offsets_of([50, 0, 0])))
+
+
+def test_products_and_losses_in_parts_captured():
+    # sums and rows in parts, in a padded batch: rows of no group before, and
+    # behind, the groups keep what they held.  One graph, replayed with other
+    # inputs, against the same calls made eagerly
+    g = gen(35)
+    T, d, C, first = 12000, 2048, 72, 5
+    lengths = [0, 1, 9000, 2000]
+    off = offsets_of(lengths, first)
+    end = first + sum(lengths)
+    few = offsets_of([3, 0, 20], first)                    # few rows of a long sum
+    X = normal(g, (T, d), torch.bfloat16)
+    Y0 = normal(g, (T, C), torch.bfloat16)
+    y = torch.randint(-1, C, (T,), generator=g, device="cuda", dtype=torch.int32)
+    W = normal(g, (3, d, C), torch.bfloat16, d ** -0.5)
+    small = X[:30]
+    Z, dZ = torch.empty_like(Y0), torch.full_like(Y0, 2.0)
+    Y, G = torch.full((30, C), 2.0, dtype=torch.bfloat16, device="cuda"), torch.empty((4, d, C), device="cuda")
+    dX = torch.full((30, d), 2.0, dtype=torch.bfloat16, device="cuda")
+    loss = torch.empty(4, device="cuda")
+    outs = [dZ, Y, G, dX, loss]
+
+    def call():
+        Z.copy_(Y0)
+        pb.token_loss(Z, y, off, dZ=dZ, loss=loss)
+        pb.group_weight_grad(X, dZ, off, out=G)
+        pb.group_matmul(small, W, few, out=Y)
+        pb.group_input_grad(Y, W, few, out=dX)
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        call()
+        stream.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            call()
+        for replay in range(4):
+            X.normal_(generator=g)
+            Y0.normal_(generator=g)
+            call()
+            torch.cuda.synchronize()
+            want = [x.clone() for x in outs]
+            for x in (dZ, Y, dX):
+                x.fill_(2.0)
+            G.fill_(3.0)
+            loss.fill_(3.0)
+            graph.replay()
+            torch.cuda.synchronize()
+            pb.group_matmul(X[:9], W[0], offsets_of([9]))   # unrelated eager work between the replays
+            for a, b in zip(outs, want):
+                assert torch.equal(a, b), replay
+            assert bool((dZ[:first] == 2).all()) and bool((dZ[end:] == 2).all())
+            assert bool((Y[:first] == 2).all()) and bool((Y[first + 23:] == 2).all())
+            assert bool((dX[:first] == 2).all()) and bool((dX[first + 23:] == 2).all())
+            assert bool((G[0] == 0).all())
+    check_loss(Y0[first:end], y[first:end], lengths)
