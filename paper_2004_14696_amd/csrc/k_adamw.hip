@@ -3,17 +3,23 @@
 //   k_adamw_prep   one workgroup: t, the norm, the clip factor, 1 - beta^t,
 //   k_adamw_update every tensor, a workgroup to a chunk of 1024 values.
 //
-// The update is bound by memory: 8 bytes of w, 16 (32-bit states) or 4 + 1/64
-// (8-bit) of states, and the gradient, each moved once; some 60 vector
-// operations a value with 8-bit states stay below that.  A lane holds four
-// consecutive values (16 bytes of w), a wave the 256 values of one scale, so
-// the largest magnitude of a block is a reduction over the lanes of one wave
-// and nothing goes through shared memory.  The table of chunks gives a
-// workgroup its tensor with one load, whatever the sizes of the tensors.
+// The update moves 8 bytes of w, 16 (32-bit states) or 4 + 1/64 (8-bit) of
+// states, and the gradient, each once, and is bound by that: 5.5 TB/s with
+// either.  With 8-bit states only just: 133 vector instructions a value took
+// 425 us for 128M values, 77 take 374 (codes by the stochastic conversion, a
+// shorter root, one product of the hash for four values, no 64-bit division).
+// In calls right behind each other their power lowers the clock: the step of
+// 450 us takes 550 after ten, and 470 in the long run (690 and 525 before);
+// 32-bit states keep their time.
+//
+// A lane holds four consecutive values (16 bytes of w), a wave the 256 values of
+// one scale, so the largest magnitude of a block is a reduction over the lanes
+// of one wave and nothing goes through shared memory.  The table of chunks gives
+// a workgroup its tensor with one load, whatever the sizes of the tensors.
 // 64M values, 32-bit states, fp16 gradients and copy: 329 us, 5.5 TB/s (chunks of
 // 4096 values 357: fewer loads under way); 128M, 8-bit states, bf16 gradients
-// and copy, clipped: 502 us, 424 of them the update (4.8 TB/s) and 66 the norm (3.9
-// TB/s); 0.4M values, clipped: 13.7 us, three launches.
+// and copy, clipped: 447 us, 374 of them the update and 66 the norm (3.9 TB/s);
+// 0.4M values, clipped: 14 us, three launches.
 //
 // t and what depends on it live on the device (a captured step advances them
 // at every replay) and are handed from kernel to kernel in stream order: no
@@ -21,6 +27,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cmath>
+#include <type_traits>
 
 #include "lm_ops.h"
 
@@ -119,35 +126,80 @@ __device__ __forceinline__ void decode(uint32_t codes, uint32_t e, float (&x)[4]
   x[3] = b[1] * s;
 }
 
-__device__ __forceinline__ float finite_abs(float x) {
-  const float a = fabsf(x);
-  return a <= 0x1.fffffep127f ? a : 0.f;
+// The largest of the 64 lanes' v, in all of them (a scalar).
+__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
+  const auto with = [&](auto ctrl, auto rows) {
+    const uint32_t o = static_cast<uint32_t>(__builtin_amdgcn_update_dpp(
+        0, static_cast<int>(v), decltype(ctrl)::value, decltype(rows)::value, 0xf, true));
+    v = v > o ? v : o;
+  };
+  typedef std::integral_constant<int, 0xf> all;
+  with(std::integral_constant<int, 0x111>{}, all{});   // the lanes 1, 2, 4 and 8 before, in rows of 16
+  with(std::integral_constant<int, 0x112>{}, all{});
+  with(std::integral_constant<int, 0x114>{}, all{});
+  with(std::integral_constant<int, 0x118>{}, all{});
+  with(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{});   // a row's last lane, to the next row
+  with(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});   // the first half's, to the second
+  return static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(v), 63));
+}
+
+constexpr uint32_t kInf = 0x7f800000u;
+__device__ __forceinline__ uint32_t abs_bits(float x) { return __builtin_bit_cast(uint32_t, x) & 0x7fffffffu; }
+// Magnitudes as integers: their order is that of the values, with infinities
+// and NaN on top.  The least leaves out zeros (which wrap around).
+__device__ __forceinline__ uint32_t lane_most(const float (&x)[4]) {
+  const uint32_t a = max(abs_bits(x[0]), abs_bits(x[1])), b = max(abs_bits(x[2]), abs_bits(x[3]));
+  return max(a, b);
+}
+__device__ __forceinline__ uint32_t lane_least(const float (&x)[4]) {
+  const uint32_t a = min(abs_bits(x[0]) - 1u, abs_bits(x[1]) - 1u), b = min(abs_bits(x[2]) - 1u, abs_bits(x[3]) - 1u);
+  return min(a, b);
 }
 
 // Codes of the 256 values of a wave, four a lane, and the biased exponent of
-// their scale.  `bits`: 16 random bits a value.  FLOOR: what is above 0 stays
-// above 0.
+// their scale.  `most`: wave_max of lane_most(x).  `bits`: a value's 16
+// random bits, above 16 zeros (the conversion would look at four of those).
+// FLOOR: what is above 0 stays above 0.
+//
+// Where all values are finite and none but zeros is below 2^-6 in units of the
+// scale, the conversion with stochastic rounding gives the formula's codes, sign
+// included (compared for all floats of [2^-6, 448], each with the drawn bits
+// where its code turns and others: 10^9 pairs; of smaller values 4 in 10^5
+// pairs differ, where the formula's sum in fp32 is rounded).  It takes one
+// instruction a value for some fifteen.
 template <bool FLOOR>
-__device__ __forceinline__ uint32_t encode(const float (&x)[4], const uint32_t (&bits)[4], uint32_t* scale) {
-  float top = 0x1p-118f;
+__device__ __forceinline__ uint32_t encode(const float (&x)[4], const uint32_t (&bits)[4], uint32_t most,
+                                           uint32_t* scale) {
+  const bool finite = most < kInf;
+  if (!finite) {
+    uint32_t lane = 0;
 #pragma unroll
-  for (int j = 0; j < 4; ++j) top = fmaxf(top, finite_abs(x[j]));
-#pragma unroll
-  for (int d = 32; d; d /= 2) top = fmaxf(top, __shfl_xor(top, d));
-  const uint32_t tb = __builtin_bit_cast(uint32_t, top);
+    for (int j = 0; j < 4; ++j) lane = max(lane, abs_bits(x[j]) < kInf ? abs_bits(x[j]) : 0u);
+    most = wave_max(lane);
+  }
+  const uint32_t tb = max(most, __builtin_bit_cast(uint32_t, 0x1p-118f));
   // the largest value times 2^-e is in (224, 448]: 448 = 1.75 2^8 is the
   // largest code
   const int e = static_cast<int>(tb >> 23) - 127 - 8 + ((tb & 0x7fffffu) > 0x600000u ? 1 : 0);
   *scale = static_cast<uint32_t>(e + 127);
   const float inv = pow2(-e);
   uint32_t codes = 0;
+  // 2^(e - 6): 0 or a subnormal's bits are below those of any normal value
+  const uint32_t low = e - 6 > -127 ? static_cast<uint32_t>(e - 6 + 127) << 23 : 1u << 23;
+  if (finite && __all(lane_least(x) >= low - 1u)) {
+    codes = __builtin_amdgcn_cvt_sr_fp8_f32(x[0] * inv, bits[0], codes, 0);
+    codes = __builtin_amdgcn_cvt_sr_fp8_f32(x[1] * inv, bits[1], codes, 1);
+    codes = __builtin_amdgcn_cvt_sr_fp8_f32(x[2] * inv, bits[2], codes, 2);
+    codes = __builtin_amdgcn_cvt_sr_fp8_f32(x[3] * inv, bits[3], codes, 3);
+    return codes;
+  }
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const float y = fabsf(x[j]) * inv;                       // exact, or below every code
     // 2^(step) is the distance of the codes at y: 8 to a power of two, down
     // to 2^-6, evenly spaced below
     const int ey = static_cast<int>(__builtin_bit_cast(uint32_t, fmaxf(y, 0x1p-6f)) >> 23) - 127;
-    uint32_t q = static_cast<uint32_t>(y * pow2(3 - ey) + static_cast<float>(bits[j]) * 0x1p-16f);
+    uint32_t q = static_cast<uint32_t>(y * pow2(3 - ey) + static_cast<float>(bits[j] >> 16) * 0x1p-16f);
     if (FLOOR) q = q == 0 && x[j] > 0.f ? 1u : q;
     uint32_t c = static_cast<uint32_t>((ey + 6) * 8) + q;    // a carry of q moves to the next power
     c = fabsf(x[j]) <= 0x1.fffffep127f ? c : 0x7fu;
@@ -155,6 +207,18 @@ __device__ __forceinline__ uint32_t encode(const float (&x)[4], const uint32_t (
     codes |= c << (8 * j);
   }
   return codes;
+}
+
+// sqrt(v), correctly rounded for v = 0 and from 2^-100 to 2^127: y is within an
+// ulp or so of 1/sqrt(v), g of sqrt(v), and one Newton step with its residual,
+// which is exact in a fused multiply-add, gives the rounded root (Markstein,
+// "Computation of elementary functions on the IBM RISC System/6000", 1990;
+// compared for every float of that range).  Other v that are not 0 give a root
+// below 2^-50, an infinity or a NaN.
+__device__ __forceinline__ float root(float v) {
+  const float y = __builtin_amdgcn_rsqf(fmaxf(v, 0x1p-100f));
+  const float g = v * y;
+  return fmaf(fmaf(-g, g, v), 0.5f * y, g);
 }
 
 template <typename G>
@@ -210,7 +274,7 @@ __global__ __launch_bounds__(kThreads) void k_adamw_prep(AdamStep* step, const d
   step->t = t;
   step->skip = skip;
   step->f = static_cast<float>(f);
-  step->bc1 = 1.0 - pow(h.beta1, static_cast<double>(t));
+  step->ibc1 = 1.0 / (1.0 - pow(h.beta1, static_cast<double>(t)));
   step->ibc2 = static_cast<float>(1.0 / sqrt(1.0 - pow(h.beta2, static_cast<double>(t))));
   step->key = adam_mix(adam_mix(h.seed) + static_cast<uint32_t>(t));
 }
@@ -230,7 +294,7 @@ __global__ __launch_bounds__(kThreads) void k_adamw_update(const AdamTensor* __r
   const int64_t left = t.count - first;
   const double lr = h.lr * t.lr_scale;
   const float f = step->f, ibc2 = step->ibc2, eps = static_cast<float>(h.eps);
-  const float keep = static_cast<float>(1.0 - lr * t.decay), rate = static_cast<float>(lr / step->bc1);
+  const float keep = static_cast<float>(1.0 - lr * t.decay), rate = static_cast<float>(lr * step->ibc1);
   const float b1 = static_cast<float>(h.beta1), c1 = static_cast<float>(1.0 - h.beta1);
   const float b2 = static_cast<float>(h.beta2), c2 = static_cast<float>(1.0 - h.beta2);
   const uint32_t key = BITS == 8 ? adam_mix(step->key + static_cast<uint32_t>(ch.tensor)) : 0;
@@ -259,9 +323,24 @@ __global__ __launch_bounds__(kThreads) void k_adamw_update(const AdamTensor* __r
     const float x = g[j] * f;
     m[j] = m[j] * b1 + x * c1;
     v[j] = v[j] * b2 + x * x * c2;
-    r[j] = sqrtf(v[j]);
-    w[j] = w[j] * keep - m[j] / (r[j] * ibc2 + eps) * rate;
+    r[j] = BITS == 32 ? sqrtf(v[j]) : root(v[j]);
   }
+  uint32_t most_r = 0;
+  if (BITS == 8) {
+    if (n < 4) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (j >= n) m[j] = v[j] = r[j] = 0.f;   // beyond the tensor: no part in the scale
+    }
+    most_r = wave_max(lane_most(r));
+    if (most_r >= kInf || !__all(lane_least(r) >= __builtin_bit_cast(uint32_t, 0x1p-50f) - 1u)) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) r[j] = sqrtf(v[j]);
+      most_r = wave_max(lane_most(r));
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j) w[j] = w[j] * keep - m[j] / (r[j] * ibc2 + eps) * rate;
   store4(t.w + i, n, w);
   if (t.low) {
     if (low_dtype == DBW_BF16)
@@ -274,15 +353,16 @@ __global__ __launch_bounds__(kThreads) void k_adamw_update(const AdamTensor* __r
     store4(static_cast<float*>(t.v) + i, n, v);
   } else {
     uint32_t lo[4], hi[4];
+    // (the indices of a lane start at a multiple of four: one product for all)
+    const uint32_t at0 = adam_index(i) + key;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const uint32_t u = adam_mix(adam_index(i + j) + key);
-      lo[j] = u & 0xffffu;
-      hi[j] = u >> 16;
-      if (j >= n) m[j] = r[j] = 0.f;   // beyond the tensor: no part in the scale
+      const uint32_t u = adam_mix(at0 + adam_index(j));
+      lo[j] = u << 16;
+      hi[j] = u & 0xffff0000u;
     }
     uint32_t em, ev;
-    const uint32_t cm = encode<false>(m, lo, &em), cv = encode<true>(r, hi, &ev);
+    const uint32_t cm = encode<false>(m, lo, wave_max(lane_most(m)), &em), cv = encode<true>(r, hi, most_r, &ev);
     store_codes(static_cast<uint8_t*>(t.m) + i, n, cm);
     store_codes(static_cast<uint8_t*>(t.v) + i, n, cv);
     if (threadIdx.x % 64 == 0) {

@@ -91,7 +91,7 @@ struct AdamStep {
   int64_t t;
   float f;          // factor of the gradients
   float ibc2;       // 1 / sqrt(1 - beta2^t)
-  double bc1;       // 1 - beta1^t
+  double ibc1;      // 1 / (1 - beta1^t)
   uint32_t key;     // mix(mix(seed) + t)
   int32_t skip;     // the norm is not finite: leave everything
 };

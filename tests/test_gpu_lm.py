@@ -539,6 +539,74 @@ def test_adamw_of_unaligned_tensors_with_their_own_rates(bits, shift):
         check_step(opt, w, g, st, lows, t, decay=decay, scale=scale)
 
 
+def exact_codes(x, bits, floor):
+    """Codes and scale exponents of fp32 values x [blocks][256], by the
+    definition: the sum of a value's place and its random bits is rounded to
+    fp32 (in 64 bits it is exact wherever it is near a whole number)."""
+    ab = np.abs(x.astype(np.float64))
+    finite = np.isfinite(ab)
+    top = np.maximum(np.where(finite, ab, 0.0).max(1), 2.0 ** -118)
+    mant, exp = np.frexp(top)                       # mant in [1/2, 1)
+    e = exp - 1 - 8 + (mant > 0.875)
+    y = np.where(finite, ab, 0.0) * 2.0 ** -e.astype(np.float64)[:, None]
+    ey = np.frexp(np.maximum(y, 2.0 ** -6))[1] - 1
+    q = np.floor((y * 2.0 ** (3.0 - ey) + bits / 65536.0).astype(np.float32)).astype(np.int64)
+    if floor:
+        q = np.where((q == 0) & (x > 0), 1, q)
+    c = np.where(finite, (ey + 6) * 8 + q, 0x7F) | np.where(np.signbit(x), 0x80, 0)
+    return c, e + 127
+
+
+def states_that_are_known_exactly(n):
+    """Gradients whose states with both betas 0 are themselves and their
+    magnitudes: blocks of ordinary values, of a wide range, with zeros, of
+    values whose squares are 0, subnormal or infinite, and not finite."""
+    rng = np.random.default_rng(50)
+    x = rng.standard_normal((n, 256)).astype(np.float32)
+    x[1::16] *= np.exp2(rng.uniform(-40, 0, (len(x[1::16]), 256))).astype(np.float32)
+    x[2::16] *= np.float32(2.0) ** rng.integers(-16, 1, (len(x[2::16]), 256)).astype(np.float32)
+    x[3::16][rng.random((len(x[3::16]), 256)) < 0.5] = 0.0
+    x[4::16] *= np.float32(2.0 ** -70)
+    x[5::16] *= np.float32(2.0 ** -45)
+    x[6::16, :200] *= np.float32(2.0 ** -52)
+    x[7::16, 5] = 2.0 ** 80
+    x[8::16, 17], x[8::32, 40] = np.inf, -np.inf
+    x[9::16, 3] = np.nan
+    x[10::16] = 0.0
+    x[11::16] = np.float32(1.75) * np.float32(2.0) ** rng.integers(-6, 7, (len(x[11::16]), 256)).astype(np.float32)
+    return x
+
+
+def test_adamw_8_bit_codes_are_exactly_those_of_their_definition():
+    # m = g and v = g^2 rounded, r its rounded root: no tolerance.  Two tensors,
+    # the second one's last block cut short
+    x = states_that_are_known_exactly(8192)
+    cut = 256 * 5000 + 101
+    parts = [x[:3000].reshape(-1), x[3000:].reshape(-1)[:cut]]
+    w = [torch.zeros(len(p), device="cuda") for p in parts]
+    grads = [torch.tensor(p, device="cuda") for p in parts]
+    st = pb.adamw_states(w, 8)
+    opt = pb.AdamW(w, grads, **st)
+    opt.step(lr=1e-3, beta1=0.0, beta2=0.0, seed=91)
+    torch.cuda.synchronize()
+    for i, p in enumerate(parts):
+        full = np.zeros(-(-len(p) // 256) * 256, np.float32)
+        full[:len(p)] = p
+        full = full.reshape(-1, 256)
+        b = bits_of(91, 1, i, full.size).reshape(full.shape)
+        with np.errstate(over="ignore", invalid="ignore"):
+            r = np.sqrt(full * full)
+        m = np.float32(0.0) + full                  # (-0 becomes 0)
+        for name, val, bits, floor in (("m", m, b & np.uint64(0xFFFF), False), ("v", r, b >> np.uint64(16), True)):
+            want, e = exact_codes(val, bits.astype(np.float64), floor)
+            got = host(st[name][i].view(torch.uint8)).astype(np.int64)
+            scale = host(st[name + "_scale"][i].view(torch.uint8)).astype(np.int64)
+            want, odd = want.reshape(-1)[:len(p)], ~np.isfinite(val).reshape(-1)[:len(p)]
+            assert np.array_equal(scale, e), (i, name, np.sum(scale != e))
+            assert np.all((got[odd] & 0x7F) == 0x7F), (i, name)
+            assert np.array_equal(got[~odd], want[~odd]), (i, name, np.sum(got[~odd] != want[~odd]))
+
+
 def test_adamw_of_empty_and_zero_tensors():
     opt, w, g, st, lows = make([0, 300, 0], 8, torch.float32, None, 23)
     g[1].zero_()
