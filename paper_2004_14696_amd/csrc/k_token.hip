@@ -19,13 +19,19 @@
 // values fill a CU by themselves (2048 x 128000 fp16 233 us, 4.5 TB/s), longer ones
 // are read twice (1024 x 200000 bf16 239 us, 3.4 TB/s by their size).
 //
-// softmax(z)_c = 2^(b z_c - b max) / sum 2^(b z - b max) with b = log2(e), in
-// fp32: one fused multiply-add and one exponential a value.  b max is rounded;
-// that factor is the same above and below, and is taken out of the loss.
+// softmax(z)_c = 2^(b (z_c - max)) / sum 2^(b (z - max)) with b = log2(e), in
+// fp32.  The difference comes first where that costs nothing: it is 0 at the
+// maximum, whatever its size.  16-bit rows held in registers take 2^(b z - b max)
+// instead, one fused multiply-add for two operations (2048 x 128000 fp16 246 us
+// for 265, 8192 x 50257 bf16 345 for 356; 4096 x 32000 fp32 203 for 202).  There b
+// max is rounded; that factor is the same above and below, and is taken out of
+// the loss.  It is at most 2 below |max| = 2^24, but would be beyond every
+// exponent from 2^31 on: see HalfPower.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "lm_ops.h"
 
@@ -155,28 +161,27 @@ __device__ __forceinline__ float row_sum(float v, float* lds) {
   return v;
 }
 
-// 2^(b x - b max) of a row, b max rounded.  Where b max would overflow, a value
-// below max is so far below that any base will do.
-struct Powers {
-  float b, bm;
-  __device__ __forceinline__ void set(float max) {
+// e^(x - max): 0 where the difference is infinite, NaN for two infinities of
+// one sign.
+struct Power {
+  float max;
+  __device__ __forceinline__ explicit Power(float m) : max(m) {}
+  __device__ __forceinline__ float operator()(float x) const { return __builtin_amdgcn_exp2f((x - max) * kLog2e); }
+  __device__ __forceinline__ float lost() const { return 0.f; }
+};
+// The same of 16-bit values, times a factor that all of a row share and whose
+// logarithm is lost().  From |max| = 2^24 on, bf16 values below max are 2^16 or
+// more below it: their powers are 0 to any base, and with b = 1 nothing is
+// rounded.
+struct HalfPower {
+  float b, bm, max;
+  __device__ __forceinline__ explicit HalfPower(float m) : max(m) {
 #pragma clang fp contract(off)   // bm is the rounded product wherever it is used
-    const bool large = !(fabsf(max) < 0x1p126f);
-    b = large ? 1.f : kLog2e;
-    bm = b * max;
+    b = fabsf(m) < 0x1p24f ? kLog2e : 1.f;
+    bm = b * m;
   }
   __device__ __forceinline__ float operator()(float x) const { return __builtin_amdgcn_exp2f(fmaf(x, b, -bm)); }
-  // another maximum: the factor of powers taken before (from -infinity: 0)
-  __device__ __forceinline__ float move(float max) {
-#pragma clang fp contract(off)
-    const float was = bm;
-    set(max);
-    return __builtin_amdgcn_exp2f(was - bm);
-  }
-  // log of the factor that the rounding of b max put on every power
-  __device__ __forceinline__ float lost(float max) const {
-    return fabsf(max) < 0x1p126f ? fmaf(max, b, -bm) * 0.693147180559945309f : 0.f;
-  }
+  __device__ __forceinline__ float lost() const { return fmaf(max, b, -bm) * 0.693147180559945309f; }
 };
 
 // One row by THREADS threads, PACKS packs of 16 bytes a thread held in
@@ -216,8 +221,8 @@ __device__ __forceinline__ void token_row(const TokenArgs& a, int64_t t, int tid
   const E low = static_cast<E>(-INFINITY);
   const float zy = y < C ? lm_to_f32(z[y]) : NAN;   // read before any store: dZ may be Z
   const float ze = has_edge ? lm_to_f32(z[edge]) : -INFINITY;
+  typedef std::conditional_t<PACKS && sizeof(E) == 2, HalfPower, Power> P;
   float top, sum;
-  Powers e;
   lm_u32x4 held[PACKS ? PACKS : 1];
   if (PACKS) {
     V fill;
@@ -236,7 +241,7 @@ __device__ __forceinline__ void token_row(const TokenArgs& a, int64_t t, int tid
       for (int j = 0; j < N; ++j) top = fmaxf(top, lm_to_f32(v[j]));
     }
     top = row_max<THREADS>(top, lds);
-    e.set(top);
+    const P e(top);
     sum = e(ze);
 #pragma unroll
     for (int p = 0; p < PACKS; ++p) {
@@ -250,28 +255,28 @@ __device__ __forceinline__ void token_row(const TokenArgs& a, int64_t t, int tid
     // running maximum and sum of every thread, joined at the end; a thread
     // that has seen only -infinities keeps 0
     float mx = ze;
-    e.set(mx);
-    sum = ze == -INFINITY ? 0.f : e(ze);
+    sum = ze == -INFINITY ? 0.f : Power(mx)(ze);
     for (int p = tid; p < packs; p += THREADS) {
       const V v = __builtin_bit_cast(V, static_cast<lm_u32x4>(*reinterpret_cast<const lm_u32x4_any*>(zb + p * N)));
       float m = mx;
 #pragma unroll
       for (int j = 0; j < N; ++j) m = fmaxf(m, lm_to_f32(v[j]));
       if (m != mx) {
-        sum *= e.move(m);
+        sum *= Power(m)(mx);
         mx = m;
       }
 #pragma unroll
       for (int j = 0; j < N; ++j) {
         const float x = lm_to_f32(v[j]);
-        sum += x == -INFINITY ? 0.f : e(x);
+        sum += x == -INFINITY ? 0.f : Power(mx)(x);
       }
     }
     top = row_max<THREADS>(mx, lds);
-    sum *= e.move(top);
+    sum *= Power(top)(mx);
     sum = row_sum<THREADS>(sum, lds);
   }
-  if (tid == 0) a.row_loss[t] = logf(sum) - e.lost(top) + (top - zy);
+  const P e(top);
+  if (tid == 0) a.row_loss[t] = logf(sum) - e.lost() + (top - zy);
   if (!dz) return;
   // live rows of the worker (at least this one)
   int count = 0;

@@ -364,6 +364,45 @@ def test_token_loss_of_masked_and_broken_logits(C, dtype):
     assert float(loss[0]) == math.inf and bool(torch.isfinite(dZ).all())
 
 
+@pytest.mark.parametrize("C", [9, 3000, 20000, 150000])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_token_loss_of_logits_of_any_magnitude(C, dtype):
+    # the largest power of a row is 1 whatever its logit: rows of equal logits
+    # (one masked as a whole with a large negative value among them), at every
+    # power of two
+    g = gen(C + 2)
+    v = torch.tensor([s * 1.3 * 2.0 ** k for k in range(20, 128) for s in (1, -1)] + [3e9, 1e10, -1e10, -1e20, 1e30, -1e30],
+                     dtype=torch.float64, device="cuda").to(dtype)
+    T = len(v)
+    y = torch.randint(0, C, (T,), generator=g, device="cuda", dtype=torch.int32)
+    check_loss(v.view(-1, 1).repeat(1, C), y, [1] * T)
+    # the type's next values below among them
+    Z = v.view(-1, 1).repeat(1, C)
+    down = torch.nextafter(v, torch.full_like(v, -math.inf))
+    Z[:, 1::3] = down.view(-1, 1)
+    Z[:, 2::3] = torch.nextafter(down, torch.full_like(v, -math.inf)).view(-1, 1)
+    check_loss(Z, torch.zeros(T, dtype=torch.int32, device="cuda"), [1] * T)
+    # one logit of that size among ordinary ones, or behind and before smaller
+    # ones of a neighbouring power of two: at the label and elsewhere
+    for k in (20, 29, 30, 31, 32, 40, 66, 100, 124, 125, 126, 127):
+        top = 1.3 * 2.0 ** k
+        Z = normal(g, (6, C), dtype, 2.0)
+        Z[:2, C // 2] = top
+        Z[2:4] = -top
+        Z[2:4, C // 2] = 1.0
+        # every thread's maximum grows on its way through the row
+        Z[4:] = top / 2.0
+        Z[4:, C // 2:] = top
+        y = torch.tensor([C // 2, 1] * 2 + [C - 1, 0], dtype=torch.int32, device="cuda")
+        for rows in (0, 1, 2, 3, 4, 5):
+            check_loss(Z[rows:rows + 1].clone(), y[rows:rows + 1], [1])
+    for first, then in ((0.95, 1.05), (0.5, 1.9), (1.05, 0.95)):
+        for k in (30, 126):
+            Z = torch.full((1, C), first * 2.0 ** k, dtype=dtype, device="cuda")
+            Z[:, C // 2:] = then * 2.0 ** k
+            check_loss(Z, torch.tensor([C - 1 if then > first else 0], dtype=torch.int32, device="cuda"), [1])
+
+
 def test_token_loss_gradient_against_differences():
     g = gen(11)
     T, C, lengths = 12, 40, [5, 7]
