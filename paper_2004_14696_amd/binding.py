@@ -673,8 +673,23 @@ def _torch():
     return torch
 
 
+class _Simulation:
+    """A dbw_ctx, destroyed with the last reference to it: its Context's, and
+    those of views of its memory.  It refers to neither, as no collector would
+    find a cycle through a tensor's memory."""
+
+    def __init__(self, lib, handle):
+        self.lib, self.handle = lib, handle
+
+    def __del__(self):
+        try:
+            self.lib.dbw_destroy(self.handle)
+        except Exception:
+            pass
+
+
 class _DeviceArray:
-    """float32 [n] device memory of a context, for torch.as_tensor."""
+    """float32 [n] device memory of a _Simulation, for torch.as_tensor."""
 
     def __init__(self, owner, ptr, n):
         self.owner = owner
@@ -685,6 +700,7 @@ class Context:
     """One DBW parameter-server simulation bound to a torch CUDA (HIP) stream."""
 
     _adamw = None   # the plan of use_adamw
+    _simulation = None
 
     def __init__(self, cfg: Config, stream=None, device=None):
         torch = _torch()
@@ -698,12 +714,13 @@ class Context:
         if s != DBW_OK:
             raise DBWError(s, "dbw_create failed (invalid configuration or HIP error)")
         self.h = handle
+        self._simulation = _Simulation(self.lib, handle)
         self.P = param_count(cfg)
 
     def close(self):
-        if getattr(self, "h", None):
-            self.lib.dbw_destroy(self.h)
-            self.h = None
+        """Ends the simulation.  Its memory is freed here, or with the last
+        view of gradient() (a plan keeps those that it was given)."""
+        self.h = self._adamw = self._simulation = None
 
     def __del__(self):
         try:
@@ -812,11 +829,11 @@ class Context:
         return int(kout.value) if wait else None
 
     def gradient(self):
-        """The context's g_t [P], which every step writes (a view, valid while
-        the context is open): the gradients of a plan for use_adamw."""
+        """The context's g_t [P], which every step writes (a view, which keeps
+        the simulation's memory): the gradients of a plan for use_adamw."""
         bufs = StepBuffers()
         self._check(self.lib.dbw_step_outputs(self.h, ctypes.byref(bufs)), "dbw_step_outputs")
-        return _torch().as_tensor(_DeviceArray(self, bufs.g, self.P), device=self.device)
+        return _torch().as_tensor(_DeviceArray(self._simulation, bufs.g, self.P), device=self.device)
 
     def use_adamw(self, opt, lr=0.0, beta1=0.9, beta2=0.999, eps=1e-8, max_norm=0.0, grad_scale=1.0, seed=0):
         """From now on every step updates w by one step of ``opt`` (an AdamW

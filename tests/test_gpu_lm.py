@@ -894,6 +894,59 @@ def test_dbw_step_with_adamw_as_the_servers_update(model, kw, g_rows, bits):
     assert opt.t == 4
 
 
+def test_a_context_and_its_plan_end_with_their_last_reference():
+    import gc
+    import weakref
+
+    def simulation():
+        n, B, d, C = 4, 8, 1 << 21, 8                  # 64 MiB a parameter vector
+        ctx = pb.Context(pb.make_config("softmax", n, B, d, C))
+        w = torch.zeros(ctx.P, device="cuda")
+        view = ctx.gradient()
+        opt = pb.AdamW([w[:64]], [view[:64]], **pb.adamw_states([w[:64]]))
+        ctx.use_adamw(opt, lr=0.1)
+        return ctx, opt, w, view
+    gc.collect()
+    ctx, opt, w, view = simulation()
+    # memory that is only a context's (torch keeps what its tensors leave)
+    del opt, w, view
+    ref, plan = weakref.ref(ctx), weakref.ref(ctx._adamw)
+    torch.cuda.synchronize()
+    held = torch.cuda.mem_get_info()[0]
+    del ctx
+    gc.collect()
+    assert ref() is None and plan() is None
+    assert torch.cuda.mem_get_info()[0] - held > 64 << 20
+    # a closed context keeps no plan; a view, or a plan over it, keeps the memory
+    for last in ("view", "plan"):
+        ctx, opt, w, view = simulation()
+        ref, plan = weakref.ref(ctx), weakref.ref(opt)
+        view.fill_(3.0)
+        view[:64] = 0.5
+        held = torch.cuda.mem_get_info()[0]
+        ctx.close()
+        ctx.close()
+        if last == "view":
+            del opt
+            assert plan() is None
+        else:
+            del view
+        del ctx
+        gc.collect()
+        assert ref() is None and torch.cuda.mem_get_info()[0] - held < 64 << 20
+        if last == "view":
+            assert float(view[0]) == 0.5 and float(view[64:].min()) == 3.0 == float(view[64:].max())
+            del view
+        else:
+            opt.step(lr=0.25)                         # the first step moves every weight by lr
+            assert bool(((w[:64] + 0.25).abs() < 1e-5).all()) and not bool(w[64:].any())
+            del opt
+            assert plan() is None
+        gc.collect()
+        torch.cuda.synchronize()
+        assert torch.cuda.mem_get_info()[0] - held > 64 << 20
+
+
 def test_calls_on_another_stream_and_twice_give_the_same_bits():
     g = gen(33)
     T, d, C, n = 900, 256, 520, 7
