@@ -508,7 +508,8 @@ void dbw_adamw_destroy(dbw_adamw* opt);
 
 /* One step on `stream` of the plan's device (allocates nothing; t lives on
  * the device, so a captured step advances it at every replay).  norm, if not
- * NULL, is DEVICE float [1] and gets the norm before clipping.  Steps of one
+ * NULL, is DEVICE float [1] and gets the norm before clipping (infinite where
+ * fp32 cannot hold it: the step itself takes it in fp64).  Steps of one
  * plan must not run at the same time. */
 dbw_status dbw_adamw_step(dbw_adamw* opt, const dbw_adamw_hyper* hyper, float* norm, void* stream);
 

@@ -273,7 +273,11 @@ __global__ __launch_bounds__(kThreads) void k_adamw_prep(AdamStep* step, const d
   const int64_t t = step->t + (skip ? 0 : 1);
   step->t = t;
   step->skip = skip;
-  step->f = static_cast<float>(f);
+  // a factor near fp32's smallest values would lose its digits there: it goes in
+  // two, the first of which loses none of a gradient that matters
+  const double pre = fabs(f) < 0x1p-100 ? 0x1p-64 : 1.0;
+  step->f = static_cast<float>(f / pre);
+  step->pre = static_cast<float>(pre);
   step->ibc1 = 1.0 / (1.0 - pow(h.beta1, static_cast<double>(t)));
   step->ibc2 = static_cast<float>(1.0 / sqrt(1.0 - pow(h.beta2, static_cast<double>(t))));
   step->key = adam_mix(adam_mix(h.seed) + static_cast<uint32_t>(t));
@@ -293,7 +297,7 @@ __global__ __launch_bounds__(kThreads) void k_adamw_update(const AdamTensor* __r
   const int64_t first = static_cast<int64_t>(ch.index) * kAdamChunk;
   const int64_t left = t.count - first;
   const double lr = h.lr * t.lr_scale;
-  const float f = step->f, ibc2 = step->ibc2, eps = static_cast<float>(h.eps);
+  const float f = step->f, pre = step->pre, ibc2 = step->ibc2, eps = static_cast<float>(h.eps);
   const float keep = static_cast<float>(1.0 - lr * t.decay), rate = static_cast<float>(lr * step->ibc1);
   const float b1 = static_cast<float>(h.beta1), c1 = static_cast<float>(1.0 - h.beta1);
   const float b2 = static_cast<float>(h.beta2), c2 = static_cast<float>(1.0 - h.beta2);
@@ -307,6 +311,10 @@ __global__ __launch_bounds__(kThreads) void k_adamw_update(const AdamTensor* __r
   float w[4], g[4], m[4], v[4];
   load4(t.w + i, n, w);
   load4(static_cast<const G*>(t.g) + i, n, g);
+  if (pre != 1.f) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) g[j] *= pre;
+  }
   if (BITS == 32) {
     load4(static_cast<const float*>(t.m) + i, n, m);
     load4(static_cast<const float*>(t.v) + i, n, v);

@@ -89,7 +89,7 @@ struct AdamChunk {
 // Values of one step that all workgroups share, made by its first kernel.
 struct AdamStep {
   int64_t t;
-  float f;          // factor of the gradients
+  float f, pre;     // factors of the gradients: f, behind pre = 1 or 2^-64
   float ibc2;       // 1 / sqrt(1 - beta2^t)
   double ibc1;      // 1 / (1 - beta1^t)
   uint32_t key;     // mix(mix(seed) + t)

@@ -687,6 +687,27 @@ def test_adamw_norm_of_large_and_small_gradients():
     assert abs(float(norm) - 1e-30 * math.sqrt(1e5)) <= 4 * u * 1e-27
 
 
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_adamw_clips_norms_whose_factor_fp32_cannot_hold(bits, dtype):
+    # gradients of 2^100 to 2^127: factors down to 2^-145, below 2^-126 with
+    # fewer digits than fp32 has
+    for top in (100, 117, 127):
+        opt, w, g, st, lows = make([70001, 500], bits, dtype, None, 26)
+        for x in g:
+            x.copy_(x.float().clamp(-0.5, 0.5) * 2.0 ** top)
+        g[1][:400] *= 2.0 ** -30
+        norm = math.sqrt(sum(float((x.double() ** 2).sum()) for x in g))
+
+        class Plan:                                    # a norm beyond fp32 is told as infinite
+            @staticmethod
+            def step(**kw):
+                got = float(opt.step(**kw))
+                assert abs(got - norm) <= 2 * u * norm or (got == math.inf and norm > torch.finfo(torch.float32).max)
+                return norm
+        check_step(Plan, w, g, st, lows, 1, max_norm=1e-3 if top > 100 else 1.0)
+
+
 def test_adamw_8_bit_states_keep_their_mean():
     # v moves by 1e-3 of itself a step, a code apart by 6 to 12%: only the
     # random rounding lets it decay.  After t steps without gradients the mean of
