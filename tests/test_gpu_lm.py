@@ -236,6 +236,51 @@ def test_products_beyond_two_to_the_31_elements():
     assert not bool(Y[:-70].any()) and not bool(dX[:-70].any())
 
 
+def test_rows_around_two_to_the_31_elements_reach_their_sums():
+    # rows at the start, around the 2^31st element of X (and of dX) and at the
+    # end; all others are 0, and add no rounding: K is what is left of them and
+    # the parts of a sum, at most 64
+    T, d, C = (1 << 21) + 3, 1032, 8
+    edge = (1 << 31) // d
+    rows = torch.cat([torch.arange(40), torch.arange(edge - 30, edge + 30), torch.arange(T - 50, T)]).cuda()
+    X = torch.zeros((T, d), dtype=torch.bfloat16, device="cuda")
+    dY = torch.zeros((T, C), dtype=torch.bfloat16, device="cuda")
+    X[rows], dY[rows] = normal(gen(60), (150, d), torch.bfloat16), normal(gen(61), (150, C), torch.bfloat16)
+    W = normal(gen(62), (2, d, C), torch.bfloat16)
+    lengths, some = [edge + 7, T - edge - 7], [77, 73]     # of the rows that are not 0
+    off = offsets_of(lengths)
+    for form, a, b, got, K in (("forward", X[rows], W, pb.group_matmul(X, W, off), d),
+                               ("input", dY[rows], W, pb.group_input_grad(dY, W, off), C),
+                               ("weight", X[rows], dY[rows], pb.group_weight_grad(X, dY, off), 77 + 64)):
+        mine = got if form == "weight" else got[rows]
+        ref, size = product_ref(form, a, b, some, 0, torch.zeros_like(mine))
+        assert bool(((mine.double() - ref).abs() <= 2 * K * u * size + rounded(ref, got.dtype)).all()), form
+        if form != "weight":
+            got[rows] = 0
+            assert not bool(got.any()), form
+
+
+def test_weights_beyond_two_to_the_31_elements():
+    # W and G of 2.25e9 values: the first groups, those around the 2^31st element
+    # (2^32 bytes of W, and of G half way), the last
+    n, d, C = 1000, 1504, 1496
+    edge = (1 << 31) // (d * C)
+    groups = [0, 1, edge // 2 - 1, edge // 2, edge // 2 + 1, edge - 1, edge, edge + 1, n - 2, n - 1]
+    lengths = [2 + i % 2 for i in range(n)]
+    off = offsets_of(lengths)
+    T = sum(lengths)
+    X, dY = normal(gen(63), (T, d), torch.bfloat16), normal(gen(64), (T, C), torch.bfloat16)
+    W = torch.empty((n, d, C), dtype=torch.bfloat16, device="cuda").normal_(generator=gen(65))
+    got = {"forward": pb.group_matmul(X, W, off), "input": pb.group_input_grad(dY, W, off),
+           "weight": pb.group_weight_grad(X, dY, off)}
+    for i in groups:
+        rows = slice(int(off[i]), int(off[i + 1]))
+        for form, a, b, K in (("forward", X, W[i], d), ("input", dY, W[i], C), ("weight", X, dY, 3)):
+            mine = got[form][i:i + 1] if form == "weight" else got[form][rows]
+            ref, size = product_ref(form, a[rows], b[rows] if form == "weight" else b, [lengths[i]], 0, torch.zeros_like(mine))
+            assert bool(((mine.double() - ref).abs() <= 2 * K * u * size + rounded(ref, mine.dtype)).all()), (form, i)
+
+
 # -- token loss -------------------------------------------------------------------
 def loss_ref(Z, y, lengths, first, scale):
     Z = Z.double()
