@@ -747,21 +747,45 @@ Estimate best_plan(const dbw_group_shape& p, int variant) {
   return best;
 }
 
+// The parts of G's sums in 128 x 128 tiles, by an estimate of the time in us:
+// steps of 64 terms, with one workgroup on a CU and with two, and what the parts
+// cost: a launch, their loads (eight under way at once) and every workgroup's
+// part written and read; where the lines are whole chunks, and where not.
+// Fitted to 2 to 256 tiles with 2048, 8192 and 30000 terms (and 1024 in odd
+// widths) in 1 to 64 parts; of the parts timed, its choice took at most 17% more
+// than the fastest.
+// Neither one nor two workgroups a CU is best throughout (us for 256 and for 512
+// workgroups): 2048 terms 64 tiles 21 and 24, 192 tiles 25 and 30; 8192 terms 24
+// tiles 20 and 23, 64 tiles 32 and 30, 128 tiles 53 and 43; 30000 terms 32 tiles 49
+// and 41, 64 tiles 87 and 66, 128 tiles 166 and 137.
+int weight_grad_parts(const dbw_group_shape& p, int64_t tiles) {
+  const bool whole = p.d % 8 == 0 && p.C % 8 == 0 && p.ld_d % 8 == 0 && p.ld_C % 8 == 0;
+  const double one = whole ? 0.60 : 1.27, two = whole ? 0.88 : 1.57;
+  const double launch = whole ? 3.3 : 4.4, load = whole ? 0.17 : 0.90, block = whole ? 0.0145 : 0.026;
+  const int64_t length = terms(p);
+  const int most = static_cast<int>(std::min<int64_t>({512 / tiles, length / 256, 64}));
+  int best = 1;
+  double best_us = 0.0;
+  for (int s = 1; s <= most; ++s) {
+    const int64_t blocks = tiles * s, steps = ceil_div(ceil_div(length, 64), s);
+    const double us = steps * (blocks <= 256 ? one : two) + (s > 1 ? launch + load * (s / 8 + s % 8) + block * blocks : 0.0);
+    if (s == 1 || us < best_us) {
+      best = s;
+      best_us = us;
+    }
+  }
+  return best;
+}
+
 }  // namespace
 
 GroupPlan group_plan(const dbw_group_shape& p) {
   if (p.form == DBW_GROUP_WEIGHT_GRAD) {
     // 128 x 256: more products a value read, from one and a half tiles a CU on
     // (1 x 4096 x 1024 x 8192: 81 us either way; 32 groups 8192 x 2048 x 1536: 104
-    // against 121 us).  Below, parts of the sum for one workgroup a CU, each
-    // with 256 terms at least; a second one a CU is lost again to the sum of
-    // the parts (1 x 4096 x 1024 x 4096: 56 against 48 us) but with very few tiles
-    // (2 x 15000 x 512 x 512, 32 tiles: 38 against 46 us).
+    // against 121 us).  Below, parts of the sum, each with 256 terms at least.
     if (const GroupPlan large = plan_of(p, LARGE, 1); large.tiles >= 384) return large;
-    const GroupPlan middle = plan_of(p, MIDDLE, 1);
-    const int64_t target = middle.tiles <= 32 ? 512 : 256;
-    return plan_of(p, MIDDLE,
-                   static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({target / middle.tiles, terms(p) / 256, 64}))));
+    return plan_of(p, MIDDLE, weight_grad_parts(p, plan_of(p, MIDDLE, 1).tiles));
   }
   // Y in tiles of 128 x 256 from one and a half a CU on (1 x 4096 x 1024 x 4096, 512
   // tiles: 37 against 47 us; 1 x 2560 x 1024 x 4096, 320 tiles: 32 against 33 us; 1 x

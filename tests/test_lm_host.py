@@ -172,6 +172,24 @@ def test_unaligned_products_near_the_most_tiles_are_refused(lib):
     assert lib.dbw_group_workspace(ctypes.byref(s), ctypes.byref(need)) == pb.DBW_OK and need.value == 0
 
 
+@pytest.mark.parametrize("tiles,d,C", [(1, 100, 128), (16, 512, 512), (32, 512, 1024), (33, 1408, 384), (36, 768, 768),
+                                       (64, 1024, 1024), (128, 1024, 2048), (192, 1536, 2048), (256, 2048, 2048),
+                                       (280, 2560, 1792), (64, 1021, 1023)])
+def test_parts_of_weight_gradients(lib, tiles, d, C):
+    # parts of 256 terms at least, in at most 512 workgroups and 64 parts; the
+    # longest sums take more than half of what they may, at any number of tiles
+    last = 1
+    for T in (1, 200, 511, 512, 1024, 2048, 4096, 8192, 16384, 65536, 1 << 20, 1 << 30):
+        s = _shape(form=pb.DBW_GROUP_WEIGHT_GRAD, out_dtype=pb.DBW_F32, n=1, T=T, d=d, C=C, ld_d=d, ld_C=C, ld_W=C, st_W=0)
+        need = ctypes.c_int64(-5)
+        assert lib.dbw_group_workspace(ctypes.byref(s), ctypes.byref(need)) == pb.DBW_OK
+        parts = max(1, need.value // (4 * d * C))
+        assert need.value in (0, 4 * parts * d * C)
+        assert parts == 1 or (parts * tiles <= 512 and parts <= 64 and parts * 256 <= T)
+        last = parts
+    assert last > min(64, 512 // tiles) // 2 or 512 // tiles == 1
+
+
 def test_adamw_refuses_arrays_that_overlap(lib):
     # two tensors of 300 values, states in 8 bits, each array at a place of its own
     def create(edit):
