@@ -163,10 +163,9 @@ __device__ __forceinline__ uint32_t lane_least(const float (&x)[4]) {
 //
 // Where all values are finite and none but zeros is below 2^-6 in units of the
 // scale, the conversion with stochastic rounding gives the formula's codes, sign
-// included (compared for all floats of [2^-6, 448], each with the drawn bits
-// where its code turns and others: 10^9 pairs; of smaller values 4 in 10^5
-// pairs differ, where the formula's sum in fp32 is rounded).  It takes one
-// instruction a value for some fifteen.
+// included (a test compares all floats of [2^-6, 448], each with bits of the
+// mix; of smaller values some pairs differ, where the formula's sum in fp32 is
+// rounded).  It takes one instruction a value for some fifteen.
 template <bool FLOOR>
 __device__ __forceinline__ uint32_t encode(const float (&x)[4], const uint32_t (&bits)[4], uint32_t most,
                                            uint32_t* scale) {
@@ -212,8 +211,9 @@ __device__ __forceinline__ uint32_t encode(const float (&x)[4], const uint32_t (
 // sqrt(v), correctly rounded for v = 0 and from 2^-100 to 2^127: y is within an
 // ulp or so of 1/sqrt(v), g of sqrt(v), and one Newton step with its residual,
 // which is exact in a fused multiply-add, gives the rounded root (Markstein,
-// "Computation of elementary functions on the IBM RISC System/6000", 1990;
-// compared for every float of that range).  Other v that are not 0 give a root
+// "Computation of elementary functions on the IBM RISC System/6000", 1990; a
+// test compares updates by 2^24 roots at five powers of four with those by
+// sqrtf).  Other v that are not 0 give a root
 // below 2^-50, an infinity or a NaN.
 __device__ __forceinline__ float root(float v) {
   const float y = __builtin_amdgcn_rsqf(fmaxf(v, 0x1p-100f));

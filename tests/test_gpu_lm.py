@@ -691,6 +691,57 @@ def test_adamw_8_bit_codes_are_exactly_those_of_their_definition():
             assert np.array_equal(got[~odd], want[~odd]), (i, name, np.sum(got[~odd] != want[~odd]))
 
 
+def test_adamw_8_bit_codes_of_every_float_of_a_scale():
+    # every fp32 value of [2^-6, 448], 255 to a block beside a 448 that sets the
+    # scale to 1, signs in turn: m = x, r = sqrt(x^2) = |x|.  Codes against the
+    # definition, whose sum of place and random bits is rounded to fp32
+    first, last = 0x3C800000, 0x43E00000
+    blocks = -(-(last - first + 1) // 255)
+    x = torch.arange(first, first + blocks * 255, dtype=torch.int32, device="cuda").clamp(max=last).view(blocks, 255)
+    x = torch.cat([torch.full((blocks, 1), last, dtype=torch.int32, device="cuda"), x], 1).view(torch.float32)
+    x[:, 1::2] *= -1
+    w = [torch.zeros(x.numel(), device="cuda")]
+    st = pb.adamw_states(w, 8)
+    opt = pb.AdamW(w, [x.view(-1)], **st)
+    opt.step(lr=1e-3, beta1=0.0, beta2=0.0, seed=17)
+    for name in ("m_scale", "v_scale"):
+        assert bool((st[name][0].view(torch.uint8) == 127).all())
+    M = 0xFFFFFFFF
+
+    def mix_t(h):
+        h = (h ^ (h >> 16)) * 0x9E3779B1 & M
+        h = (h ^ (h >> 15)) * 0xB7E15163 & M
+        return h ^ (h >> 16)
+    key = int(mix(mix(mix(np.uint64(17)) + np.uint64(1) & np.uint64(M)) & np.uint64(M)))
+    step = 1 << 24
+    for at in range(0, x.numel(), step):
+        val = x.view(-1)[at:at + step]
+        index = torch.arange(at, at + len(val), device="cuda")
+        bits = mix_t((index * 0x6A09E667 + key) & M)
+        y = val.abs().double()
+        ey = (val.view(torch.int32) >> 23 & 0xFF).long() - 127
+        for name, part, sign in (("m", bits & 0xFFFF, val < 0), ("v", bits >> 16, None)):
+            place = (y * torch.exp2(3.0 - ey) + part.double() / 65536).float()
+            want = (ey + 6) * 8 + place.long() + (128 * sign if sign is not None else 0)
+            got = st[name][0].view(torch.uint8)[at:at + step].long()
+            assert torch.equal(got, want), (name, at, int((got != want).sum()))
+
+
+def test_adamw_takes_the_same_roots_with_either_states():
+    # from zero states a step's update depends on the root alone, which the two
+    # kinds of states take by different instructions: the same bits for every
+    # fp32 gradient of [1, 4), at several powers of four
+    x = torch.arange(0x3F800000, 0x40800000, dtype=torch.int32, device="cuda").view(torch.float32)
+    for power in (-20, -6, 0, 7, 28):
+        g = x * 4.0 ** power
+        out = []
+        for bits in (32, 8):
+            w = [torch.zeros_like(g)]
+            pb.AdamW(w, [g], **pb.adamw_states(w, bits)).step(lr=1.0, beta1=0.9, beta2=0.99, eps=1e-30)
+            out.append(w[0])
+        assert torch.equal(*out) and bool((out[0] < -0.99).all()), power
+
+
 def test_adamw_of_empty_and_zero_tensors():
     opt, w, g, st, lows = make([0, 300, 0], 8, torch.float32, None, 23)
     g[1].zero_()
