@@ -495,7 +495,8 @@ def token_loss(Z, y, offsets, scale=1.0, dZ=None, loss=None, grad=True, workspac
     (dbw_token_loss).  Z [T][C] float32, bfloat16 or float16 logits, y [T] int32
     labels (negative: the row is masked), offsets [n+1] int32.  Returns
     (loss [n] float32, dZ [T][C] of the type of Z, times ``scale``); dZ may be
-    Z, to write the gradient in its place; ``grad`` False: no gradient (None)."""
+    Z, to write the gradient in its place; ``grad`` False: no gradient (None),
+    and nothing is written to a dZ that is given."""
     if stream is not None:
         return _on(stream, Z.device, token_loss, Z, y, offsets, scale, dZ, loss, grad, workspace)
     torch = _torch()
@@ -510,7 +511,9 @@ def token_loss(Z, y, offsets, scale=1.0, dZ=None, loss=None, grad=True, workspac
     po = _flat(offsets, (n + 1,), torch.int32, dev, "offsets")
     py = _flat(y, (T,), torch.int32, dev, "y")
     pz, ld_Z = _rows_of(Z, (T, C), dtype, dev, "Z")
-    if dZ is None and grad:
+    if not grad:
+        dZ = None
+    elif dZ is None:
         dZ = torch.empty((T, C), dtype=dtype, device=dev)
     pd, ld_dZ = _rows_of(dZ, (T, C), dtype, dev, "dZ") if dZ is not None else (None, 0)
     if loss is None:

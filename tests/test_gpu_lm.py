@@ -448,6 +448,19 @@ def test_token_loss_of_logits_of_any_magnitude(C, dtype):
             check_loss(Z, torch.tensor([C - 1 if then > first else 0], dtype=torch.int32, device="cuda"), [1])
 
 
+def test_token_loss_without_a_gradient_writes_none():
+    g = gen(13)
+    Z = normal(g, (5, 300), torch.bfloat16)
+    y = torch.tensor([1, 0, -1, 299, 7], dtype=torch.int32, device="cuda")
+    off = offsets_of([2, 3])
+    want, _ = pb.token_loss(Z, y, off)
+    before, buffer = Z.clone(), torch.full_like(Z, 2.0)
+    for dZ in (None, buffer, Z):
+        loss, none = pb.token_loss(Z, y, off, dZ=dZ, grad=False)
+        assert none is None and torch.equal(loss, want) and torch.equal(Z, before)
+    assert bool((buffer == 2.0).all())
+
+
 def test_token_loss_gradient_against_differences():
     g = gen(11)
     T, C, lengths = 12, 40, [5, 7]
