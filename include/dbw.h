@@ -426,10 +426,11 @@ typedef struct {
 dbw_status dbw_group_workspace(const dbw_group_shape* shape, int64_t* bytes);
 
 /* One product.  offsets, a, b, out and workspace are DEVICE; out must not
- * overlap the inputs, and rows (or G_i) of out must not overlap each other.
- * workspace holds at least dbw_group_workspace bytes, 16-byte aligned (NULL
- * where that is 0); its contents need no clearing and are used up when the
- * call is done: calls that may run at the same time need their own. */
+ * overlap the inputs (DBW_EINVAL where it is one of them), and rows (or G_i) of
+ * out must not overlap each other.  workspace holds at least
+ * dbw_group_workspace bytes, 16-byte aligned (NULL where that is 0); its
+ * contents need no clearing and are used up when the call is done: calls that
+ * may run at the same time need their own. */
 dbw_status dbw_group_product(const dbw_group_shape* shape, const int32_t* offsets, const void* a, const void* b,
                              void* out, void* workspace, int64_t workspace_bytes, void* stream);
 

@@ -95,6 +95,8 @@ DBW_API dbw_status dbw_group_product(const dbw_group_shape* shape, const int32_t
   if (need > 0 && (!workspace || workspace_bytes < need || !aligned(workspace, 16)))
     return set_free_error(DBW_EINVAL, "%s: needs %lld bytes of workspace, 16-byte aligned (%lld given)", call,
                           (long long)need, (long long)workspace_bytes);
+  if (out && (out == a || out == b))
+    return set_free_error(DBW_EINVAL, "%s: out must not overlap the inputs", call);
   const dbw::GroupPlan plan = dbw::group_plan(*shape);
   const hipError_t e = dbw::launch_group(*shape, plan, offsets, a, b, out, static_cast<float*>(workspace),
                                          static_cast<hipStream_t>(stream));

@@ -65,6 +65,15 @@ def test_group_product_refuses_pointers_and_workspaces(lib):
     assert lib.dbw_group_workspace(ctypes.byref(s), None) == pb.DBW_EINVAL
 
 
+def test_group_product_refuses_an_output_in_the_place_of_an_input(lib):
+    other, third = ctypes.c_void_p(1 << 20), ctypes.c_void_p(1 << 21)
+    for form in (pb.DBW_GROUP_FORWARD, pb.DBW_GROUP_INPUT_GRAD, pb.DBW_GROUP_WEIGHT_GRAD):
+        s = _shape(form=form, d=32, ld_d=32, st_W=32 * 32)
+        for a, b, out in ((P, other, P), (P, other, other)):
+            assert lib.dbw_group_product(ctypes.byref(s), third, a, b, out, third, 1 << 40, NULL) == pb.DBW_EINVAL
+            assert b"overlap" in lib.dbw_last_error(None)
+
+
 def test_token_loss_refusals(lib):
     assert lib.dbw_token_workspace(0, 1) == -1 and lib.dbw_token_workspace(1, -1) == -1
     assert lib.dbw_token_workspace(pb.DBW_MAX_N + 1, 1) == -1 and lib.dbw_token_workspace(1, 1 << 31) == -1
