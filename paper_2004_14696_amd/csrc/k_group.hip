@@ -19,12 +19,12 @@
 // of the cycles, the rest LDS reads and barriers.  4096 rows, 16384 columns, bf16,
 // TFLOP/s of Y, G and dX (a library product): 256 terms 670, 600, 540 (570); 1024
 // 1030, 1050, 845 (1070); 4096 1310, 1370, 1155 (1370); 8192 1215, 1315, 1035
-// (1390).  Head 4096 x 1024 x 32000 258 us, 1040 TFLOP/s.  Ragged
-// groups, how evenly their tiles fall on the CUs: 32 groups 8192 x 2048 x 1536 80
-// us, 650 TFLOP/s and 3.3 TB/s.  G of short minibatches, its stores: 16 workers
-// 8000 x 784 x 4000 78 us (200 MB; streamed past the caches 123 us became 107 for
-// 32 groups, in pieces of 16 bytes instead of lines they had taken 163).  Few
-// rows, the weights from memory: 16 groups 37 x 2048 x 1408 16.6 us, 5.6 TB/s.
+// (1390).  Head 4096 x 1024 x 32000 254 us, 1060 TFLOP/s.  Ragged groups, how evenly
+// their tiles fall on the CUs: 32 groups (28 with rows) 8192 x 2048 x 1536 79 us, 650
+// TFLOP/s and 3.0 TB/s.  G of short minibatches, its stores: 16 workers 8000 x 784 x
+// 4000 78 us (200 MB; streamed past the caches 123 us became 107 for 32 groups, in
+// pieces of 16 bytes instead of lines they had taken 163).  Few rows, the weights
+// from memory: 16 groups (14 with rows) 37 x 2048 x 1408 16.5 us, 4.9 TB/s.
 //
 // v_mfma_f32_16x16x32 takes, in lane l = 16 g + c, row c and terms 8 g .. 8 g
 // + 7 of each operand; its result r of a lane is row 4 g + r of the first

@@ -17,7 +17,7 @@
 // stores: 8192 x 50257 bf16 330 us, 5.0 TB/s (a large copy reaches 4.9), where 1024
 // threads of 8 packs, alone on a CU, took 542.  Rows of up to 131072 16-bit
 // values fill a CU by themselves (2048 x 128000 fp16 233 us, 4.5 TB/s), longer ones
-// are read twice (1024 x 200000 bf16 239 us, 3.4 TB/s by their size).
+// are read twice (1024 x 200000 bf16 233 us, 3.5 TB/s by their size).
 //
 // softmax(z)_c = 2^(b (z_c - max)) / sum 2^(b (z - max)) with b = log2(e), in
 // fp32.  The difference comes first where that costs nothing: it is 0 at the
