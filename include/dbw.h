@@ -444,10 +444,10 @@ dbw_status dbw_group_product(const dbw_group_shape* shape, const int32_t* offset
  *   dZ[t][c] = (scale/count_i) (softmax(Z[t])_c - [c = y_t])
  * dZ (DEVICE, of dtype, row stride ld_dZ) may be NULL (no gradient) or Z
  * itself; it must not overlap Z otherwise.  Sums are held in fp32, a worker's
- * over its rows in fp64 in a fixed order.  Logits of -infinity have
- * probability 0; a row with a NaN, a +infinity or only -infinities, and a row
- * whose label is >= C, give a NaN loss and a NaN gradient row.  scale must be
- * finite.  n in [1, DBW_MAX_N], C in [1, 2^24], T below 2^31.  workspace
+ * over its rows in fp64 in a fixed order.  Logits of -infinity, and those whose
+ * probability is below 2^-126 of the row's largest, have probability 0; a row
+ * with a NaN, a +infinity or only -infinities, and a row whose label is >= C,
+ * give a NaN loss and a NaN gradient row.  scale must be finite.  n in [1, DBW_MAX_N], C in [1, 2^24], T below 2^31.  workspace
  * (DEVICE, 16-byte aligned, at least dbw_token_workspace bytes): as for
  * dbw_group_product. */
 int64_t dbw_token_workspace(int32_t n, int64_t T);
