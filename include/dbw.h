@@ -535,6 +535,135 @@ dbw_status dbw_set_adamw(dbw_ctx* ctx, dbw_adamw* opt, const dbw_adamw_hyper* hy
  * for the halves lo and hi of index. */
 uint32_t dbw_adamw_bits(uint32_t seed, int64_t t, int32_t tensor, int64_t index);
 
+/* ---------------------------------------------------------------------------
+ * A transformer block in training, beside the products, the loss and the
+ * update above: attention, layer norm, the products with what surrounds them,
+ * and dropout.  The rules above hold here too: no context, a stream, device
+ * offsets of n ragged groups (the workers' rows; for attention the sequences),
+ * nothing allocated, capturable; rows of no group are not read, and left as
+ * they were in outputs.  Outputs must not overlap inputs or each other, but for
+ * what is said below (DBW_EINVAL where one is the other).  Vectors of weights
+ * (gamma, beta, bias) are fp32, as AdamW keeps them, and so are their
+ * gradients, one row for each worker: with the row stride P they lie in the
+ * worker gradients G [n][P].  NaN and infinities of one group's rows never
+ * reach another's. */
+
+/* Layer norm: with the mean and variance (of all d values) of row t,
+ *   H[t] = (X[t] - mean) / sqrt(var + eps),   Y[t] = H[t] gamma + beta.
+ * X and Y are DEVICE [T][d] of dtype (row strides ld_X, ld_Y, in elements),
+ * gamma and beta DEVICE float [d] (beta may be NULL: 0).  Statistics are formed
+ * in fp32, the variance from differences to the mean.  n in [1, DBW_MAX_N], d
+ * in [1, 16384] (DBW_EUNSUPPORTED above), T below 2^31, eps in [1e-30, 1e30]. */
+dbw_status dbw_layer_norm(int32_t n, int64_t T, int32_t d, int32_t dtype, const int32_t* offsets, const void* X,
+                          int64_t ld_X, const float* gamma, const float* beta, double eps, void* Y, int64_t ld_Y,
+                          void* stream);
+
+/* Its gradients, from the same X (the statistics are formed again):
+ *   dX[t] = (dH - mean(dH) - H mean(dH H)) / sqrt(var + eps),  dH = dY[t] gamma
+ *   dgamma_i = sum over the rows t of group i of dY[t] H[t],  dbeta_i = sum dY[t]
+ * dX is DEVICE [T][d] of dtype, dgamma and dbeta DEVICE float [n][d] (row
+ * strides ld_dgamma, ld_dbeta; zero for an empty group; dbeta may be NULL).
+ * The sums are taken in a fixed order.  workspace: as for dbw_group_product, at
+ * least dbw_layer_norm_workspace bytes (-1 for arguments out of range). */
+int64_t dbw_layer_norm_workspace(int32_t n, int64_t T, int32_t d);
+dbw_status dbw_layer_norm_grad(int32_t n, int64_t T, int32_t d, int32_t dtype, const int32_t* offsets, const void* dY,
+                               int64_t ld_dY, const void* X, int64_t ld_X, const float* gamma, double eps, void* dX,
+                               int64_t ld_dX, float* dgamma, int64_t ld_dgamma, float* dbeta, int64_t ld_dbeta,
+                               void* workspace, int64_t workspace_bytes, void* stream);
+
+/* A product with bias, activation and residual:
+ *   Z[t] = X[t] W_i + b_i,   Y[t] = act(Z[t]) + R[t]
+ * for the rows t of group i; the FORWARD form of dbw_group_product, whose
+ * shape, workspace and rules it has.  act(z) = z, max(z, 0), z / (1 + exp(-2 (a
+ * z + b z^3))) with a = sqrt(2/pi), b = 0.044715 a (the tanh form of GELU), or z
+ * / (1 + exp(-z)).  Z and Y are rounded once each, from the fp32 sum. */
+typedef enum { DBW_ACT_NONE = 0, DBW_ACT_RELU = 1, DBW_ACT_GELU = 2, DBW_ACT_SILU = 3 } dbw_activation;
+typedef struct {
+  int32_t activation;   /* dbw_activation                                    */
+  const float* bias;    /* DEVICE [C] of group i at bias + i st_bias, or NULL */
+  int64_t st_bias;      /* >= C, or 0: the same for all groups, as it has to be
+                           where the groups share W                          */
+  const void* residual; /* DEVICE [T][C] of out_dtype, or NULL; may be Y     */
+  int64_t ld_residual;  /* row stride, below 2^21; that of Y where it is Y   */
+  void* pre;            /* DEVICE [T][C] of dtype: gets Z (for
+                           dbw_linear_grad), or NULL                         */
+  int64_t ld_pre;       /* row stride, below 2^21                            */
+} dbw_linear_epilogue;
+dbw_status dbw_group_linear(const dbw_group_shape* shape, const dbw_linear_epilogue* epilogue, const int32_t* offsets,
+                            const void* X, const void* W, void* Y, void* workspace, int64_t workspace_bytes,
+                            void* stream);
+
+/* The way back to Z and the bias:
+ *   dZ[t] = dY[t] act'(Z[t]),   dbias_i = sum over the rows t of group i of dZ[t]
+ * (from there dbw_group_product: INPUT_GRAD and WEIGHT_GRAD of dZ; the
+ * gradient to R is dY).  dY, Z and dZ are DEVICE [T][C] of dtype (fp32, bf16
+ * or fp16); Z may be NULL with DBW_ACT_NONE, and dZ too (then only dbias is
+ * formed).  dbias is DEVICE float [n][C], row stride ld_dbias, zero for an
+ * empty group, a sum in a fixed order of the values before they are rounded;
+ * NULL: not formed.  act'(0) of RELU is 0.  C in [1, 2^20].  workspace: at
+ * least dbw_linear_grad_workspace bytes. */
+int64_t dbw_linear_grad_workspace(int32_t n, int64_t T, int32_t C);
+dbw_status dbw_linear_grad(int32_t n, int64_t T, int32_t C, int32_t dtype, int32_t activation, const int32_t* offsets,
+                           const void* dY, int64_t ld_dY, const void* Z, int64_t ld_Z, void* dZ, int64_t ld_dZ,
+                           float* dbias, int64_t ld_dbias, void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Causal attention over packed sequences: group i is a sequence, and for its
+ * rows t and each of `heads` heads, whose keys and values are those of head
+ * floor(head kv_heads / heads),
+ *   S[t][s] = scale Q[t] . K[s]  for the rows s <= t of t's sequence,
+ *   lse[t] = log sum_s exp S[t][s],   O[t] = sum_s exp(S[t][s] - lse[t]) V[s].
+ * Products take bf16 or fp16 and sum in fp32; the exponentials are rounded to
+ * dtype for the second product, and summed unrounded.  Arrays are DEVICE
+ * [T][heads or kv_heads][D] of dtype, the D values contiguous; lse is DEVICE
+ * float [heads][T], or NULL.  NaN and infinities of a row may reach all rows of
+ * its sequence. */
+typedef struct {
+  void* data;             /* 16-byte aligned                                 */
+  int64_t token, head;    /* elements from a token, or a head, to the next:
+                             multiples of 8, token below 2^21, head below 2^40;
+                             not below 0, and outputs' rows apart            */
+} dbw_heads;
+typedef struct {
+  int32_t dtype;           /* DBW_BF16 or DBW_F16                            */
+  int32_t n;               /* sequences, in [1, 65536]                       */
+  int32_t heads, kv_heads; /* kv_heads divides heads; heads at most 1024     */
+  int32_t D;               /* a multiple of 8, in [8, 128]                   */
+  int64_t T;               /* rows, in [0, 2^31)                             */
+  double scale;            /* in [1e-20, 1e20]                               */
+} dbw_attention_shape;
+dbw_status dbw_attention(const dbw_attention_shape* shape, const int32_t* offsets, const dbw_heads* Q,
+                         const dbw_heads* K, const dbw_heads* V, const dbw_heads* O, float* lse, void* stream);
+
+/* Its gradients, from O and lse of the call above:
+ *   P[t][s] = exp(S[t][s] - lse[t]),   dV[s] = sum_t P[t][s] dO[t],
+ *   dS[t][s] = P[t][s] (dO[t] . V[s] - dO[t] . O[t]),
+ *   dQ[t] = scale sum_s dS[t][s] K[s],   dK[s] = scale sum_t dS[t][s] Q[t]
+ * with dK and dV summed over the heads that share them, in a fixed order.  P
+ * and dS are rounded to dtype for the products.  workspace: at least
+ * dbw_attention_workspace bytes (-1 for a shape out of range). */
+int64_t dbw_attention_workspace(const dbw_attention_shape* shape);
+dbw_status dbw_attention_grad(const dbw_attention_shape* shape, const int32_t* offsets, const dbw_heads* dO,
+                              const dbw_heads* Q, const dbw_heads* K, const dbw_heads* V, const dbw_heads* O,
+                              const float* lse, const dbw_heads* dQ, const dbw_heads* dK, const dbw_heads* dV,
+                              void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Dropout, with a mask that is never stored:
+ *   Y[t][c] = R[t][c] + (u[t][c] >= q ? X[t][c] * 65536 / (65536 - q) : 0)
+ * with q = round(65536 p), p in [0, 1] (q = 65536: Y = R), and u the 16 random
+ * bits of a value: those at 16 (c mod 8) of the 128 bits of Philox4x32-10
+ * (Salmon, Moraes, Dror and Shaw, 2011), with the low half of each word before
+ * its high half, counter (floor(c/8), t, low and high half of *step), key (low
+ * and high half of seed); see dbw_dropout_bits.  The gradient to X is the same
+ * call on dY, without R.  X, Y and R (may be NULL: 0) are DEVICE [T][d] of
+ * dtype; Y may be X or R, with its row stride.  step is DEVICE int64 [1] (NULL:
+ * 0), so that a captured call draws anew at each replay.  d in [1, 2^20]. */
+dbw_status dbw_dropout(int32_t n, int64_t T, int32_t d, int32_t dtype, const int32_t* offsets, const void* X,
+                       int64_t ld_X, double p, uint64_t seed, const int64_t* step, const void* R, int64_t ld_R,
+                       void* Y, int64_t ld_Y, void* stream);
+
+/* The 16 bits u of value [t][c] (HOST). */
+uint32_t dbw_dropout_bits(uint64_t seed, int64_t step, int64_t t, int32_t c);
+
 #ifdef __cplusplus
 }
 #endif

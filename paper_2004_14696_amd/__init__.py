@@ -7,12 +7,13 @@ kernels for gfx950 behind the C ABI of ``include/dbw.h``.  This package is
 the Python binding of that library.
 """
 from .binding import (DBW_MLP, DBW_SOFTMAX, AdamW, Config, Context, DBWError, adamw_states,  # noqa: F401
-                      grads_route, group_input_grad, group_matmul, group_weight_grad, load_library, make_config,
-                      param_count, time_estimate, token_loss)
+                      attention, attention_grad, dropout, grads_route, group_input_grad, group_linear,
+                      group_linear_grad, group_matmul, group_weight_grad, layer_norm, layer_norm_grad, load_library,
+                      make_config, param_count, time_estimate, token_loss)
 
-__all__ = ["AdamW", "Config", "Context", "DBWError", "adamw_states", "grads_route", "group_input_grad",
-           "group_matmul", "group_weight_grad", "load_library", "make_config", "param_count", "time_estimate",
-           "token_loss", "DBW_SOFTMAX", "DBW_MLP", "config_from"]
+__all__ = ["AdamW", "Config", "Context", "DBWError", "adamw_states", "attention", "attention_grad", "dropout",
+           "grads_route", "group_input_grad", "group_linear", "group_linear_grad", "group_matmul", "group_weight_grad",
+           "layer_norm", "layer_norm_grad", "load_library", "make_config", "param_count", "time_estimate", "token_loss", "DBW_SOFTMAX", "DBW_MLP", "config_from"]
 
 
 def config_from(wl, S: int = 0) -> Config:

@@ -11,7 +11,7 @@ from __future__ import annotations
 import ctypes
 import functools
 import os
-from ctypes import POINTER, c_double, c_int32, c_int64, c_size_t, c_uint8, c_uint32, c_void_p
+from ctypes import POINTER, c_double, c_int32, c_int64, c_size_t, c_uint8, c_uint32, c_uint64, c_void_p
 
 import numpy as np
 
@@ -29,6 +29,7 @@ DBW_KT_GRADS, DBW_KT_AGGREGATE, DBW_KT_CHOOSE, DBW_KT_HOST_ESTIMATE, DBW_KT_HOST
 DBW_KT_HOST_WAIT, DBW_KT_HOST_QUEUE = 5, 6
 DBW_F32, DBW_BF16, DBW_F16 = 0, 1, 2
 DBW_GROUP_FORWARD, DBW_GROUP_INPUT_GRAD, DBW_GROUP_WEIGHT_GRAD = 0, 1, 2
+DBW_ACT_NONE, DBW_ACT_RELU, DBW_ACT_GELU, DBW_ACT_SILU = 0, 1, 2, 3
 ADAMW_BLOCK = 256   # values of one scale of the 8-bit states
 
 STATUS_NAMES = {0: "DBW_OK", -1: "DBW_EINVAL", -2: "DBW_ERANGE", -3: "DBW_EHIP",
@@ -45,6 +46,9 @@ EXPORTED = (
     "dbw_group_workspace", "dbw_group_product", "dbw_token_workspace", "dbw_token_loss",
     "dbw_adamw_create", "dbw_adamw_destroy", "dbw_adamw_step", "dbw_adamw_export", "dbw_adamw_import",
     "dbw_adamw_bits", "dbw_set_adamw",
+    "dbw_layer_norm", "dbw_layer_norm_workspace", "dbw_layer_norm_grad", "dbw_group_linear",
+    "dbw_linear_grad_workspace", "dbw_linear_grad", "dbw_attention", "dbw_attention_workspace",
+    "dbw_attention_grad", "dbw_dropout", "dbw_dropout_bits",
 )
 DBW_STATIC_SCRATCH_BYTES = 8 * 1024 * 1024
 
@@ -82,6 +86,20 @@ class GroupShape(ctypes.Structure):
     _fields_ = [("form", c_int32), ("dtype", c_int32), ("out_dtype", c_int32), ("n", c_int32), ("d", c_int32),
                 ("C", c_int32), ("T", c_int64), ("ld_d", c_int64), ("ld_C", c_int64), ("ld_W", c_int64),
                 ("st_W", c_int64)]
+
+
+class LinearEpilogue(ctypes.Structure):
+    _fields_ = [("activation", c_int32), ("bias", c_void_p), ("st_bias", c_int64), ("residual", c_void_p),
+                ("ld_residual", c_int64), ("pre", c_void_p), ("ld_pre", c_int64)]
+
+
+class Heads(ctypes.Structure):
+    _fields_ = [("data", c_void_p), ("token", c_int64), ("head", c_int64)]
+
+
+class AttentionShape(ctypes.Structure):
+    _fields_ = [("dtype", c_int32), ("n", c_int32), ("heads", c_int32), ("kv_heads", c_int32), ("D", c_int32),
+                ("T", c_int64), ("scale", c_double)]
 
 
 class AdamWTensor(ctypes.Structure):
@@ -198,6 +216,32 @@ def load_library(path: str = LIB_PATH):
     lib.dbw_set_adamw.restype = st
     lib.dbw_adamw_bits.argtypes = [c_uint32, c_int64, c_int32, c_int64]
     lib.dbw_adamw_bits.restype = c_uint32
+    lib.dbw_layer_norm.argtypes = [c_int32, c_int64, c_int32, c_int32, P, P, c_int64, P, P, c_double, P, c_int64, P]
+    lib.dbw_layer_norm.restype = st
+    lib.dbw_layer_norm_workspace.argtypes = [c_int32, c_int64, c_int32]
+    lib.dbw_layer_norm_workspace.restype = c_int64
+    lib.dbw_layer_norm_grad.argtypes = [c_int32, c_int64, c_int32, c_int32, P, P, c_int64, P, c_int64, P, c_double, P,
+                                        c_int64, P, c_int64, P, c_int64, P, c_int64, P]
+    lib.dbw_layer_norm_grad.restype = st
+    lib.dbw_group_linear.argtypes = [POINTER(GroupShape), POINTER(LinearEpilogue), P, P, P, P, P, c_int64, P]
+    lib.dbw_group_linear.restype = st
+    lib.dbw_linear_grad_workspace.argtypes = [c_int32, c_int64, c_int32]
+    lib.dbw_linear_grad_workspace.restype = c_int64
+    lib.dbw_linear_grad.argtypes = [c_int32, c_int64, c_int32, c_int32, c_int32, P, P, c_int64, P, c_int64, P, c_int64,
+                                    P, c_int64, P, c_int64, P]
+    lib.dbw_linear_grad.restype = st
+    H = POINTER(Heads)
+    lib.dbw_attention.argtypes = [POINTER(AttentionShape), P, H, H, H, H, P, P]
+    lib.dbw_attention.restype = st
+    lib.dbw_attention_workspace.argtypes = [POINTER(AttentionShape)]
+    lib.dbw_attention_workspace.restype = c_int64
+    lib.dbw_attention_grad.argtypes = [POINTER(AttentionShape), P, H, H, H, H, H, P, H, H, H, P, c_int64, P]
+    lib.dbw_attention_grad.restype = st
+    lib.dbw_dropout.argtypes = [c_int32, c_int64, c_int32, c_int32, P, P, c_int64, c_double, c_uint64, P, P, c_int64, P,
+                                c_int64, P]
+    lib.dbw_dropout.restype = st
+    lib.dbw_dropout_bits.argtypes = [c_uint64, c_int64, c_int64, c_int32]
+    lib.dbw_dropout_bits.restype = c_uint32
     _lib = lib
     return lib
 
@@ -417,9 +461,9 @@ def _group_shape(*sizes):
     return ref, need.value
 
 
-def _group(form, a, b, offsets, out, out_dtype, d, C, workspace, stream=None):
+def _group(form, a, b, offsets, out, out_dtype, d, C, workspace, stream=None, epilogue=None):
     if stream is not None:
-        return _on(stream, a.device, _group, form, a, b, offsets, out, out_dtype, d, C, workspace)
+        return _on(stream, a.device, _group, form, a, b, offsets, out, out_dtype, d, C, workspace, epilogue=epilogue)
     torch = _torch()
     lib = load_library()
     dev, dtype = a.device, a.dtype
@@ -453,8 +497,12 @@ def _group(form, a, b, offsets, out, out_dtype, d, C, workspace, stream=None):
         st_W = b.stride(0) if b.dim() == 3 and n > 1 else 0
     ref, need = _group_shape(form, codes[0], codes[1], n, d, C, T, ld_d, ld_C, ld_W, st_W)
     pw, nbytes, keep = _workspace(torch, need, dev, workspace)
-    _call(torch, lib, dev, lib.dbw_group_product, ref, po, pa, pb, pc, pw, nbytes, raw)
-    return out
+    if epilogue is None:
+        _call(torch, lib, dev, lib.dbw_group_product, ref, po, pa, pb, pc, pw, nbytes, raw)
+        return out
+    e, pre = epilogue(torch, dev, n, T, C, dtype, out_dtype)
+    _call(torch, lib, dev, lib.dbw_group_linear, ref, ctypes.byref(e), po, pa, pb, pc, pw, nbytes, raw)
+    return out, pre
 
 
 def group_matmul(X, W, offsets, out=None, out_dtype=None, workspace=None, stream=None):
@@ -522,6 +570,249 @@ def token_loss(Z, y, offsets, scale=1.0, dZ=None, loss=None, grad=True, workspac
     pw, nbytes, keep = _workspace(torch, lib.dbw_token_workspace(n, T), dev, workspace)
     _call(torch, lib, dev, lib.dbw_token_loss, n, T, C, code, po, pz, ld_Z, py, scale, pd, ld_dZ, pl, pw, nbytes, raw)
     return loss, dZ
+
+
+# -- a transformer block -----------------------------------------------------------
+_ACTIVATIONS = {"none": DBW_ACT_NONE, "relu": DBW_ACT_RELU, "gelu": DBW_ACT_GELU, "silu": DBW_ACT_SILU}
+
+
+def _activation(name):
+    code = _ACTIVATIONS.get(name)
+    if code is None:
+        raise ValueError(f"activation must be one of {', '.join(_ACTIVATIONS)}, not {name!r}")
+    return code
+
+
+def _token_rows(torch, X, offsets, name, allowed=_FLOATS):
+    """Rows, columns, groups, type and device of X [T][columns] in groups."""
+    if X.dim() != 2 or offsets.dim() != 1 or offsets.numel() < 2:
+        raise ValueError(f"{name} must be [T][columns] and offsets [n + 1]")
+    n = offsets.numel() - 1
+    code = _dtype_code(torch, X.dtype, name, allowed)
+    raw = _stream_of(torch, X.device)
+    po = _flat(offsets, (n + 1,), torch.int32, X.device, "offsets")
+    return X.shape[0], X.shape[1], n, code, raw, po
+
+
+def layer_norm(X, gamma, beta, offsets, eps=1e-5, out=None, stream=None):
+    """Layer norm of each row (dbw_layer_norm): (X - mean) / sqrt(var + eps)
+    gamma + beta.  X [T][d] float32, bfloat16 or float16, gamma and beta [d]
+    float32 (beta may be None), offsets [n+1] int32.  Returns Y [T][d] of the
+    type of X; rows of no group keep what ``out`` held."""
+    if stream is not None:
+        return _on(stream, X.device, layer_norm, X, gamma, beta, offsets, eps, out)
+    torch = _torch()
+    lib = load_library()
+    T, d, n, code, raw, po = _token_rows(torch, X, offsets, "X")
+    dev, dtype = X.device, X.dtype
+    px, ld_X = _rows_of(X, (T, d), dtype, dev, "X")
+    pg = _flat(gamma, (d,), torch.float32, dev, "gamma")
+    pb = _flat(beta, (d,), torch.float32, dev, "beta") if beta is not None else None
+    if out is None:
+        out = torch.empty((T, d), dtype=dtype, device=dev)
+    py, ld_Y = _rows_of(out, (T, d), dtype, dev, "out")
+    _call(torch, lib, dev, lib.dbw_layer_norm, n, T, d, code, po, px, ld_X, pg, pb, eps, py, ld_Y, raw)
+    return out
+
+
+def layer_norm_grad(dY, X, gamma, offsets, eps=1e-5, dX=None, dgamma=None, dbeta=None, workspace=None, stream=None):
+    """Gradients of layer_norm, from its input X (dbw_layer_norm_grad).  Returns
+    (dX [T][d] of the type of X, dgamma [n][d] and dbeta [n][d] float32: those
+    of each group); given ones may have strided rows, as the columns of the
+    worker gradients G [n][P] do.  ``dbeta`` False: not formed (None)."""
+    if stream is not None:
+        return _on(stream, X.device, layer_norm_grad, dY, X, gamma, offsets, eps, dX, dgamma, dbeta, workspace)
+    torch = _torch()
+    lib = load_library()
+    T, d, n, code, raw, po = _token_rows(torch, X, offsets, "X")
+    dev, dtype = X.device, X.dtype
+    pd, ld_dY = _rows_of(dY, (T, d), dtype, dev, "dY")
+    px, ld_X = _rows_of(X, (T, d), dtype, dev, "X")
+    pg = _flat(gamma, (d,), torch.float32, dev, "gamma")
+    if dX is None:
+        dX = torch.empty((T, d), dtype=dtype, device=dev)
+    if dgamma is None:
+        dgamma = torch.empty((n, d), dtype=torch.float32, device=dev)
+    if dbeta is None:
+        dbeta = torch.empty((n, d), dtype=torch.float32, device=dev)
+    elif dbeta is False:
+        dbeta = None
+    po_x, ld_dX = _rows_of(dX, (T, d), dtype, dev, "dX")
+    pgg, ld_g = _rows_of(dgamma, (n, d), torch.float32, dev, "dgamma")
+    pgb, ld_b = _rows_of(dbeta, (n, d), torch.float32, dev, "dbeta") if dbeta is not None else (None, 0)
+    pw, nbytes, keep = _workspace(torch, lib.dbw_layer_norm_workspace(n, T, d), dev, workspace)
+    _call(torch, lib, dev, lib.dbw_layer_norm_grad, n, T, d, code, po, pd, ld_dY, px, ld_X, pg, eps, po_x, ld_dX, pgg,
+          ld_g, pgb, ld_b, pw, nbytes, raw)
+    return dX, dgamma, dbeta
+
+
+def group_linear(X, W, offsets, bias=None, activation="none", residual=None, pre=False, out=None, out_dtype=None,
+                 workspace=None, stream=None):
+    """Y[t] = act(X[t] W_i + b_i) + R[t] for the rows t of each group i
+    (dbw_group_linear): group_matmul with what surrounds it.  bias [n][C] float32,
+    or [C] for all groups (as it has to be where W is [d][C]); ``activation``
+    "none", "relu", "gelu" (its tanh form) or "silu"; residual [T][C] of the type
+    of Y, which may be ``out``.  Returns (Y, Z): with ``pre`` True or a tensor
+    [T][C] of the type of X, Z = X W_i + b_i, which group_linear_grad takes;
+    else None."""
+    if W.dim() not in (2, 3):
+        raise ValueError("W must be [n][d][C] or [d][C]")
+    if bias is not None and bias.dim() not in (1, 2):
+        raise ValueError("bias must be [n][C] or [C]")
+    act = _activation(activation)
+    d, C = W.shape[-2:]
+
+    def epilogue(torch, dev, n, T, C, dtype, out_dtype):
+        e, Z = LinearEpilogue(activation=act), None
+        if bias is not None:
+            if bias.dim() == 2:
+                e.bias, e.st_bias = _rows_of(bias, (n, C), torch.float32, dev, "bias")
+            else:
+                e.bias, e.st_bias = _flat(bias, (C,), torch.float32, dev, "bias"), 0
+        if residual is not None:
+            e.residual, e.ld_residual = _rows_of(residual, (T, C), out_dtype, dev, "residual")
+        if pre is not False and pre is not None:
+            Z = torch.empty((T, C), dtype=dtype, device=dev) if pre is True else pre
+            e.pre, e.ld_pre = _rows_of(Z, (T, C), dtype, dev, "pre")
+        return e, Z
+    return _group(DBW_GROUP_FORWARD, X, W, offsets, out, out_dtype, d, C, workspace, stream, epilogue)
+
+
+def group_linear_grad(dY, offsets, pre=None, activation="none", dZ=None, dbias=None, workspace=None, stream=None):
+    """The way back through group_linear's activation (dbw_linear_grad): dZ =
+    dY act'(Z) of the type of dY, with Z = ``pre``, and dbias [n][C] float32, the
+    sums of each group's dZ (a given one may have strided rows).  group_input_grad
+    and group_weight_grad of dZ follow; the residual's gradient is dY.  Returns
+    (dZ, dbias); with the activation "none" dZ is dY itself unless a ``dZ`` is
+    given.  ``dbias`` False: not formed (None)."""
+    if stream is not None:
+        return _on(stream, dY.device, group_linear_grad, dY, offsets, pre, activation, dZ, dbias, workspace)
+    torch = _torch()
+    lib = load_library()
+    act = _activation(activation)
+    T, C, n, code, raw, po = _token_rows(torch, dY, offsets, "dY")
+    dev, dtype = dY.device, dY.dtype
+    pd, ld_dY = _rows_of(dY, (T, C), dtype, dev, "dY")
+    if act != DBW_ACT_NONE and pre is None:
+        raise ValueError("the activation's gradient needs its argument, pre")
+    pz, ld_Z = _rows_of(pre, (T, C), dtype, dev, "pre") if act != DBW_ACT_NONE else (None, 0)
+    own = dZ is None and act == DBW_ACT_NONE
+    if dZ is None and not own:
+        dZ = torch.empty((T, C), dtype=dtype, device=dev)
+    pg, ld_dZ = _rows_of(dZ, (T, C), dtype, dev, "dZ") if dZ is not None else (None, 0)
+    if dbias is None:
+        dbias = torch.empty((n, C), dtype=torch.float32, device=dev)
+    elif dbias is False:
+        dbias = None
+    pb, ld_b = _rows_of(dbias, (n, C), torch.float32, dev, "dbias") if dbias is not None else (None, 0)
+    need = lib.dbw_linear_grad_workspace(n, T, C) if dbias is not None else 0
+    pw, nbytes, keep = _workspace(torch, need, dev, workspace)
+    if not own or dbias is not None:
+        _call(torch, lib, dev, lib.dbw_linear_grad, n, T, C, code, act, po, pd, ld_dY, pz, ld_Z, pg, ld_dZ, pb, ld_b, pw,
+              nbytes, raw)
+    return dY if own else dZ, dbias
+
+
+def _heads_of(t, shape, dtype, dev, name):
+    """dbw_heads of a tensor [T][heads][D] with contiguous D."""
+    if t.device != dev or t.dtype != dtype or t.shape != shape:
+        raise ValueError(f"{name} must be {dtype} {tuple(shape)} on {dev}, not {t.dtype} {tuple(t.shape)} on {t.device}")
+    token, head, one = t.stride()
+    if one != 1 and shape[2] > 1:
+        raise ValueError(f"the last dimension of {name} must be contiguous")
+    # a single head, or a single token, has no stride of its own
+    if shape[1] == 1:
+        head = shape[2]
+    if shape[0] == 1:
+        token = (shape[1] - 1) * head + shape[2] if shape[1] * head < 1 << 21 else shape[2]
+    return Heads(t.data_ptr(), token, head)
+
+
+def _attention_shape(torch, Q, K, offsets, scale):
+    if Q.dim() != 3 or K.dim() != 3 or offsets.dim() != 1 or offsets.numel() < 2:
+        raise ValueError("Q must be [T][heads][D], K and V [T][kv_heads][D] and offsets [n + 1]")
+    T, heads, D = Q.shape
+    n, dev = offsets.numel() - 1, Q.device
+    code = _dtype_code(torch, Q.dtype, "Q", _HALVES)
+    raw = _stream_of(torch, dev)
+    po = _flat(offsets, (n + 1,), torch.int32, dev, "offsets")
+    if scale is None:
+        scale = D ** -0.5 if D else 1.0
+    return AttentionShape(code, n, heads, K.shape[1], D, T, scale), raw, po
+
+
+def attention(Q, K, V, offsets, scale=None, out=None, lse=None, stream=None):
+    """Causal attention over packed sequences (dbw_attention).  Q [T][heads][D],
+    K and V [T][kv_heads][D] bfloat16 or float16, D a multiple of 8 up to 128,
+    offsets [n+1] int32: the sequences; tokens and heads may be strided, by
+    multiples of 8 values (slices of one array of queries, keys and values).
+    ``scale`` 1/sqrt(D) unless given.  Returns (O [T][heads][D], lse [heads][T]
+    float32, which attention_grad takes); ``lse`` False: not formed (None)."""
+    if stream is not None:
+        return _on(stream, Q.device, attention, Q, K, V, offsets, scale, out, lse)
+    torch = _torch()
+    lib = load_library()
+    shape, raw, po = _attention_shape(torch, Q, K, offsets, scale)
+    dev, dtype, kv = Q.device, Q.dtype, (shape.T, shape.kv_heads, shape.D)
+    if out is None:
+        out = torch.empty(Q.shape, dtype=dtype, device=dev)
+    if lse is None or lse is True:
+        lse = torch.empty((shape.heads, shape.T), dtype=torch.float32, device=dev)
+    elif lse is False:
+        lse = None
+    pl = _flat(lse, (shape.heads, shape.T), torch.float32, dev, "lse") if lse is not None else None
+    arrays = [ctypes.byref(_heads_of(t, s, dtype, dev, name)) for t, s, name in
+              ((Q, Q.shape, "Q"), (K, kv, "K"), (V, kv, "V"), (out, Q.shape, "out"))]
+    _call(torch, lib, dev, lib.dbw_attention, ctypes.byref(shape), po, *arrays, pl, raw)
+    return out, lse
+
+
+def attention_grad(dO, Q, K, V, O, lse, offsets, scale=None, dQ=None, dK=None, dV=None, workspace=None,  # noqa: E741
+                   stream=None):
+    """Gradients of attention (dbw_attention_grad), from its O and lse.  Returns
+    (dQ, dK, dV) of the shapes of Q, K and V; given ones may be strided as those
+    are."""
+    if stream is not None:
+        return _on(stream, Q.device, attention_grad, dO, Q, K, V, O, lse, offsets, scale, dQ, dK, dV, workspace)
+    torch = _torch()
+    lib = load_library()
+    shape, raw, po = _attention_shape(torch, Q, K, offsets, scale)
+    dev, dtype, kv = Q.device, Q.dtype, (shape.T, shape.kv_heads, shape.D)
+    dQ, dK, dV = (torch.empty(s, dtype=dtype, device=dev) if t is None else t
+                  for t, s in ((dQ, Q.shape), (dK, kv), (dV, kv)))
+    pl = _flat(lse, (shape.heads, shape.T), torch.float32, dev, "lse")
+    dO, Q_, K_, V_, O, *grads = (                                                                        # noqa: E741
+        ctypes.byref(_heads_of(t, s, dtype, dev, name)) for t, s, name in
+        ((dO, Q.shape, "dO"), (Q, Q.shape, "Q"), (K, kv, "K"), (V, kv, "V"), (O, Q.shape, "O"), (dQ, Q.shape, "dQ"),
+         (dK, kv, "dK"), (dV, kv, "dV")))
+    pw, nbytes, keep = _workspace(torch, lib.dbw_attention_workspace(ctypes.byref(shape)), dev, workspace)
+    _call(torch, lib, dev, lib.dbw_attention_grad, ctypes.byref(shape), po, dO, Q_, K_, V_, O, pl, *grads, pw, nbytes, raw)
+    return dQ, dK, dV
+
+
+def dropout(X, p, seed, offsets, residual=None, step=None, out=None, stream=None):
+    """Y = R + X kept / (1 - p), with a mask drawn from a counter and never stored
+    (dbw_dropout): each value is kept or dropped by 16 random bits of (seed, step,
+    row, column), so the gradient is the same call on dY with no residual.  X
+    [T][d] float32, bfloat16 or float16, residual [T][d] of its type or None,
+    ``seed`` an integer, ``step`` an int64 tensor [1] on the device (a captured
+    call then draws anew at each replay) or None.  Returns Y; ``out`` may be X or
+    the residual."""
+    if stream is not None:
+        return _on(stream, X.device, dropout, X, p, seed, offsets, residual, step, out)
+    torch = _torch()
+    lib = load_library()
+    T, d, n, code, raw, po = _token_rows(torch, X, offsets, "X")
+    dev, dtype = X.device, X.dtype
+    px, ld_X = _rows_of(X, (T, d), dtype, dev, "X")
+    pr, ld_R = _rows_of(residual, (T, d), dtype, dev, "residual") if residual is not None else (None, 0)
+    ps = _flat(step, (1,), torch.int64, dev, "step") if step is not None else None
+    if out is None:
+        out = torch.empty((T, d), dtype=dtype, device=dev)
+    py, ld_Y = _rows_of(out, (T, d), dtype, dev, "out")
+    _call(torch, lib, dev, lib.dbw_dropout, n, T, d, code, po, px, ld_X, p, seed & 0xFFFFFFFFFFFFFFFF, ps, pr, ld_R, py,
+          ld_Y, raw)
+    return out
 
 
 def adamw_states(w, bits=32):

@@ -1,0 +1,556 @@
+// Causal attention over packed sequences, and its gradients.
+//   k_attention       O and lse: a workgroup takes 128 queries of a head
+//   k_attention_dq    dQ, and delta = dO . O of each query: the same
+//   k_attention_dkv   dK and dV: a workgroup takes 128 keys of a head of keys
+//
+// v_mfma_f32_32x32x16 takes, in lane l = 32 h + c, row c and terms 8 h .. 8 h +
+// 7 of each operand; its result r of a lane is row 8 (r / 4) + 4 h + r % 4 of
+// the first operand, row c of the second.  A wave takes 32 queries as the
+// second operand of S^T = K Q^T, so that a lane has 16 keys of one query: the
+// softmax needs one exchange between the halves of a wave.  Its exponentials,
+// packed as they are, are terms 4 h .. 4 h + 3 and 8 + 4 h .. of sixteen keys;
+// the order of terms does not matter, so they are the second operand of O^T =
+// V^T P^T without any exchange, when V's transposing loads take the same keys.
+// The gradients do the same with K^T, and, with keys for queries, with Q^T and
+// dO^T.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "dbw_buffer.h"
+#include "lm_ops.h"
+#include "lm_tiles.h"
+
+namespace dbw {
+namespace {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+__device__ __forceinline__ f32x16 mma(const lm_u32x4& a, const lm_u32x4& b, const f32x16& c, __bf16) {
+  typedef __bf16 V __attribute__((ext_vector_type(8)));
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(V, a), __builtin_bit_cast(V, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16 mma(const lm_u32x4& a, const lm_u32x4& b, const f32x16& c, _Float16) {
+  typedef _Float16 V __attribute__((ext_vector_type(8)));
+  return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(V, a), __builtin_bit_cast(V, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16 zero16() {
+  return f32x16{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+}
+
+// The halves of a wave exchange: a's upper and b's lower one.  (The waits are
+// those between a vector result and this instruction.)
+__device__ __forceinline__ void swap_halves(uint32_t& a, uint32_t& b) {
+  asm volatile("s_nop 3\n\tv_permlane32_swap_b32 %0, %1\n\ts_nop 1" : "+v"(a), "+v"(b));
+}
+__device__ __forceinline__ float max_halves(float x) {
+  uint32_t a = __builtin_bit_cast(uint32_t, x), b = a;
+  swap_halves(a, b);
+  return fmaxf(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b));
+}
+__device__ __forceinline__ float sum_halves(float x) {
+  uint32_t a = __builtin_bit_cast(uint32_t, x), b = a;
+  swap_halves(a, b);
+  return __builtin_bit_cast(float, a) + __builtin_bit_cast(float, b);
+}
+
+// Rows of DP values in LDS, as a stage of ROWS of them.  A line's chunks of 16
+// bytes are turned by its number, so that eight lanes that read a chunk of
+// eight lines, and sixteen that read 32 bytes of four lines by the transposing
+// load, meet in no bank.
+template <int DP, int ROWS, int THREADS>
+struct Rows {
+  static constexpr int LINE = DP / 8;                     // chunks of a line
+  static constexpr int CHUNKS = ROWS * LINE / THREADS;    // a thread
+  static constexpr int BYTES = ROWS * DP * 2;
+  static_assert(DP == 64 || DP == 96 || DP == 128, "turn() is for these");
+  static_assert(ROWS * LINE % THREADS == 0, "whole chunks a thread");
+  static __device__ __forceinline__ int turn(int line) {
+    if (DP == 96) return (line >> 1 & 1) << 1 | (line >> 2 & 1);   // (lines start at two places among the banks)
+    return (line & 3) << 1 | (line >> 2 & 1);
+  }
+  // Byte offset of thread tid's chunk i from the stage's first row, or one
+  // behind every buffer (such loads give 0): of `left` rows, of D values each.
+  static __device__ __forceinline__ uint32_t offset(int64_t token, int left, int D, int tid, int i) {
+    const int id = i * THREADS + tid, line = id / LINE, chunk = id % LINE ^ turn(line);
+    return line < left && chunk * 8 < D ? static_cast<uint32_t>(line * token * 2 + chunk * 16) : kOutOfRange;
+  }
+  static __device__ __forceinline__ void load(const char* p, int64_t token, int left, int D, char* lds, int wave,
+                                              int lane, const uint32_t (&off)[CHUNKS]) {
+    const __amdgpu_buffer_rsrc_t r = make_rsrc(p, static_cast<uint32_t>(kMaxBufferBytes));
+    if (left >= ROWS) {
+#pragma unroll
+      for (int i = 0; i < CHUNKS; ++i) load_lds(r, lds + (i * (THREADS / 64) + wave) * 1024, off[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < CHUNKS; ++i)
+        load_lds(r, lds + (i * (THREADS / 64) + wave) * 1024, offset(token, left, D, wave * 64 + lane, i));
+    }
+  }
+  // Terms 16 kk + 8 h .. + 7 of line first + c (first: a multiple of 32).
+  static __device__ __forceinline__ lm_u32x4 row(const char* lds, int first, int kk, int lane) {
+    const int c = lane % 32, h = lane / 32;
+    return *reinterpret_cast<const lm_u32x4*>(lds + (first + c) * (DP * 2) + ((2 * kk + h) ^ turn(c)) * 16);
+  }
+  // Addresses of a lane for column(): of the columns 32 i + 16 (lane / 16 % 2)
+  // + 4 q .. + 3 of line 4 h + r, with r and q from lane % 16 = 4 r + q.
+  static __device__ __forceinline__ void columns(const char* lds, int lane, uint32_t (&p)[DP / 32]) {
+    const int q = lane % 4, line = lane / 32 * 4 + lane % 16 / 4;
+    typedef __attribute__((address_space(3))) const char* P;
+#pragma unroll
+    for (int i = 0; i < DP / 32; ++i)
+      p[i] = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(
+          (P)(lds + line * (DP * 2) + ((4 * i + lane / 16 % 2 * 2 + q / 2) ^ turn(line)) * 16 + q % 2 * 8)));
+  }
+  // Sixteen lines from AT bytes behind them on, transposed: in lane 32 h + c,
+  // column 32 i + c of lines 4 h .. + 3 and 8 + 4 h .. + 3.  The wait is in the
+  // statement: as builtins, the compiler would first wait for every load on
+  // its way to LDS.
+  template <int AT>
+  static __device__ __forceinline__ void column(const uint32_t (&p)[2], lm_u32x4 (&f)[2]) {
+    lm_u32x2 x[2][2];
+    asm volatile(
+        "ds_read_b64_tr_b16 %0, %4 offset:%6\n\tds_read_b64_tr_b16 %1, %4 offset:%7\n\t"
+        "ds_read_b64_tr_b16 %2, %5 offset:%6\n\tds_read_b64_tr_b16 %3, %5 offset:%7\n\t"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(x[0][0]), "=&v"(x[0][1]), "=&v"(x[1][0]), "=&v"(x[1][1])
+        : "v"(p[0]), "v"(p[1]), "n"(AT), "n"(AT + 8 * DP * 2)
+        : "memory");
+    join(x, f);
+  }
+  template <int AT>
+  static __device__ __forceinline__ void column(const uint32_t (&p)[3], lm_u32x4 (&f)[3]) {
+    lm_u32x2 x[3][2];
+    asm volatile(
+        "ds_read_b64_tr_b16 %0, %6 offset:%9\n\tds_read_b64_tr_b16 %1, %6 offset:%10\n\t"
+        "ds_read_b64_tr_b16 %2, %7 offset:%9\n\tds_read_b64_tr_b16 %3, %7 offset:%10\n\t"
+        "ds_read_b64_tr_b16 %4, %8 offset:%9\n\tds_read_b64_tr_b16 %5, %8 offset:%10\n\t"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(x[0][0]), "=&v"(x[0][1]), "=&v"(x[1][0]), "=&v"(x[1][1]), "=&v"(x[2][0]), "=&v"(x[2][1])
+        : "v"(p[0]), "v"(p[1]), "v"(p[2]), "n"(AT), "n"(AT + 8 * DP * 2)
+        : "memory");
+    join(x, f);
+  }
+  template <int AT>
+  static __device__ __forceinline__ void column(const uint32_t (&p)[4], lm_u32x4 (&f)[4]) {
+    lm_u32x2 x[4][2];
+    asm volatile(
+        "ds_read_b64_tr_b16 %0, %8 offset:%12\n\tds_read_b64_tr_b16 %1, %8 offset:%13\n\t"
+        "ds_read_b64_tr_b16 %2, %9 offset:%12\n\tds_read_b64_tr_b16 %3, %9 offset:%13\n\t"
+        "ds_read_b64_tr_b16 %4, %10 offset:%12\n\tds_read_b64_tr_b16 %5, %10 offset:%13\n\t"
+        "ds_read_b64_tr_b16 %6, %11 offset:%12\n\tds_read_b64_tr_b16 %7, %11 offset:%13\n\t"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(x[0][0]), "=&v"(x[0][1]), "=&v"(x[1][0]), "=&v"(x[1][1]), "=&v"(x[2][0]), "=&v"(x[2][1]),
+          "=&v"(x[3][0]), "=&v"(x[3][1])
+        : "v"(p[0]), "v"(p[1]), "v"(p[2]), "v"(p[3]), "n"(AT), "n"(AT + 8 * DP * 2)
+        : "memory");
+    join(x, f);
+  }
+  template <int N>
+  static __device__ __forceinline__ void join(const lm_u32x2 (&x)[N][2], lm_u32x4 (&f)[N]) {
+    static_assert(ROWS * DP * 2 <= 65536, "offsets have sixteen bits");
+#pragma unroll
+    for (int i = 0; i < N; ++i) f[i] = lm_u32x4{x[i][0][0], x[i][0][1], x[i][1][0], x[i][1][1]};
+  }
+};
+
+// Address of row `row` of a head's rows.
+__device__ __forceinline__ char* at(const HeadRows& r, int64_t row, int head) {
+  return r.p + (row * r.token + head * r.head) * 2;
+}
+
+// Rows first + c of a head as a wave's operand in registers; rows from `left`
+// on are 0.
+template <int DP>
+__device__ __forceinline__ void operand(const char* first, int64_t token, int left, int D, int lane,
+                                        lm_u32x4 (&f)[DP / 16]) {
+  const __amdgpu_buffer_rsrc_t r = make_rsrc(first, static_cast<uint32_t>(kMaxBufferBytes));
+  const int c = lane % 32, h = lane / 32;
+#pragma unroll
+  for (int kk = 0; kk < DP / 16; ++kk) {
+    const uint32_t off =
+        c < left && 16 * kk + 8 * h < D ? static_cast<uint32_t>((c * token + 16 * kk + 8 * h) * 2) : kOutOfRange;
+    f[kk] = __builtin_bit_cast(lm_u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, 0));
+  }
+}
+
+// A wave's results, transposed: column c of tile i is row first + c, of which
+// a lane has values 32 i + 8 (r / 4) + 4 h + r % 4; times `by`.
+template <typename E, int DP>
+__device__ __forceinline__ void write_rows(char* first, int64_t token, int left, int D, int lane,
+                                           const f32x16 (&x)[DP / 32], float by) {
+  const int c = lane % 32, h = lane / 32;
+#pragma unroll
+  for (int i = 0; i < DP / 32; ++i)
+#pragma unroll
+    for (int k = 0; k < 16; k += 8) {
+      // the halves exchange, so that each has eight values in a row
+      uint32_t a0 = pack2<E>(x[i][k] * by, x[i][k + 1] * by), a1 = pack2<E>(x[i][k + 2] * by, x[i][k + 3] * by);
+      uint32_t b0 = pack2<E>(x[i][k + 4] * by, x[i][k + 5] * by), b1 = pack2<E>(x[i][k + 6] * by, x[i][k + 7] * by);
+      swap_halves(a0, b0);
+      swap_halves(a1, b1);
+      const int d = 32 * i + 2 * k + 8 * h;
+      if (c < left && d < D) *reinterpret_cast<lm_u32x4*>(first + (c * token + d) * 2) = lm_u32x4{a0, a1, b0, b1};
+    }
+}
+
+// Results r = 8 u .. 8 u + 7 of a lane, as eight terms of an operand.
+template <typename E>
+__device__ __forceinline__ lm_u32x4 terms(const f32x16& x, int u) {
+  return lm_u32x4{pack2<E>(x[8 * u], x[8 * u + 1]), pack2<E>(x[8 * u + 2], x[8 * u + 3]),
+                  pack2<E>(x[8 * u + 4], x[8 * u + 5]), pack2<E>(x[8 * u + 6], x[8 * u + 7])};
+}
+
+__device__ __forceinline__ int place(int r, int h) { return 8 * (r / 4) + 4 * h + r % 4; }
+
+constexpr int BM = kAttentionRows, BN = 64;
+
+// What a workgroup works on: rows first .. of a sequence [start, end) and a head.
+struct Work {
+  LmChunk rows;
+  int head;
+};
+// Workgroups start in the order of their numbers: the last tiles of a sequence
+// have the most keys before them, and go first.
+__device__ __forceinline__ Work work(const AttentionArgs& a, int heads, bool reverse, int lane) {
+  const uint32_t slot = blockIdx.x / heads;
+  Work w;
+  w.head = static_cast<int>(blockIdx.x % heads);
+  w.rows = lm_chunk(a.offsets, a.n, a.T, BM, reverse ? a.slots - 1 - slot : slot, lane);
+  return w;
+}
+
+template <typename E, int DP>
+__global__ __launch_bounds__(256, 2) void k_attention(AttentionArgs a) {
+  typedef Rows<DP, BN, 256> R;
+  __shared__ __align__(16) char lds[4 * R::BYTES];   // two stages of K and V
+  const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
+  const int c = lane % 32, h = lane / 32;
+  const Work w = work(a, a.heads, true, lane);
+  if (w.rows.empty()) return;
+  const int len = w.rows.end - w.rows.start, q0 = w.rows.first - w.rows.start, qw = q0 + 32 * wave, qi = qw + c;
+  const int kv_head = w.head / (a.heads / a.kv_heads);
+  const float scale2 = a.scale * kLog2E;
+  const float lim = 8.f / scale2;    // a maximum may grow by 2^8 before sums are scaled
+
+  lm_u32x4 q[DP / 16];
+  operand<DP>(at(a.Q, w.rows.first + 32 * wave, w.head), a.Q.token, len - qw, a.D, lane, q);
+  f32x16 o[DP / 32];
+#pragma unroll
+  for (int i = 0; i < DP / 32; ++i) o[i] = zero16();
+  float m = -INFINITY, sum = 0.f;
+
+  uint32_t off_k[R::CHUNKS], off_v[R::CHUNKS], pv[DP / 32];
+#pragma unroll
+  for (int i = 0; i < R::CHUNKS; ++i) {
+    off_k[i] = R::offset(a.K.token, BN, a.D, tid, i);
+    off_v[i] = R::offset(a.V.token, BN, a.D, tid, i);
+  }
+  R::columns(lds + R::BYTES, lane, pv);
+  const int keys = std::min(len, q0 + BM);   // the workgroup's
+  const auto issue = [&](int k0, int slot) {
+    char* to = lds + slot * (2 * R::BYTES);
+    R::load(at(a.K, w.rows.start + static_cast<int64_t>(k0), kv_head), a.K.token, len - k0, a.D, to, wave, lane, off_k);
+    R::load(at(a.V, w.rows.start + static_cast<int64_t>(k0), kv_head), a.V.token, len - k0, a.D, to + R::BYTES, wave, lane, off_v);
+  };
+  issue(0, 0);
+  for (int k0 = 0, slot = 0; k0 < keys; k0 += BN, slot ^= 1) {
+    wait_step<0>();
+    if (k0 + BN < keys) issue(k0 + BN, slot ^ 1);
+    if (k0 > qw + 31 || qw >= len) continue;
+    const char* stage = lds + slot * (2 * R::BYTES);
+    f32x16 s[2] = {zero16(), zero16()};
+#pragma unroll
+    for (int kk = 0; kk < DP / 16; ++kk)
+#pragma unroll
+      for (int t = 0; t < 2; ++t) s[t] = mma(R::row(stage, 32 * t, kk, lane), q[kk], s[t], E{});
+    if (k0 + BN - 1 > qw) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (k0 + 32 * t + place(r, h) > qi) s[t][r] = -INFINITY;
+    }
+    float mx = s[0][0];
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[t][r]);
+    mx = max_halves(mx);
+    if (__any(mx > m + lim)) {
+      const float top = fmaxf(m, mx), by = __builtin_amdgcn_exp2f((m - top) * scale2);
+      m = top;
+      sum *= by;
+#pragma unroll
+      for (int i = 0; i < DP / 32; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[i][r] *= by;
+    }
+    const float m2 = m * scale2;
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        s[t][r] = __builtin_amdgcn_exp2f(fmaf(s[t][r], scale2, -m2));
+        sum += s[t][r];
+      }
+    uint32_t p[DP / 32];
+#pragma unroll
+    for (int i = 0; i < DP / 32; ++i) p[i] = pv[i] + slot * (2 * R::BYTES);
+    lm_u32x4 v[DP / 32];
+    const auto product = [&](auto tu) {
+      constexpr int t = decltype(tu)::value / 2, u = decltype(tu)::value % 2;
+      R::template column<(32 * t + 16 * u) * DP * 2>(p, v);
+      const lm_u32x4 x = terms<E>(s[t], u);
+#pragma unroll
+      for (int i = 0; i < DP / 32; ++i) o[i] = mma(v[i], x, o[i], E{});
+    };
+    product(std::integral_constant<int, 0>{});
+    product(std::integral_constant<int, 1>{});
+    product(std::integral_constant<int, 2>{});
+    product(std::integral_constant<int, 3>{});
+  }
+  if (qw >= len) return;
+  sum = sum_halves(sum);
+  write_rows<E, DP>(at(a.O, w.rows.first + 32 * wave, w.head), a.O.token, len - qw, a.D, lane, o, 1.f / sum);
+  if (a.lse && h == 0 && qi < len)
+    a.lse[w.head * a.T + w.rows.start + qi] = (m * scale2 + __builtin_amdgcn_logf(sum)) * (1.f / kLog2E);
+}
+
+template <typename E, int DP>
+__global__ __launch_bounds__(256, 2) void k_attention_dq(AttentionArgs a) {
+  typedef Rows<DP, BN, 256> R;
+  __shared__ __align__(16) char lds[4 * R::BYTES];   // two stages of K and V
+  const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
+  const int c = lane % 32, h = lane / 32;
+  const Work w = work(a, a.heads, true, lane);
+  if (w.rows.empty()) return;
+  const int len = w.rows.end - w.rows.start, q0 = w.rows.first - w.rows.start, qw = q0 + 32 * wave, qi = qw + c;
+  const int kv_head = w.head / (a.heads / a.kv_heads);
+  const float scale2 = a.scale * kLog2E;
+  const int64_t row = w.rows.first + 32 * wave;
+
+  lm_u32x4 q[DP / 16], dy[DP / 16];
+  operand<DP>(at(a.Q, row, w.head), a.Q.token, len - qw, a.D, lane, q);
+  operand<DP>(at(a.dO, row, w.head), a.dO.token, len - qw, a.D, lane, dy);
+  float delta = 0.f, lse2 = 0.f;
+  {
+    lm_u32x4 y[DP / 16];
+    operand<DP>(at(a.O, row, w.head), a.O.token, len - qw, a.D, lane, y);
+    typedef E V __attribute__((ext_vector_type(8)));
+#pragma unroll
+    for (int kk = 0; kk < DP / 16; ++kk) {
+      const V x = __builtin_bit_cast(V, y[kk]), g = __builtin_bit_cast(V, dy[kk]);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) delta = fmaf(lm_to_f32(x[j]), lm_to_f32(g[j]), delta);
+    }
+    delta = sum_halves(delta);
+    if (qi < len) {
+      const int64_t to = w.head * a.T + w.rows.start + qi;
+      lse2 = a.lse[to] * kLog2E;
+      if (h == 0) {
+        a.delta[to] = delta;
+        a.delta[a.heads * a.T + to] = lse2;
+      }
+    }
+  }
+  f32x16 dq[DP / 32];
+#pragma unroll
+  for (int i = 0; i < DP / 32; ++i) dq[i] = zero16();
+
+  uint32_t off_k[R::CHUNKS], off_v[R::CHUNKS], pk[DP / 32];
+#pragma unroll
+  for (int i = 0; i < R::CHUNKS; ++i) {
+    off_k[i] = R::offset(a.K.token, BN, a.D, tid, i);
+    off_v[i] = R::offset(a.V.token, BN, a.D, tid, i);
+  }
+  R::columns(lds, lane, pk);
+  const int keys = std::min(len, q0 + BM);
+  const auto issue = [&](int k0, int slot) {
+    char* to = lds + slot * (2 * R::BYTES);
+    R::load(at(a.K, w.rows.start + static_cast<int64_t>(k0), kv_head), a.K.token, len - k0, a.D, to, wave, lane, off_k);
+    R::load(at(a.V, w.rows.start + static_cast<int64_t>(k0), kv_head), a.V.token, len - k0, a.D, to + R::BYTES, wave, lane, off_v);
+  };
+  issue(0, 0);
+  for (int k0 = 0, slot = 0; k0 < keys; k0 += BN, slot ^= 1) {
+    wait_step<0>();
+    if (k0 + BN < keys) issue(k0 + BN, slot ^ 1);
+    const char* stage = lds + slot * (2 * R::BYTES);
+    uint32_t p[DP / 32];
+#pragma unroll
+    for (int i = 0; i < DP / 32; ++i) p[i] = pk[i] + slot * (2 * R::BYTES);
+    const auto part = [&](auto half) {
+      constexpr int t = decltype(half)::value;
+      const int k = k0 + 32 * t;
+      if (k > qw + 31 || qw >= len) return;
+      f32x16 s = zero16(), ds = zero16();
+#pragma unroll
+      for (int kk = 0; kk < DP / 16; ++kk) {
+        s = mma(R::row(stage, 32 * t, kk, lane), q[kk], s, E{});
+        ds = mma(R::row(stage + R::BYTES, 32 * t, kk, lane), dy[kk], ds, E{});
+      }
+#pragma unroll
+      for (int r = 0; r < 16; ++r) ds[r] = __builtin_amdgcn_exp2f(fmaf(s[r], scale2, -lse2)) * (ds[r] - delta);
+      if (k + 31 > qw) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (k + place(r, h) > qi) ds[r] = 0.f;
+      }
+      lm_u32x4 f[DP / 32];
+      R::template column<32 * t * DP * 2>(p, f);
+      const lm_u32x4 x0 = terms<E>(ds, 0), x1 = terms<E>(ds, 1);
+#pragma unroll
+      for (int i = 0; i < DP / 32; ++i) dq[i] = mma(f[i], x0, dq[i], E{});
+      R::template column<(32 * t + 16) * DP * 2>(p, f);
+#pragma unroll
+      for (int i = 0; i < DP / 32; ++i) dq[i] = mma(f[i], x1, dq[i], E{});
+    };
+    part(std::integral_constant<int, 0>{});
+    part(std::integral_constant<int, 1>{});
+  }
+  if (qw >= len) return;
+  write_rows<E, DP>(at(a.dQ, row, w.head), a.dQ.token, len - qw, a.D, lane, dq, a.scale);
+}
+
+template <typename E, int DP>
+__global__ __launch_bounds__(256, 1) void k_attention_dkv(AttentionArgs a) {
+  typedef Rows<DP, BN, 256> R;
+  constexpr int STAGE = 2 * R::BYTES + 4 * 256;      // Q, dO, and of each query: delta, lse (twice: every wave loads)
+  __shared__ __align__(16) char lds[2 * STAGE];
+  const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
+  const int c = lane % 32, h = lane / 32;
+  const Work w = work(a, a.kv_heads, false, lane);
+  if (w.rows.empty()) return;
+  const int len = w.rows.end - w.rows.start, k0 = w.rows.first - w.rows.start, kw = k0 + 32 * wave, ki = kw + c;
+  const int share = a.heads / a.kv_heads;
+  const float scale2 = a.scale * kLog2E;
+  const int64_t row = w.rows.first + 32 * wave;
+
+  lm_u32x4 k[DP / 16], v[DP / 16];
+  operand<DP>(at(a.K, row, w.head), a.K.token, len - kw, a.D, lane, k);
+  operand<DP>(at(a.V, row, w.head), a.V.token, len - kw, a.D, lane, v);
+  f32x16 dk[DP / 32], dv[DP / 32];
+#pragma unroll
+  for (int i = 0; i < DP / 32; ++i) dk[i] = dv[i] = zero16();
+
+  uint32_t off_q[R::CHUNKS], off_d[R::CHUNKS], pq[DP / 32];
+#pragma unroll
+  for (int i = 0; i < R::CHUNKS; ++i) {
+    off_q[i] = R::offset(a.Q.token, BN, a.D, tid, i);
+    off_d[i] = R::offset(a.dO.token, BN, a.D, tid, i);
+  }
+  R::columns(lds, lane, pq);
+  // tiles of queries from the workgroup's first key on, for each head in turn
+  const int first = k0 / BN * BN;
+  const int steps = (len - first + BN - 1) / BN, all = steps * share;
+  int head_of = 0, q_of = first;      // the next stage to load
+  const auto issue = [&](int slot) {
+    char* to = lds + slot * STAGE;
+    const int head = w.head * share + head_of, left = len - q_of;
+    const int64_t from = w.rows.start + static_cast<int64_t>(q_of);
+    R::load(at(a.Q, from, head), a.Q.token, left, a.D, to, wave, lane, off_q);
+    R::load(at(a.dO, from, head), a.dO.token, left, a.D, to + R::BYTES, wave, lane, off_d);
+    typedef __attribute__((address_space(3))) void* P;
+    const float* x = a.delta + (wave % 2 * a.heads + head) * a.T + from;
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(make_rsrc(x, static_cast<uint32_t>(kMaxBufferBytes)),
+                                             (P)(to + 2 * R::BYTES + wave * 256), 4,
+                                             lane < left ? static_cast<uint32_t>(lane * 4) : kOutOfRange, 0, 0, 0);
+    q_of += BN;
+    if (q_of >= len) {
+      q_of = first;
+      ++head_of;
+    }
+  };
+  issue(0);
+  int q0 = first;
+  for (int i = 0, slot = 0; i < all; ++i, slot ^= 1) {
+    wait_step<0>();
+    if (i + 1 < all) issue(slot ^ 1);
+    const char* stage = lds + slot * STAGE;
+    uint32_t p[DP / 32];
+#pragma unroll
+    for (int j = 0; j < DP / 32; ++j) p[j] = pq[j] + slot * STAGE;
+    const auto part = [&](auto half) {
+      constexpr int t = decltype(half)::value;
+      const int q = q0 + 32 * t;
+      if (q + 31 < kw || q >= len || kw >= len) return;
+      f32x16 s = zero16(), ds = zero16();
+#pragma unroll
+      for (int kk = 0; kk < DP / 16; ++kk) {
+        s = mma(R::row(stage, 32 * t, kk, lane), k[kk], s, E{});
+        ds = mma(R::row(stage + R::BYTES, 32 * t, kk, lane), v[kk], ds, E{});
+      }
+      const char* stats = stage + 2 * R::BYTES + (32 * t + 4 * h) * 4;
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const lm_f32x4 delta = *reinterpret_cast<const lm_f32x4*>(stats + 32 * g);
+        const lm_f32x4 lse2 = *reinterpret_cast<const lm_f32x4*>(stats + 256 + 32 * g);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int r = 4 * g + j;
+          s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], scale2, -lse2[j]));
+          ds[r] = s[r] * (ds[r] - delta[j]);
+        }
+      }
+      if (q < kw + 31 || q + 31 >= len) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (ki > q + place(r, h) || q + place(r, h) >= len) s[r] = ds[r] = 0.f;
+      }
+      const auto product = [&](auto at_) {
+        constexpr int u = decltype(at_)::value;
+        lm_u32x4 f[DP / 32];
+        R::template column<(32 * t + 16 * u) * DP * 2>(p, f);
+        const lm_u32x4 y = terms<E>(ds, u);
+#pragma unroll
+        for (int j = 0; j < DP / 32; ++j) dk[j] = mma(f[j], y, dk[j], E{});
+        R::template column<(32 * t + 16 * u) * DP * 2 + R::BYTES>(p, f);
+        const lm_u32x4 x = terms<E>(s, u);
+#pragma unroll
+        for (int j = 0; j < DP / 32; ++j) dv[j] = mma(f[j], x, dv[j], E{});
+      };
+      product(std::integral_constant<int, 0>{});
+      product(std::integral_constant<int, 1>{});
+    };
+    part(std::integral_constant<int, 0>{});
+    part(std::integral_constant<int, 1>{});
+    q0 += BN;
+    if (q0 >= len) q0 = first;
+  }
+  if (kw >= len) return;
+  write_rows<E, DP>(at(a.dK, row, w.head), a.dK.token, len - kw, a.D, lane, dk, a.scale);
+  write_rows<E, DP>(at(a.dV, row, w.head), a.dV.token, len - kw, a.D, lane, dv, 1.f);
+}
+
+uint32_t slots_of(const AttentionArgs& a) { return static_cast<uint32_t>(a.T / BM + a.n); }
+
+template <typename E, int DP>
+void launch_typed(const AttentionArgs& a, bool grad, hipStream_t s) {
+  if (!grad) {
+    k_attention<E, DP><<<a.slots * a.heads, 256, 0, s>>>(a);
+    return;
+  }
+  k_attention_dq<E, DP><<<a.slots * a.heads, 256, 0, s>>>(a);
+  k_attention_dkv<E, DP><<<a.slots * a.kv_heads, 256, 0, s>>>(a);
+}
+template <typename E>
+void launch_wide(const AttentionArgs& a, bool grad, hipStream_t s) {
+  if (a.D <= 64) launch_typed<E, 64>(a, grad, s);
+  else if (a.D <= 96) launch_typed<E, 96>(a, grad, s);
+  else launch_typed<E, 128>(a, grad, s);
+}
+hipError_t launch(AttentionArgs a, bool grad, hipStream_t s) {
+  if (a.T == 0) return hipSuccess;
+  a.slots = slots_of(a);
+  if (a.dtype == DBW_BF16) launch_wide<__bf16>(a, grad, s);
+  else launch_wide<_Float16>(a, grad, s);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_attention(AttentionArgs a, hipStream_t s) { return launch(a, false, s); }
+hipError_t launch_attention_grad(AttentionArgs a, hipStream_t s) { return launch(a, true, s); }
+
+}  // namespace dbw

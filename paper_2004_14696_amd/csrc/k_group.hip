@@ -39,6 +39,7 @@
 
 #include "dbw_buffer.h"
 #include "lm_ops.h"
+#include "lm_tiles.h"
 
 namespace dbw {
 namespace {
@@ -66,6 +67,19 @@ struct Tile {
   int k0, k1;
   int rows, cols;
   int line_a, line_b;   // values of a line of either matrix
+};
+
+// What becomes of the sums z of a tile in a product with an epilogue: Z = z + b
+// is stored, and act(Z) + R is the output.  Pointers are those of the tile's
+// first row and column.
+struct Epilogue {
+  int act = DBW_ACT_NONE;
+  const float* bias = nullptr;
+  int64_t st_bias = 0;
+  const void* residual = nullptr;
+  int64_t ld_residual = 0;
+  void* pre = nullptr;
+  int64_t ld_pre = 0;
 };
 
 // One operand's part of a step: L outputs x BK terms, by THREADS threads.
@@ -170,12 +184,6 @@ struct Operand {
         : "memory");
   }
 };
-
-// 16 bytes a lane from r + off to the wave's 1 KiB at `to`.
-__device__ __forceinline__ void load_lds(__amdgpu_buffer_rsrc_t r, char* to, uint32_t off) {
-  typedef __attribute__((address_space(3))) void* P;
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (P)to, 16, off, 0, 0, 0);
-}
 
 // Loads of one step after the other straight into LDS: a wave's instruction
 // fills 1 KiB, lane by lane.  Needs whole chunks: every line of memory starts
@@ -296,24 +304,6 @@ struct Staged {
   }
 };
 
-// Waits until at most `loads` of this wave's loads are outstanding and all its
-// LDS reads are done, then for the other waves.
-template <int loads>
-__device__ __forceinline__ void wait_step() {
-  static_assert(loads < 64, "six bits");
-  asm volatile("" ::: "memory");
-  __builtin_amdgcn_s_waitcnt((loads & 15) | 7 << 4 | 0 << 8 | (loads >> 4) << 14);
-  __builtin_amdgcn_s_barrier();
-  asm volatile("" ::: "memory");
-}
-
-template <typename E>
-__device__ __forceinline__ uint32_t pack2(float a, float b) {
-  typedef float F __attribute__((ext_vector_type(2)));
-  typedef E V __attribute__((ext_vector_type(2)));
-  return __builtin_bit_cast(uint32_t, __builtin_convertvector(F{a, b}, V));
-}
-
 // N consecutive outputs of one row, `left` of them inside.
 template <typename O, int N, bool STREAM = false>
 __device__ __forceinline__ void store_out(O* p, const lm_u32x4& v, int left) {
@@ -370,9 +360,86 @@ __device__ __forceinline__ void write_out(const f32x4 (&acc)[WM / 16][WN / 16], 
   }
 }
 
+// Four values of type O at p, `left` of them inside (the others are 0).
+template <typename O>
+__device__ __forceinline__ f32x4 load4(const O* p, int left) {
+  f32x4 x = {0.f, 0.f, 0.f, 0.f};
+  if (left >= 4) {
+    if constexpr (sizeof(O) == 4) {
+      x = *reinterpret_cast<const lm_f32x4_any*>(p);
+    } else {
+      typedef O V __attribute__((ext_vector_type(4)));
+      const V v = __builtin_bit_cast(V, static_cast<lm_u32x2>(*reinterpret_cast<const lm_u32x2_any*>(p)));
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[j] = lm_to_f32(v[j]);
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 3; ++j)
+      if (j < left) x[j] = lm_to_f32(p[j]);
+  }
+  return x;
+}
+template <typename O>
+__device__ __forceinline__ void store4(O* p, const f32x4& x, int left) {
+  if constexpr (sizeof(O) == 4) {
+    store_out<O, 4>(p, __builtin_bit_cast(lm_u32x4, x), left);
+  } else if (left >= 4) {
+    *reinterpret_cast<lm_u32x2_any*>(p) = lm_u32x2{pack2<O>(x[0], x[1]), pack2<O>(x[2], x[3])};
+  } else {
+#pragma unroll
+    for (int j = 0; j < 3; ++j)
+      if (j < left) p[j] = static_cast<O>(x[j]);
+  }
+}
+
+// Four columns of one row, from their sums z: n and m count from the tile's
+// first column and row.
+template <typename E, typename O>
+__device__ __forceinline__ void finish4(const Epilogue& e, O* out, int64_t ldo, int m, int n, int left, f32x4 z) {
+  if (e.bias) z += load4<float>(e.bias + n, left);
+  if (e.pre) store4<E>(static_cast<E*>(e.pre) + m * e.ld_pre + n, z, left);
+  if (e.act != DBW_ACT_NONE)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) z[j] = lm_act(z[j], e.act);
+  if (e.residual) z += load4<O>(static_cast<const O*>(e.residual) + m * e.ld_residual + n, left);
+  store4<O>(out + m * ldo + n, z, left);
+}
+
+// A wave's outputs with an epilogue: the sums go through LDS as they are, so
+// that a lane finishes four columns of a row and memory takes whole lines.
+template <typename E, typename O, int WM, int WN, int LDS>
+__device__ __forceinline__ void write_finished(const f32x4 (&acc)[WM / 16][WN / 16], const Tile& t, const Epilogue& e,
+                                               int m0, int n0, char* lds, int lane) {
+  constexpr int BYTES = WN * 4, CH = BYTES / 16;
+  constexpr int TILES = LDS / BYTES / 16 >= WM / 16 ? WM / 16 : LDS / BYTES >= 64 ? 4 : LDS / BYTES >= 32 ? 2 : 1;
+  constexpr int ROWS = 16 * TILES;
+  static_assert(ROWS * BYTES <= LDS && WM % ROWS == 0 && ROWS * CH % 64 == 0, "whole passes");
+  const int c = lane % 16, g = lane / 16;
+#pragma unroll
+  for (int p = 0; p < WM / ROWS; ++p) {
+#pragma unroll
+    for (int i = 0; i < TILES; ++i) {
+      const int row = i * 16 + c;
+#pragma unroll
+      for (int j = 0; j < WN / 16; ++j)
+        *reinterpret_cast<f32x4*>(lds + row * BYTES + ((j * 4 + g) ^ (row & (CH - 1) & 15)) * 16) = acc[p * TILES + i][j];
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll 4
+    for (int i = 0; i < ROWS * CH / 64; ++i) {
+      const int row = (i * 64 + lane) / CH, q = (i * 64 + lane) % CH;
+      const f32x4 z = *reinterpret_cast<const f32x4*>(lds + row * BYTES + (q ^ (row & (CH - 1) & 15)) * 16);
+      const int m = m0 + p * ROWS + row, n = n0 + q * 4;
+      if (m < t.rows && n < t.cols) finish4<E, O>(e, static_cast<O*>(t.out), t.ldo, m, n, t.cols - n, z);
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  }
+}
+
 template <typename E, int BM, int BN, int WM, int WN, int BK, int STAGES, bool A_SWAP, bool B_SWAP, bool WIDE,
-          bool STREAM>
-__device__ __forceinline__ void product(const Tile& t, bool out_f32, char* lds) {
+          bool STREAM, bool EPILOGUE>
+__device__ __forceinline__ void product(const Tile& t, const Epilogue& e, bool out_f32, bool parts, char* lds) {
   constexpr int THREADS = (BM / WM) * (BN / WN) * 64;
   constexpr int TM = WM / 16, TN = WN / 16;
   typedef Operand<E, BM, BK, THREADS, A_SWAP> OpA;
@@ -468,7 +535,15 @@ __device__ __forceinline__ void product(const Tile& t, bool out_f32, char* lds) 
 
   constexpr int LDS = (WIDE ? STAGES : 2) * STAGE / (THREADS / 64);   // bytes a wave
   char* mine = lds + wave * LDS;
-  if (out_f32)
+  if constexpr (EPILOGUE)
+    if (!parts) {
+      if (out_f32)
+        write_finished<E, float, WM, WN, LDS>(acc, t, e, m0, n0, mine, lane);
+      else
+        write_finished<E, E, WM, WN, LDS>(acc, t, e, m0, n0, mine, lane);
+      return;
+    }
+  if (out_f32 || parts)
     write_out<float, WM, WN, LDS, STREAM>(acc, t, m0, n0, mine, lane);
   else
     write_out<E, WM, WN, LDS, STREAM>(acc, t, m0, n0, mine, lane);
@@ -485,6 +560,7 @@ struct GroupArgs {
   int64_t part;
   uint32_t row_tiles, col_tiles, blocks, run;
   int out_f32, out_bytes;
+  Epilogue epilogue;
 };
 
 // Terms of one part of a sum of `length` terms: whole steps.
@@ -492,7 +568,7 @@ __device__ __forceinline__ int64_t split_of(int64_t length, int splits) {
   return ((length + 63) / 64 + splits - 1) / splits * 64;
 }
 
-template <typename E, int BM, int BN, int WM, int WN, int BK, int STAGES, int FORM, bool WIDE>
+template <typename E, int BM, int BN, int WM, int WN, int BK, int STAGES, int FORM, bool WIDE, bool EPILOGUE>
 __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64, 2) void k_group(GroupArgs g) {
   constexpr bool A_SWAP = FORM == DBW_GROUP_WEIGHT_GRAD, B_SWAP = FORM != DBW_GROUP_INPUT_GRAD;
   __shared__ __align__(16) char lds[(WIDE ? STAGES : 2) * (BM + BN) * BK * 2];
@@ -503,6 +579,7 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64, 2) void k_group(GroupAr
   if (id >= g.blocks) return;
   const int lane = threadIdx.x % 64;
   Tile t;
+  Epilogue e;
   if (FORM == DBW_GROUP_WEIGHT_GRAD) {
     uint32_t q = id;
     const uint32_t rt = q % g.row_tiles;
@@ -595,8 +672,15 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64, 2) void k_group(GroupAr
       t.ldo = FORM == DBW_GROUP_FORWARD ? g.ld_C : g.ld_d;
       t.out = static_cast<char*>(g.out) + (row * t.ldo + n) * g.out_bytes;
     }
+    if constexpr (EPILOGUE) {
+      e = g.epilogue;
+      if (e.bias) e.bias += group * e.st_bias + n;
+      if (e.residual) e.residual = static_cast<const char*>(e.residual) + (row * e.ld_residual + n) * g.out_bytes;
+      if (e.pre) e.pre = static_cast<E*>(e.pre) + row * e.ld_pre + n;
+    }
   }
-  product<E, BM, BN, WM, WN, BK, STAGES, A_SWAP, B_SWAP, WIDE, FORM == DBW_GROUP_WEIGHT_GRAD>(t, g.splits > 1 || g.out_f32, lds);
+  product<E, BM, BN, WM, WN, BK, STAGES, A_SWAP, B_SWAP, WIDE, FORM == DBW_GROUP_WEIGHT_GRAD, EPILOGUE>(
+      t, e, g.out_f32, g.splits > 1, lds);
 }
 
 // out = the sum of the partial outputs, in the order of the parts; a thread
@@ -642,38 +726,72 @@ __global__ __launch_bounds__(256) void k_group_sum(GroupArgs g, const float* __r
   }
 }
 
+// The same with an epilogue (Y only).
+template <typename E, typename O>
+__global__ __launch_bounds__(256) void k_group_finish(GroupArgs g, const float* __restrict__ parts) {
+  const uint32_t N = g.C, quads = (N + 3) / 4;
+  const uint32_t first = static_cast<uint32_t>(lm_offset(g.offsets, 0, g.T));
+  const uint32_t end = static_cast<uint32_t>(lm_offset(g.offsets, g.n, g.T));
+  if (end <= first) return;
+  const uint32_t all = (end - first) * quads;
+  for (uint32_t i = blockIdx.x * 256 + threadIdx.x; i < all; i += gridDim.x * 256) {
+    const uint32_t row = first + i / quads, n = i % quads * 4;
+    const float* p = parts + static_cast<int64_t>(row) * N + n;
+    const int left = N - n < 4 ? static_cast<int>(N - n) : 4;
+    f32x4 z = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+    for (int s = 0; s < g.splits; ++s) z += load4<float>(p + s * g.part, left);
+    Epilogue e = g.epilogue;
+    if (e.bias && e.st_bias) {
+      // the row's group: the last whose first row is not behind it
+      int lo = 0, hi = g.n;
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        if (lm_offset(g.offsets, mid, g.T) <= row) lo = mid;
+        else hi = mid;
+      }
+      e.bias += lo * e.st_bias;
+    }
+    if (e.residual) e.residual = static_cast<const O*>(e.residual) + row * e.ld_residual;
+    if (e.pre) e.pre = static_cast<E*>(e.pre) + row * e.ld_pre;
+    finish4<E, O>(e, static_cast<O*>(g.out) + row * g.ld_C, 0, 0, n, left, z);
+  }
+}
+
 enum GroupVariant { SMALL = 0, MIDDLE = 1, LARGE = 2 };
 struct VariantSize {
   int bm, bn;
 };
 constexpr VariantSize kSize[] = {{32, 128}, {128, 128}, {128, 256}};
 
-template <typename E, int FORM, bool WIDE>
+template <typename E, int FORM, bool WIDE, bool EPI>
 void launch_variant(const GroupPlan& plan, const GroupArgs& g, uint32_t grid, hipStream_t s) {
   constexpr bool GRAD = FORM == DBW_GROUP_WEIGHT_GRAD;
   constexpr int BK = WIDE && GRAD ? 32 : 64;
   if constexpr (WIDE && FORM != DBW_GROUP_INPUT_GRAD)
     if (plan.variant == LARGE) {
-      k_group<E, 128, 256, 64, 128, 32, 3, FORM, WIDE><<<grid, 256, 0, s>>>(g);
+      k_group<E, 128, 256, 64, 128, 32, 3, FORM, WIDE, EPI><<<grid, 256, 0, s>>>(g);
       return;
     }
   if constexpr (!GRAD)
     if (plan.variant == SMALL) {
-      k_group<E, 32, 128, 16, 64, 64, 3, FORM, WIDE><<<grid, 256, 0, s>>>(g);
+      k_group<E, 32, 128, 16, 64, 64, 3, FORM, WIDE, EPI><<<grid, 256, 0, s>>>(g);
       return;
     }
-  k_group<E, 128, 128, 64, 64, BK, 128 / BK, FORM, WIDE><<<grid, 256, 0, s>>>(g);
+  k_group<E, 128, 128, 64, 64, BK, 128 / BK, FORM, WIDE, EPI><<<grid, 256, 0, s>>>(g);
 }
-template <typename E, int FORM>
+template <typename E, int FORM, bool EPI = false>
 void launch_wide(bool wide, const GroupPlan& plan, const GroupArgs& g, uint32_t grid, hipStream_t s) {
   if (wide)
-    launch_variant<E, FORM, true>(plan, g, grid, s);
+    launch_variant<E, FORM, true, EPI>(plan, g, grid, s);
   else
-    launch_variant<E, FORM, false>(plan, g, grid, s);
+    launch_variant<E, FORM, false, EPI>(plan, g, grid, s);
 }
 template <typename E>
-void launch_form(bool wide, const GroupPlan& plan, const GroupArgs& g, uint32_t grid, hipStream_t s) {
-  if (g.form == DBW_GROUP_FORWARD)
+void launch_form(bool wide, bool epilogue, const GroupPlan& plan, const GroupArgs& g, uint32_t grid, hipStream_t s) {
+  if (epilogue)
+    launch_wide<E, DBW_GROUP_FORWARD, true>(wide, plan, g, grid, s);
+  else if (g.form == DBW_GROUP_FORWARD)
     launch_wide<E, DBW_GROUP_FORWARD>(wide, plan, g, grid, s);
   else if (g.form == DBW_GROUP_INPUT_GRAD)
     launch_wide<E, DBW_GROUP_INPUT_GRAD>(wide, plan, g, grid, s);
@@ -804,7 +922,7 @@ GroupPlan group_plan(const dbw_group_shape& p) {
 }
 
 hipError_t launch_group(const dbw_group_shape& p, GroupPlan plan, const int32_t* offsets, const void* a,
-                        const void* b, void* out, float* workspace, hipStream_t s) {
+                        const void* b, void* out, float* workspace, const dbw_linear_epilogue* epilogue, hipStream_t s) {
   const bool grad = p.form == DBW_GROUP_WEIGHT_GRAD;
   if (!grad && p.T == 0) return hipSuccess;
   // whole chunks of 16 bytes: every row starts at one and ends with one
@@ -829,18 +947,36 @@ hipError_t launch_group(const dbw_group_shape& p, GroupPlan plan, const int32_t*
   g.out_bytes = elem_bytes(p.out_dtype);
   g.blocks = static_cast<uint32_t>(plan.blocks);
   g.out = plan.splits > 1 ? workspace : out;
+  if (epilogue) {
+    g.epilogue.act = epilogue->activation;
+    g.epilogue.bias = epilogue->bias;
+    g.epilogue.st_bias = epilogue->st_bias;
+    g.epilogue.residual = epilogue->residual;
+    g.epilogue.ld_residual = epilogue->ld_residual;
+    g.epilogue.pre = epilogue->pre;
+    g.epilogue.ld_pre = epilogue->ld_pre;
+  }
   g.run = std::min((g.blocks + 7) / 8, 32u);
   const uint32_t grid = static_cast<uint32_t>(ceil_div(g.blocks, 8 * g.run)) * 8 * g.run;
   if (p.dtype == DBW_BF16)
-    launch_form<__bf16>(wide, plan, g, grid, s);
+    launch_form<__bf16>(wide, epilogue, plan, g, grid, s);
   else
-    launch_form<_Float16>(wide, plan, g, grid, s);
+    launch_form<_Float16>(wide, epilogue, plan, g, grid, s);
   if (plan.splits > 1) {
     g.out = out;
     const uint32_t sums = static_cast<uint32_t>(std::max<int64_t>(1, std::min<int64_t>(ceil_div(plan.part, 1024), 2048)));
-    if (p.out_dtype == DBW_F32)
+    const bool bf16 = p.dtype == DBW_BF16;
+    if (epilogue && p.out_dtype == DBW_F32 && bf16)
+      k_group_finish<__bf16, float><<<sums, 256, 0, s>>>(g, workspace);
+    else if (epilogue && p.out_dtype == DBW_F32)
+      k_group_finish<_Float16, float><<<sums, 256, 0, s>>>(g, workspace);
+    else if (epilogue && bf16)
+      k_group_finish<__bf16, __bf16><<<sums, 256, 0, s>>>(g, workspace);
+    else if (epilogue)
+      k_group_finish<_Float16, _Float16><<<sums, 256, 0, s>>>(g, workspace);
+    else if (p.out_dtype == DBW_F32)
       k_group_sum<float><<<sums, 256, 0, s>>>(g, workspace);
-    else if (p.dtype == DBW_BF16)
+    else if (bf16)
       k_group_sum<__bf16><<<sums, 256, 0, s>>>(g, workspace);
     else
       k_group_sum<_Float16><<<sums, 256, 0, s>>>(g, workspace);

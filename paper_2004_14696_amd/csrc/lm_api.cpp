@@ -1,4 +1,4 @@
-// C ABI of the operators for language models: argument checks, plans and
+// C ABI of the products, the token loss and AdamW: argument checks, plans and
 // launches.  The kernels are in k_group.hip, k_token.hip and k_adamw.hip.
 #include <hip/hip_runtime.h>
 
@@ -18,7 +18,7 @@ using dbw::set_free_error;
 
 namespace {
 
-bool aligned(const void* p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
+using dbw::aligned;
 
 // Makes `dev` the current device for a scope.
 struct OnDevice {
@@ -78,12 +78,12 @@ DBW_API dbw_status dbw_group_workspace(const dbw_group_shape* shape, int64_t* by
   return DBW_OK;
 }
 
-DBW_API dbw_status dbw_group_product(const dbw_group_shape* shape, const int32_t* offsets, const void* a,
-                                     const void* b, void* out, void* workspace, int64_t workspace_bytes,
-                                     void* stream) {
-  const char* call = "dbw_group_product";
+namespace {
+// Checks of a product's pointers, and the product.
+dbw_status group_call(const char* call, const dbw_group_shape* shape, const dbw_linear_epilogue* epilogue,
+                      const int32_t* offsets, const void* a, const void* b, void* out, void* workspace,
+                      int64_t workspace_bytes, void* stream) {
   int64_t need = 0;
-  if (dbw_status s = check_shape(shape, call); s != DBW_OK) return s;
   if (dbw_status s = dbw_group_workspace(shape, &need); s != DBW_OK) return s;
   const bool grad = shape->form == DBW_GROUP_WEIGHT_GRAD;
   // without rows, the arrays of T rows may be empty
@@ -98,10 +98,49 @@ DBW_API dbw_status dbw_group_product(const dbw_group_shape* shape, const int32_t
   if (out && (out == a || out == b))
     return set_free_error(DBW_EINVAL, "%s: out must not overlap the inputs", call);
   const dbw::GroupPlan plan = dbw::group_plan(*shape);
-  const hipError_t e = dbw::launch_group(*shape, plan, offsets, a, b, out, static_cast<float*>(workspace),
+  const hipError_t e = dbw::launch_group(*shape, plan, offsets, a, b, out, static_cast<float*>(workspace), epilogue,
                                          static_cast<hipStream_t>(stream));
   if (e != hipSuccess) return set_free_error(DBW_EHIP, "%s: launch failed: %s", call, hipGetErrorString(e));
   return DBW_OK;
+}
+}  // namespace
+
+DBW_API dbw_status dbw_group_product(const dbw_group_shape* shape, const int32_t* offsets, const void* a,
+                                     const void* b, void* out, void* workspace, int64_t workspace_bytes,
+                                     void* stream) {
+  const char* call = "dbw_group_product";
+  if (dbw_status s = check_shape(shape, call); s != DBW_OK) return s;
+  return group_call(call, shape, nullptr, offsets, a, b, out, workspace, workspace_bytes, stream);
+}
+
+DBW_API dbw_status dbw_group_linear(const dbw_group_shape* shape, const dbw_linear_epilogue* epilogue,
+                                    const int32_t* offsets, const void* X, const void* W, void* Y, void* workspace,
+                                    int64_t workspace_bytes, void* stream) {
+  const char* call = "dbw_group_linear";
+  if (dbw_status s = check_shape(shape, call); s != DBW_OK) return s;
+  if (shape->form != DBW_GROUP_FORWARD) return set_free_error(DBW_EINVAL, "%s: the form is FORWARD", call);
+  if (!epilogue) return set_free_error(DBW_EINVAL, "%s: epilogue is NULL", call);
+  dbw_linear_epilogue e = *epilogue;
+  if (e.activation < DBW_ACT_NONE || e.activation > DBW_ACT_SILU)
+    return set_free_error(DBW_EINVAL, "%s: unknown activation %d", call, e.activation);
+  if (!aligned(e.bias, 4) || !aligned(e.residual, dbw::elem_bytes(shape->out_dtype)) || !aligned(e.pre, 2))
+    return set_free_error(DBW_EINVAL, "%s: a pointer is not aligned to its elements", call);
+  if (!e.bias || shape->n == 1) e.st_bias = 0;
+  if (e.st_bias && e.st_bias < shape->C)
+    return set_free_error(DBW_EINVAL, "%s: b_1 would overlap b_0 (st_bias=%lld)", call, (long long)e.st_bias);
+  if (e.st_bias && shape->st_W == 0)
+    return set_free_error(DBW_EINVAL, "%s: groups that share W share its bias", call);
+  if (e.st_bias >= (int64_t{1} << 40)) return set_free_error(DBW_EUNSUPPORTED, "%s: st_bias reaches 2^40", call);
+  if ((e.residual && e.ld_residual < shape->C) || (e.pre && e.ld_pre < shape->C))
+    return set_free_error(DBW_EINVAL, "%s: a row stride is below its row", call);
+  const int64_t most = int64_t{1} << 21;
+  if ((e.residual && e.ld_residual >= most) || (e.pre && e.ld_pre >= most))
+    return set_free_error(DBW_EUNSUPPORTED, "%s: a row stride reaches 2^21", call);
+  if (e.residual && e.residual == Y && e.ld_residual != shape->ld_C)
+    return set_free_error(DBW_EINVAL, "%s: Y in the place of R needs its row stride", call);
+  if (e.pre && (e.pre == Y || e.pre == X || e.pre == W || e.pre == e.residual))
+    return set_free_error(DBW_EINVAL, "%s: Z must not overlap other arrays", call);
+  return group_call(call, shape, &e, offsets, X, W, Y, workspace, workspace_bytes, stream);
 }
 
 // ---------------------------------------------------------------------------

@@ -1,5 +1,5 @@
 // Internal declarations of the operators for language models: grouped
-// products, token loss, AdamW.  Not part of the C ABI.
+// products, token loss, AdamW, and those of a transformer block.  Not part of the C ABI.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -12,6 +12,7 @@
 namespace dbw {
 
 inline int elem_bytes(int32_t dtype) { return dtype == DBW_F32 ? 4 : 2; }
+inline bool aligned(const void* p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
 
 // 16-byte (8-byte) vectors at addresses aligned to their elements only: global
 // memory takes them, and the compiler emits one load or store.
@@ -126,6 +127,181 @@ __host__ __device__ inline uint32_t adam_index(int64_t index) {
 }
 
 // ---------------------------------------------------------------------------
+// Rows of ragged groups in chunks of `rows` rows: chunk number `slot` belongs
+// to the group i with the largest (offsets[i] - offsets[0]) / rows + i that is
+// not above it (a group has its first row's number of whole chunks, and one
+// more for each group before it, in front of it, so that groups' slots never
+// meet); T / rows + n slots hold all chunks, and some stay empty.  A whole wave
+// looks at 64 groups at once.
+struct LmChunk {
+  int group;
+  int32_t first;    // the chunk's first row
+  int32_t start;    // the group's
+  int32_t end;
+  __device__ bool empty() const { return first >= end; }
+};
+__device__ __forceinline__ uint32_t lm_first_slot(const int32_t* offsets, int i, int64_t T, uint32_t o0, uint32_t rows) {
+  const uint32_t o = static_cast<uint32_t>(lm_offset(offsets, i, T));
+  return (o > o0 ? o - o0 : 0) / rows + i;
+}
+__device__ __forceinline__ LmChunk lm_chunk(const int32_t* offsets, int n, int64_t T, uint32_t rows, uint32_t slot,
+                                            int lane) {
+  const uint32_t o0 = static_cast<uint32_t>(lm_offset(offsets, 0, T));
+  int lo = 0, count = n;
+  while (count > 1) {
+    const int step = (count + 63) / 64, at = lane * step;
+    const bool below = at < count && lm_first_slot(offsets, lo + at, T, o0, rows) <= slot;
+    const uint64_t past = __ballot(below);
+    const int k = past ? 63 - __builtin_clzll(past) : 0;
+    lo += k * step;
+    count = count - k * step < step ? count - k * step : step;
+  }
+  LmChunk c;
+  c.group = lo;
+  const int64_t start = lm_offset(offsets, lo, T);
+  const uint32_t first = lm_first_slot(offsets, lo, T, o0, rows);
+  const int64_t row = start + static_cast<int64_t>(slot > first ? slot - first : 0) * rows;
+  c.start = static_cast<int32_t>(start);
+  c.end = static_cast<int32_t>(lm_offset(offsets, lo + 1, T));
+  c.first = row < c.end ? static_cast<int32_t>(row) : c.end;
+  c.group = __builtin_amdgcn_readfirstlane(c.group);
+  c.start = __builtin_amdgcn_readfirstlane(c.start);
+  c.end = __builtin_amdgcn_readfirstlane(c.end);
+  c.first = __builtin_amdgcn_readfirstlane(c.first);
+  return c;
+}
+
+// ---------------------------------------------------------------------------
+// Activations: z sigmoid(s(z)) with s = 2 (a z + b z^3) or z, or simpler ones.
+constexpr float kLog2E = 1.44269504088896341f;
+constexpr float kGeluA = 0.797884560802865356f, kGeluB = 0.0356774081363001f;   // sqrt(2/pi), 0.044715 sqrt(2/pi)
+__device__ __forceinline__ float lm_sigmoid(float s) {
+  return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-kLog2E * s));
+}
+__device__ __forceinline__ float lm_act(float z, int act) {
+  if (act == DBW_ACT_RELU) return z < 0.f ? 0.f : z;   // (a NaN stays)
+  if (act == DBW_ACT_GELU) return z * lm_sigmoid(2.f * z * fmaf(kGeluB * z, z, kGeluA));
+  if (act == DBW_ACT_SILU) return z * lm_sigmoid(z);
+  return z;
+}
+// p + z p (1 - p) s'(z) with p = sigmoid(s): 1 - p as e / (1 + e), so that it keeps
+// its digits where p is near 1 (1 - p by subtraction left 1e-5 of GELU's slope at
+// 5).  Beyond the limits of z the slope is 0 or 1 to 2^-100, and e = exp(-s) not
+// finite.
+__device__ __forceinline__ float lm_act_slope(float z, int act) {
+  if (act == DBW_ACT_RELU) return z > 0.f ? 1.f : (z <= 0.f ? 0.f : z);
+  if (act == DBW_ACT_NONE) return 1.f;
+  const bool gelu = act == DBW_ACT_GELU;
+  const float most = gelu ? 10.f : 80.f;
+  z = z > most ? most : (z < -most ? -most : z);   // (a NaN stays)
+  const float s = gelu ? 2.f * z * fmaf(kGeluB * z, z, kGeluA) : z;
+  const float ds = gelu ? 2.f * fmaf(3.f * kGeluB * z, z, kGeluA) : 1.f;
+  const float e = __builtin_amdgcn_exp2f(-kLog2E * s), p = __builtin_amdgcn_rcpf(1.f + e);
+  return fmaf(z * p * (e * p), ds, p);
+}
+
+// ---------------------------------------------------------------------------
+// Layer norm, the gradient of an activation with its bias, dropout.
+struct NormArgs {
+  int n, d;
+  int64_t T;
+  int dtype;
+  const int32_t* offsets;
+  const void* dY;       // gradient only
+  int64_t ld_dY;
+  const void* X;
+  int64_t ld_X;
+  const float* gamma;
+  const float* beta;    // forward only, nullable
+  float eps;
+  void* out;            // Y or dX
+  int64_t ld_out;
+  float* dgamma;
+  int64_t ld_dgamma;
+  float* dbeta;         // nullable
+  int64_t ld_dbeta;
+  float* parts;         // workspace [2][slots][d]
+  uint32_t rows, slots; // rows of a chunk, chunks (set by the launch)
+};
+constexpr int kNormMost = 16384;
+int64_t norm_workspace(int n, int64_t T, int d);
+hipError_t launch_layer_norm(const NormArgs& a, hipStream_t s);
+hipError_t launch_layer_norm_grad(NormArgs a, hipStream_t s);
+
+struct LinearGradArgs {
+  int n, C;
+  int64_t T;
+  int dtype, act;
+  const int32_t* offsets;
+  const void* dY;
+  int64_t ld_dY;
+  const void* Z;        // nullable: no activation
+  int64_t ld_Z;
+  void* dZ;             // nullable
+  int64_t ld_dZ;
+  float* dbias;         // nullable
+  int64_t ld_dbias;
+  float* parts;         // workspace [slots][C]
+  uint32_t rows, slots;
+};
+int64_t linear_grad_workspace(int n, int64_t T, int C);
+hipError_t launch_linear_grad(LinearGradArgs a, hipStream_t s);
+
+struct DropoutArgs {
+  int n, d;
+  int64_t T;
+  int dtype;
+  const int32_t* offsets;
+  const void* X;
+  int64_t ld_X;
+  const void* R;        // nullable
+  int64_t ld_R;
+  void* Y;
+  int64_t ld_Y;
+  uint32_t cut;         // dropped below
+  float scale;
+  uint64_t seed;
+  const int64_t* step;  // nullable
+};
+hipError_t launch_dropout(const DropoutArgs& a, hipStream_t s);
+
+// Philox4x32-10 (J. Salmon, M. Moraes, R. Dror, D. Shaw, "Parallel random
+// numbers: as easy as 1, 2, 3", 2011).
+__host__ __device__ inline void lm_philox(uint32_t (&c)[4], uint32_t k0, uint32_t k1) {
+#pragma unroll
+  for (int r = 0; r < 10; ++r) {
+    const uint64_t p = static_cast<uint64_t>(0xD2511F53u) * c[0], q = static_cast<uint64_t>(0xCD9E8D57u) * c[2];
+    c[0] = static_cast<uint32_t>(q >> 32) ^ c[1] ^ k0;
+    c[1] = static_cast<uint32_t>(q);
+    c[2] = static_cast<uint32_t>(p >> 32) ^ c[3] ^ k1;
+    c[3] = static_cast<uint32_t>(p);
+    k0 += 0x9E3779B9u;
+    k1 += 0xBB67AE85u;
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Attention.
+struct HeadRows {
+  char* p;
+  int64_t token, head;  // elements
+};
+struct AttentionArgs {
+  int n, heads, kv_heads, D;
+  int64_t T;
+  int dtype;
+  float scale;
+  const int32_t* offsets;
+  HeadRows Q, K, V, O, dO, dQ, dK, dV;
+  float* lse;           // [heads][T], nullable in the forward pass
+  float* delta;         // workspace [2][heads][T]: dO . O, and lse log2(e)
+  uint32_t slots;       // tiles of a head's queries or keys (set by the launch)
+};
+constexpr int kAttentionRows = 128;   // queries, or keys, of a workgroup
+hipError_t launch_attention(AttentionArgs a, hipStream_t s);
+hipError_t launch_attention_grad(AttentionArgs a, hipStream_t s);
+
+// ---------------------------------------------------------------------------
 // Grouped products.
 struct GroupPlan {
   int variant = 0;        // GroupVariant
@@ -137,7 +313,8 @@ struct GroupPlan {
   int64_t blocks = 0;     // workgroups
 };
 GroupPlan group_plan(const dbw_group_shape& p);
+// epilogue: nullptr, or that of a FORWARD product
 hipError_t launch_group(const dbw_group_shape& p, GroupPlan plan, const int32_t* offsets, const void* a,
-                        const void* b, void* out, float* workspace, hipStream_t s);
+                        const void* b, void* out, float* workspace, const dbw_linear_epilogue* epilogue, hipStream_t s);
 
 }  // namespace dbw
