@@ -201,7 +201,7 @@ dbw_status check_attention(const char* call, const dbw_attention_shape* p) {
   if (p->D > 128 || p->D % 8) return set_free_error(DBW_EUNSUPPORTED, "%s: D=%d is not a multiple of 8 up to 128", call, p->D);
   if (!(p->scale >= 1e-20 && p->scale <= 1e20)) return set_free_error(DBW_EINVAL, "%s: scale lies in [1e-20, 1e20]", call);
   // (a launch holds fewer than 2^32 threads)
-  if ((p->T / dbw::kAttentionRows + p->n) * p->heads >= (int64_t{1} << 23))
+  if ((p->T / dbw::kAttentionKeys + p->n) * p->heads >= (int64_t{1} << 23))
     return set_free_error(DBW_EUNSUPPORTED, "%s: 2^23 tiles or more", call);
   return DBW_OK;
 }

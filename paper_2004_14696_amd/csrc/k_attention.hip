@@ -1,7 +1,7 @@
 // Causal attention over packed sequences, and its gradients.
 //   k_attention       O and lse: a workgroup takes 128 queries of a head
 //   k_attention_dq    dQ, and delta = dO . O of each query: the same
-//   k_attention_dkv   dK and dV: a workgroup takes 128 keys of a head of keys
+//   k_attention_dkv   dK and dV: a workgroup takes 64 keys of a head of keys
 //
 // v_mfma_f32_32x32x16 takes, in lane l = 32 h + c, row c and terms 8 h .. 8 h +
 // 7 of each operand; its result r of a lane is row 8 (r / 4) + 4 h + r % 4 of
@@ -204,7 +204,8 @@ __device__ __forceinline__ lm_u32x4 terms(const f32x16& x, int u) {
 
 __device__ __forceinline__ int place(int r, int h) { return 8 * (r / 4) + 4 * h + r % 4; }
 
-constexpr int BM = kAttentionRows, BN = 64;
+constexpr int BM = 128, BN = 64;   // queries of a workgroup, keys of a stage
+constexpr int KEYS = kAttentionKeys, STEP = 128;          // for dK and dV: keys of a workgroup, queries of a stage
 
 // What a workgroup works on: rows first .. of a sequence [start, end) and a head.
 struct Work {
@@ -213,11 +214,11 @@ struct Work {
 };
 // Workgroups start in the order of their numbers: the last tiles of a sequence
 // have the most keys before them, and go first.
-__device__ __forceinline__ Work work(const AttentionArgs& a, int heads, bool reverse, int lane) {
+__device__ __forceinline__ Work work(const AttentionArgs& a, int heads, int rows, bool reverse, int lane) {
   const uint32_t slot = blockIdx.x / heads;
   Work w;
   w.head = static_cast<int>(blockIdx.x % heads);
-  w.rows = lm_chunk(a.offsets, a.n, a.T, BM, reverse ? a.slots - 1 - slot : slot, lane);
+  w.rows = lm_chunk(a.offsets, a.n, a.T, rows, reverse ? a.slots - 1 - slot : slot, lane);
   return w;
 }
 
@@ -227,7 +228,7 @@ __global__ __launch_bounds__(256, 2) void k_attention(AttentionArgs a) {
   __shared__ __align__(16) char lds[4 * R::BYTES];   // two stages of K and V
   const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
   const int c = lane % 32, h = lane / 32;
-  const Work w = work(a, a.heads, true, lane);
+  const Work w = work(a, a.heads, BM, true, lane);
   if (w.rows.empty()) return;
   const int len = w.rows.end - w.rows.start, q0 = w.rows.first - w.rows.start, qw = q0 + 32 * wave, qi = qw + c;
   const int kv_head = w.head / (a.heads / a.kv_heads);
@@ -324,7 +325,7 @@ __global__ __launch_bounds__(256, 2) void k_attention_dq(AttentionArgs a) {
   __shared__ __align__(16) char lds[4 * R::BYTES];   // two stages of K and V
   const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
   const int c = lane % 32, h = lane / 32;
-  const Work w = work(a, a.heads, true, lane);
+  const Work w = work(a, a.heads, BM, true, lane);
   if (w.rows.empty()) return;
   const int len = w.rows.end - w.rows.start, q0 = w.rows.first - w.rows.start, qw = q0 + 32 * wave, qi = qw + c;
   const int kv_head = w.head / (a.heads / a.kv_heads);
@@ -413,23 +414,37 @@ __global__ __launch_bounds__(256, 2) void k_attention_dq(AttentionArgs a) {
   write_rows<E, DP>(at(a.dQ, row, w.head), a.dQ.token, len - qw, a.D, lane, dq, a.scale);
 }
 
+// Eight waves: two groups of 32 keys, and each the four groups of 32 queries of
+// a stage, whose sums are joined at the end.
 template <typename E, int DP>
-__global__ __launch_bounds__(256, 1) void k_attention_dkv(AttentionArgs a) {
-  typedef Rows<DP, BN, 256> R;
-  constexpr int STAGE = 2 * R::BYTES + 4 * 256;      // Q, dO, and of each query: delta, lse (twice: every wave loads)
-  __shared__ __align__(16) char lds[2 * STAGE];
+__global__ __launch_bounds__(512, 2) void k_attention_dkv(AttentionArgs a) {
+  typedef Rows<DP, STEP, 512> R;
+  typedef Rows<DP, KEYS, 512> RV;
+  // with 128 values a head, registers hold the keys but not the values beside the sums
+  constexpr bool V_IN_LDS = DP == 128;
+  constexpr int STAGE = 2 * R::BYTES + 8 * 256;      // Q, dO, and of each query: delta, lse (twice: every wave loads)
+  constexpr int VALUES = DP / 32 * 2 * 16;           // sums of a lane
+  __shared__ __align__(16) char lds[2 * STAGE + (V_IN_LDS ? KEYS * DP * 2 : 0)];
+  static_assert(4 * VALUES * 256 <= 2 * STAGE, "the sums of half the waves go through LDS");
   const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
-  const int c = lane % 32, h = lane / 32;
-  const Work w = work(a, a.kv_heads, false, lane);
+  const int c = lane % 32, h = lane / 32, part = wave / 2;
+  const Work w = work(a, a.kv_heads, KEYS, false, lane);
   if (w.rows.empty()) return;
-  const int len = w.rows.end - w.rows.start, k0 = w.rows.first - w.rows.start, kw = k0 + 32 * wave, ki = kw + c;
+  const int len = w.rows.end - w.rows.start, k0 = w.rows.first - w.rows.start, kw = k0 + 32 * (wave % 2), ki = kw + c;
   const int share = a.heads / a.kv_heads;
   const float scale2 = a.scale * kLog2E;
-  const int64_t row = w.rows.first + 32 * wave;
+  const int64_t row = w.rows.first + 32 * (wave % 2);
 
-  lm_u32x4 k[DP / 16], v[DP / 16];
+  lm_u32x4 k[DP / 16], v[V_IN_LDS ? 1 : DP / 16];
   operand<DP>(at(a.K, row, w.head), a.K.token, len - kw, a.D, lane, k);
-  operand<DP>(at(a.V, row, w.head), a.V.token, len - kw, a.D, lane, v);
+  if constexpr (V_IN_LDS) {
+    uint32_t off[RV::CHUNKS];
+#pragma unroll
+    for (int i = 0; i < RV::CHUNKS; ++i) off[i] = RV::offset(a.V.token, KEYS, a.D, tid, i);
+    RV::load(at(a.V, w.rows.first, w.head), a.V.token, len - k0, a.D, lds + 2 * STAGE, wave, lane, off);
+  } else {
+    operand<DP>(at(a.V, row, w.head), a.V.token, len - kw, a.D, lane, v);
+  }
   f32x16 dk[DP / 32], dv[DP / 32];
 #pragma unroll
   for (int i = 0; i < DP / 32; ++i) dk[i] = dv[i] = zero16();
@@ -437,14 +452,13 @@ __global__ __launch_bounds__(256, 1) void k_attention_dkv(AttentionArgs a) {
   uint32_t off_q[R::CHUNKS], off_d[R::CHUNKS], pq[DP / 32];
 #pragma unroll
   for (int i = 0; i < R::CHUNKS; ++i) {
-    off_q[i] = R::offset(a.Q.token, BN, a.D, tid, i);
-    off_d[i] = R::offset(a.dO.token, BN, a.D, tid, i);
+    off_q[i] = R::offset(a.Q.token, STEP, a.D, tid, i);
+    off_d[i] = R::offset(a.dO.token, STEP, a.D, tid, i);
   }
-  R::columns(lds, lane, pq);
+  R::columns(lds + 32 * part * DP * 2, lane, pq);
   // tiles of queries from the workgroup's first key on, for each head in turn
-  const int first = k0 / BN * BN;
-  const int steps = (len - first + BN - 1) / BN, all = steps * share;
-  int head_of = 0, q_of = first;      // the next stage to load
+  const int steps = (len - k0 + STEP - 1) / STEP, all = steps * share;
+  int head_of = 0, q_of = k0;      // the next stage to load
   const auto issue = [&](int slot) {
     char* to = lds + slot * STAGE;
     const int head = w.head * share + head_of, left = len - q_of;
@@ -452,87 +466,114 @@ __global__ __launch_bounds__(256, 1) void k_attention_dkv(AttentionArgs a) {
     R::load(at(a.Q, from, head), a.Q.token, left, a.D, to, wave, lane, off_q);
     R::load(at(a.dO, from, head), a.dO.token, left, a.D, to + R::BYTES, wave, lane, off_d);
     typedef __attribute__((address_space(3))) void* P;
-    const float* x = a.delta + (wave % 2 * a.heads + head) * a.T + from;
+    const int i = wave % 2 * 64 + lane;
+    const float* x = a.delta + (wave / 2 % 2 * a.heads + head) * a.T + from;
     __builtin_amdgcn_raw_ptr_buffer_load_lds(make_rsrc(x, static_cast<uint32_t>(kMaxBufferBytes)),
                                              (P)(to + 2 * R::BYTES + wave * 256), 4,
-                                             lane < left ? static_cast<uint32_t>(lane * 4) : kOutOfRange, 0, 0, 0);
-    q_of += BN;
+                                             i < left ? static_cast<uint32_t>(i * 4) : kOutOfRange, 0, 0, 0);
+    q_of += STEP;
     if (q_of >= len) {
-      q_of = first;
+      q_of = k0;
       ++head_of;
     }
   };
   issue(0);
-  int q0 = first;
+  int q0 = k0;
   for (int i = 0, slot = 0; i < all; ++i, slot ^= 1) {
     wait_step<0>();
     if (i + 1 < all) issue(slot ^ 1);
+    const int q = q0 + 32 * part;
+    q0 += STEP;
+    if (q0 >= len) q0 = k0;
+    if (q + 31 < kw || q >= len || kw >= len) continue;
     const char* stage = lds + slot * STAGE;
     uint32_t p[DP / 32];
 #pragma unroll
     for (int j = 0; j < DP / 32; ++j) p[j] = pq[j] + slot * STAGE;
-    const auto part = [&](auto half) {
-      constexpr int t = decltype(half)::value;
-      const int q = q0 + 32 * t;
-      if (q + 31 < kw || q >= len || kw >= len) return;
-      f32x16 s = zero16(), ds = zero16();
+    f32x16 s = zero16(), ds = zero16();
 #pragma unroll
-      for (int kk = 0; kk < DP / 16; ++kk) {
-        s = mma(R::row(stage, 32 * t, kk, lane), k[kk], s, E{});
-        ds = mma(R::row(stage + R::BYTES, 32 * t, kk, lane), v[kk], ds, E{});
+    for (int kk = 0; kk < DP / 16; ++kk) {
+      s = mma(R::row(stage, 32 * part, kk, lane), k[kk], s, E{});
+      lm_u32x4 x;
+      if constexpr (V_IN_LDS) x = RV::row(lds + 2 * STAGE, 32 * (wave % 2), kk, lane);
+      else x = v[kk];
+      ds = mma(R::row(stage + R::BYTES, 32 * part, kk, lane), x, ds, E{});
+    }
+    const char* stats = stage + 2 * R::BYTES + (32 * part + 4 * h) * 4;
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const lm_f32x4 delta = *reinterpret_cast<const lm_f32x4*>(stats + 32 * g);
+      const lm_f32x4 lse2 = *reinterpret_cast<const lm_f32x4*>(stats + 512 + 32 * g);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int r = 4 * g + j;
+        s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], scale2, -lse2[j]));
+        ds[r] = s[r] * (ds[r] - delta[j]);
       }
-      const char* stats = stage + 2 * R::BYTES + (32 * t + 4 * h) * 4;
+    }
+    if (q < kw + 31 || q + 31 >= len) {
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const lm_f32x4 delta = *reinterpret_cast<const lm_f32x4*>(stats + 32 * g);
-        const lm_f32x4 lse2 = *reinterpret_cast<const lm_f32x4*>(stats + 256 + 32 * g);
+      for (int r = 0; r < 16; ++r)
+        if (ki > q + place(r, h) || q + place(r, h) >= len) s[r] = ds[r] = 0.f;
+    }
+    const auto product = [&](auto at_) {
+      constexpr int u = decltype(at_)::value;
+      lm_u32x4 f[DP / 32];
+      R::template column<16 * u * DP * 2>(p, f);
+      const lm_u32x4 y = terms<E>(ds, u);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int r = 4 * g + j;
-          s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], scale2, -lse2[j]));
-          ds[r] = s[r] * (ds[r] - delta[j]);
-        }
-      }
-      if (q < kw + 31 || q + 31 >= len) {
+      for (int j = 0; j < DP / 32; ++j) dk[j] = mma(f[j], y, dk[j], E{});
+      R::template column<16 * u * DP * 2 + R::BYTES>(p, f);
+      const lm_u32x4 x = terms<E>(s, u);
 #pragma unroll
-        for (int r = 0; r < 16; ++r)
-          if (ki > q + place(r, h) || q + place(r, h) >= len) s[r] = ds[r] = 0.f;
-      }
-      const auto product = [&](auto at_) {
-        constexpr int u = decltype(at_)::value;
-        lm_u32x4 f[DP / 32];
-        R::template column<(32 * t + 16 * u) * DP * 2>(p, f);
-        const lm_u32x4 y = terms<E>(ds, u);
-#pragma unroll
-        for (int j = 0; j < DP / 32; ++j) dk[j] = mma(f[j], y, dk[j], E{});
-        R::template column<(32 * t + 16 * u) * DP * 2 + R::BYTES>(p, f);
-        const lm_u32x4 x = terms<E>(s, u);
-#pragma unroll
-        for (int j = 0; j < DP / 32; ++j) dv[j] = mma(f[j], x, dv[j], E{});
-      };
-      product(std::integral_constant<int, 0>{});
-      product(std::integral_constant<int, 1>{});
+      for (int j = 0; j < DP / 32; ++j) dv[j] = mma(f[j], x, dv[j], E{});
     };
-    part(std::integral_constant<int, 0>{});
-    part(std::integral_constant<int, 1>{});
-    q0 += BN;
-    if (q0 >= len) q0 = first;
+    product(std::integral_constant<int, 0>{});
+    product(std::integral_constant<int, 1>{});
   }
-  if (kw >= len) return;
+  // the sums of waves 4 to 7 join those of 0 to 3, and then 2 and 3 those of 0 and 1
+#pragma unroll
+  for (int from = 4; from >= 2; from /= 2) {
+    wait_step<0>();
+    if (wave >= from && wave < 2 * from) {
+      float* to = reinterpret_cast<float*>(lds) + (wave - from) * VALUES * 64 + lane;
+#pragma unroll
+      for (int i = 0; i < DP / 32; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          to[(i * 32 + r) * 64] = dk[i][r];
+          to[(i * 32 + 16 + r) * 64] = dv[i][r];
+        }
+    }
+    wait_step<0>();
+    if (wave < from) {
+      const float* of = reinterpret_cast<const float*>(lds) + wave * VALUES * 64 + lane;
+#pragma unroll
+      for (int i = 0; i < DP / 32; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          dk[i][r] += of[(i * 32 + r) * 64];
+          dv[i][r] += of[(i * 32 + 16 + r) * 64];
+        }
+    }
+  }
+  if (wave >= 2 || kw >= len) return;
   write_rows<E, DP>(at(a.dK, row, w.head), a.dK.token, len - kw, a.D, lane, dk, a.scale);
   write_rows<E, DP>(at(a.dV, row, w.head), a.dV.token, len - kw, a.D, lane, dv, 1.f);
 }
 
-uint32_t slots_of(const AttentionArgs& a) { return static_cast<uint32_t>(a.T / BM + a.n); }
+uint32_t slots_of(const AttentionArgs& a, int rows) { return static_cast<uint32_t>(a.T / rows + a.n); }
 
 template <typename E, int DP>
-void launch_typed(const AttentionArgs& a, bool grad, hipStream_t s) {
+void launch_typed(AttentionArgs a, bool grad, hipStream_t s) {
+  a.slots = slots_of(a, BM);
   if (!grad) {
     k_attention<E, DP><<<a.slots * a.heads, 256, 0, s>>>(a);
     return;
   }
   k_attention_dq<E, DP><<<a.slots * a.heads, 256, 0, s>>>(a);
-  k_attention_dkv<E, DP><<<a.slots * a.kv_heads, 256, 0, s>>>(a);
+  a.slots = slots_of(a, KEYS);
+  k_attention_dkv<E, DP><<<a.slots * a.kv_heads, 512, 0, s>>>(a);
 }
 template <typename E>
 void launch_wide(const AttentionArgs& a, bool grad, hipStream_t s) {
@@ -542,7 +583,6 @@ void launch_wide(const AttentionArgs& a, bool grad, hipStream_t s) {
 }
 hipError_t launch(AttentionArgs a, bool grad, hipStream_t s) {
   if (a.T == 0) return hipSuccess;
-  a.slots = slots_of(a);
   if (a.dtype == DBW_BF16) launch_wide<__bf16>(a, grad, s);
   else launch_wide<_Float16>(a, grad, s);
   return hipGetLastError();

@@ -1,9 +1,12 @@
 // Layer norm with its gradients, and the gradient of an activation with that
 // of its bias.
 //   k_norm         Y = (X - mean) / sqrt(var + eps) gamma + beta
-//   k_norm_grad    dX, and each chunk's sums of dY H and dY
-//   k_linear_grad  dZ = dY act'(Z), and each chunk's sums of dZ
-//   k_chunk_sum    the weights' gradients of each group, from its chunks' sums
+//   k_norm_grad    dX, and sums of dY H and dY over pieces of the groups
+//   k_linear_grad  dZ = dY act'(Z), and sums of dZ over pieces
+//   k_piece_sum    the weights' gradients of each group, from its pieces' sums
+//
+// The rows of all groups are dealt out evenly, in parts; where a group ends
+// inside a part, its piece ends.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -12,6 +15,8 @@
 
 namespace dbw {
 namespace {
+
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // Sixteen bytes of a row.
 template <typename E>
@@ -23,16 +28,18 @@ struct Pack {
 };
 
 // The columns of pack number p of a row of d values.  A row's last pack is its
-// last N values: `skip` of them are the pack's before, which computes the same
-// for them; sums leave them out.  Rows of fewer than N values are one pack.
-template <int N>
+// last N values: the first of them may be the pack's before, which computes the
+// same for them; sums over a row leave them out.  Rows of fewer than N values are
+// one pack.  WHOLE: d is a multiple of N.
+template <int N, bool WHOLE = false>
 struct Place {
-  int base, skip, end;   // values [skip, end) are the pack's own
+  int base, end;   // `end` values from base on
+  uint32_t mask;   // those of them that are the pack's own
   __device__ __forceinline__ Place(int p, int d) {
     base = p * N;
-    skip = 0;
     end = base < d ? N : 0;
-    if (end && base + N > d) {
+    int skip = 0;
+    if (!WHOLE && end && base + N > d) {
       if (d >= N) {
         skip = base + N - d;
         base = d - N;
@@ -40,16 +47,22 @@ struct Place {
         end = d;
       }
     }
+    mask = (1u << end) - (1u << skip);
   }
-  __device__ __forceinline__ bool own(int j) const { return j >= skip && j < end; }
-  __device__ __forceinline__ bool whole() const { return skip == 0 && end == N; }
+  // 1 for values of the pack's own: a factor, which costs less than a branch
+  __device__ __forceinline__ float own(int j) const {
+    return WHOLE ? 1.f : __builtin_bit_cast(float, static_cast<uint32_t>(static_cast<int32_t>(mask << (31 - j)) >> 31) & 0x3f800000u);
+  }
+  __device__ __forceinline__ bool full() const { return WHOLE || end == N; }
 };
 
-template <typename E>
-__device__ __forceinline__ Pack<E> load(const E* row, const Place<Pack<E>::N>& p) {
+template <typename E, typename P>
+__device__ __forceinline__ Pack<E> load(const E* row, const P& p) {
   constexpr int N = Pack<E>::N;
   Pack<E> x;
-  if (p.end == N) {
+  x.v = lm_u32x4{0, 0, 0, 0};
+  if (p.end == 0) return x;
+  if (p.full()) {
     x.v = *reinterpret_cast<const lm_u32x4_any*>(row + p.base);
   } else {
     typename Pack<E>::V v;
@@ -60,15 +73,15 @@ __device__ __forceinline__ Pack<E> load(const E* row, const Place<Pack<E>::N>& p
   return x;
 }
 
-template <typename E>
-__device__ __forceinline__ void store(E* row, const Place<Pack<E>::N>& p, const float (&y)[Pack<E>::N]) {
+template <typename E, typename P>
+__device__ __forceinline__ void store(E* row, const P& p, const float (&y)[Pack<E>::N]) {
   constexpr int N = Pack<E>::N;
   typedef float F __attribute__((ext_vector_type(N)));
   F f;
 #pragma unroll
   for (int j = 0; j < N; ++j) f[j] = y[j];
   const typename Pack<E>::V v = __builtin_convertvector(f, typename Pack<E>::V);
-  if (p.end == N) {
+  if (p.full()) {
     *reinterpret_cast<lm_u32x4_any*>(row + p.base) = __builtin_bit_cast(lm_u32x4, v);
   } else {
 #pragma unroll
@@ -78,9 +91,9 @@ __device__ __forceinline__ void store(E* row, const Place<Pack<E>::N>& p, const 
 }
 
 // N fp32 values from (to) p.base of a vector of weights.
-template <int N>
-__device__ __forceinline__ void load_f32(const float* w, const Place<N>& p, float (&x)[N]) {
-  if (p.end == N) {
+template <int N, typename P>
+__device__ __forceinline__ void load_f32(const float* w, const P& p, float (&x)[N]) {
+  if (p.full()) {
 #pragma unroll
     for (int j = 0; j < N; j += 4) {
       const lm_f32x4 v = *reinterpret_cast<const lm_f32x4_any*>(w + p.base + j);
@@ -92,9 +105,9 @@ __device__ __forceinline__ void load_f32(const float* w, const Place<N>& p, floa
     for (int j = 0; j < N; ++j) x[j] = j < p.end ? w[p.base + j] : 0.f;
   }
 }
-template <int N>
-__device__ __forceinline__ void store_f32(float* w, const Place<N>& p, const float (&x)[N]) {
-  if (p.end == N) {
+template <int N, typename P>
+__device__ __forceinline__ void store_f32(float* w, const P& p, const float (&x)[N]) {
+  if (p.full()) {
 #pragma unroll
     for (int j = 0; j < N; j += 4)
       *reinterpret_cast<lm_f32x4_any*>(w + p.base + j) = lm_f32x4{x[j], x[j + 1], x[j + 2], x[j + 3]};
@@ -129,54 +142,53 @@ __device__ __forceinline__ void row_sum(float (&v)[K], float* lds, int& turn) {
   }
 }
 
-// Sums of f(j) over the pack's own values.
-template <int N, typename F>
-__device__ __forceinline__ void own_sum(const Place<N>& p, F f) {
-  if (p.whole()) {
-#pragma unroll
-    for (int j = 0; j < N; ++j) f(j);
-  } else {
-#pragma unroll
-    for (int j = 0; j < N; ++j)
-      if (p.own(j)) f(j);
-  }
-}
-
-// W waves to a row, PACKS packs a thread.
-template <typename E, int W, int PACKS>
+// W waves to a row, PACKS packs a thread; the next row is on its way while one
+// is computed.
+template <typename E, int W, int PACKS, bool WHOLE>
 __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_norm(NormArgs a) {
   constexpr int N = Pack<E>::N, TEAMS = W == 1 ? 4 : 1;
-  __shared__ float lds[2 * 2 * W];
+  typedef Place<N, WHOLE> P;
+  __shared__ float lds[2 * W];
   const int tid = W == 1 ? threadIdx.x % 64 : threadIdx.x;
-  const int64_t first = lm_offset(a.offsets, 0, a.T), end = lm_offset(a.offsets, a.n, a.T);
+  const int64_t end = lm_offset(a.offsets, a.n, a.T), step = static_cast<int64_t>(gridDim.x) * TEAMS;
+  int64_t t = lm_offset(a.offsets, 0, a.T) + static_cast<int64_t>(blockIdx.x) * TEAMS + (W == 1 ? threadIdx.x / 64 : 0);
   const float over_d = 1.f / a.d;
   int turn = 0;
-  for (int64_t t = first + static_cast<int64_t>(blockIdx.x) * TEAMS + (W == 1 ? threadIdx.x / 64 : 0); t < end;
-       t += static_cast<int64_t>(gridDim.x) * TEAMS) {
-    const E* row = static_cast<const E*>(a.X) + t * a.ld_X;
-    Pack<E> x[PACKS];
+  const auto row = [&](int64_t t, Pack<E>(&x)[PACKS]) {
+    const E* p = static_cast<const E*>(a.X) + t * a.ld_X;
+#pragma unroll
+    for (int i = 0; i < PACKS; ++i) x[i] = load<E>(p, P(tid + i * W * 64, a.d));
+  };
+  Pack<E> x[PACKS], next[PACKS];
+  if (t < end) row(t, x);
+  for (; t < end; t += step) {
+    if (t + step < end) row(t + step, next);
     float sum[1] = {0.f};
 #pragma unroll
     for (int i = 0; i < PACKS; ++i) {
-      const Place<N> p(tid + i * W * 64, a.d);
-      x[i] = load<E>(row, p);
-      own_sum(p, [&](int j) { sum[0] += x[i][j]; });
+      const P p(tid + i * W * 64, a.d);
+#pragma unroll
+      for (int j = 0; j < N; ++j) sum[0] = WHOLE ? sum[0] + x[i][j] : fmaf(x[i][j], p.own(j), sum[0]);
     }
     row_sum<W, 1>(sum, lds, turn);
     const float mean = sum[0] * over_d;
     float sq[1] = {0.f};
 #pragma unroll
-    for (int i = 0; i < PACKS; ++i)
-      own_sum(Place<N>(tid + i * W * 64, a.d), [&](int j) {
-        const float c = x[i][j] - mean;
+    for (int i = 0; i < PACKS; ++i) {
+      const P p(tid + i * W * 64, a.d);
+      if (p.end == 0) continue;
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        const float c = WHOLE ? x[i][j] - mean : (x[i][j] - mean) * p.own(j);
         sq[0] = fmaf(c, c, sq[0]);
-      });
+      }
+    }
     row_sum<W, 1>(sq, lds, turn);
     const float r = 1.f / sqrtf(fmaf(sq[0], over_d, a.eps));
     E* out = static_cast<E*>(a.out) + t * a.ld_out;
 #pragma unroll
     for (int i = 0; i < PACKS; ++i) {
-      const Place<N> p(tid + i * W * 64, a.d);
+      const P p(tid + i * W * 64, a.d);
       if (p.end == 0) continue;
       float g[N], b[N], y[N];
       load_f32<N>(a.gamma, p, g);
@@ -187,134 +199,185 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_norm(NormArgs a) {
       for (int j = 0; j < N; ++j) y[j] = fmaf((x[i][j] - mean) * r, g[j], b[j]);
       store<E>(out, p, y);
     }
+#pragma unroll
+    for (int i = 0; i < PACKS; ++i) x[i] = next[i];
   }
 }
 
-template <typename E, int W, int PACKS>
+// The rows of part number `part` of all rows, a.rows of them, group by group:
+// f(group, first, last) for each piece.  Piece and part make a slot of their
+// own for the piece's sums, part + group: from one piece to the next, the part
+// or the group goes up.
+template <typename F>
+__device__ __forceinline__ void pieces(const int32_t* offsets, int n, int64_t T, uint32_t rows, uint32_t part, F f) {
+  const int lane = threadIdx.x % 64;
+  const int64_t o0 = lm_offset(offsets, 0, T), end = lm_offset(offsets, n, T);
+  int64_t t = o0 + static_cast<int64_t>(part) * rows;
+  const int64_t last = std::min<int64_t>(end, t + rows);
+  if (t >= last) return;
+  // the last group that starts at t or before, 64 at once
+  int i = 0;
+  for (int count = n; count > 1;) {
+    const int step = (count + 63) / 64, at = lane * step;
+    const uint64_t below = __ballot(at < count && lm_offset(offsets, i + at, T) <= t);
+    const int k = below ? 63 - __builtin_clzll(below) : 0;
+    i += k * step;
+    count = std::min(step, count - k * step);
+  }
+  i = __builtin_amdgcn_readfirstlane(i);
+  for (; i < n && t < last; ++i) {
+    const int64_t to = std::min(last, lm_offset(offsets, i + 1, T));
+    if (to <= t) continue;
+    f(i, t, to);
+    t = to;
+  }
+}
+
+template <typename E, int W, int PACKS, bool WHOLE>
 __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_norm_grad(NormArgs a) {
   constexpr int N = Pack<E>::N, TEAMS = W == 1 ? 4 : 1;
+  typedef Place<N, WHOLE> P;
   __shared__ float lds[2 * 3 * W];
   const int tid = W == 1 ? threadIdx.x % 64 : threadIdx.x;
-  const uint32_t slot = blockIdx.x * TEAMS + (W == 1 ? threadIdx.x / 64 : 0);
-  if (slot >= a.slots) return;
-  const LmChunk chunk = lm_chunk(a.offsets, a.n, a.T, a.rows, slot, threadIdx.x % 64);
-  const int64_t last = std::min<int64_t>(chunk.end, static_cast<int64_t>(chunk.first) + a.rows);
-  if (chunk.empty()) return;
+  const uint32_t part = blockIdx.x * TEAMS + (W == 1 ? threadIdx.x / 64 : 0);
+  if (part >= a.parts_of_rows) return;
   const float over_d = 1.f / a.d;
   float dg[PACKS][N], db[PACKS][N];
-#pragma unroll
-  for (int i = 0; i < PACKS; ++i)
-#pragma unroll
-    for (int j = 0; j < N; ++j) dg[i][j] = db[i][j] = 0.f;
   int turn = 0;
-  for (int64_t t = chunk.first; t < last; ++t) {
-    const E* row = static_cast<const E*>(a.X) + t * a.ld_X;
-    const E* grad = static_cast<const E*>(a.dY) + t * a.ld_dY;
-    Pack<E> x[PACKS], dy[PACKS];
-    float sum[1] = {0.f};
+  const auto row = [&](int64_t t, Pack<E>(&x)[PACKS], Pack<E>(&dy)[PACKS]) {
+    const E* p = static_cast<const E*>(a.X) + t * a.ld_X;
+    const E* q = static_cast<const E*>(a.dY) + t * a.ld_dY;
 #pragma unroll
     for (int i = 0; i < PACKS; ++i) {
-      const Place<N> p(tid + i * W * 64, a.d);
-      x[i] = load<E>(row, p);
-      dy[i] = load<E>(grad, p);
-      own_sum(p, [&](int j) { sum[0] += x[i][j]; });
+      const P at(tid + i * W * 64, a.d);
+      x[i] = load<E>(p, at);
+      dy[i] = load<E>(q, at);
     }
-    row_sum<W, 1>(sum, lds, turn);
-    const float mean = sum[0] * over_d;
-    // sums of (x - mean)^2, dH and dH (x - mean)
-    float s[3] = {0.f, 0.f, 0.f};
+  };
+  pieces(a.offsets, a.n, a.T, a.rows, part, [&](int group, int64_t first, int64_t last) {
 #pragma unroll
-    for (int i = 0; i < PACKS; ++i) {
-      const Place<N> p(tid + i * W * 64, a.d);
-      float g[N];
-      load_f32<N>(a.gamma, p, g);
-      own_sum(p, [&](int j) {
-        const float c = x[i][j] - mean, h = dy[i][j] * g[j];
-        s[0] = fmaf(c, c, s[0]);
-        s[1] += h;
-        s[2] = fmaf(h, c, s[2]);
-      });
-    }
-    row_sum<W, 3>(s, lds, turn);
-    const float r = 1.f / sqrtf(fmaf(s[0], over_d, a.eps));
-    const float m1 = s[1] * over_d, m2 = s[2] * over_d * r;
-    E* out = static_cast<E*>(a.out) + t * a.ld_out;
+    for (int i = 0; i < PACKS; ++i)
 #pragma unroll
-    for (int i = 0; i < PACKS; ++i) {
-      const Place<N> p(tid + i * W * 64, a.d);
-      if (p.end == 0) continue;
-      float g[N], y[N];
-      load_f32<N>(a.gamma, p, g);
+      for (int j = 0; j < N; ++j) dg[i][j] = db[i][j] = 0.f;
+    Pack<E> x[PACKS], dy[PACKS], next_x[PACKS], next_dy[PACKS];
+    row(first, x, dy);
+    for (int64_t t = first; t < last; ++t) {
+      if (t + 1 < last) row(t + 1, next_x, next_dy);
+      float sum[1] = {0.f};
 #pragma unroll
-      for (int j = 0; j < N; ++j) {
-        const float h = (x[i][j] - mean) * r, d = dy[i][j];
-        dg[i][j] = fmaf(d, h, dg[i][j]);
-        db[i][j] += d;
-        y[j] = r * (fmaf(-h, m2, fmaf(d, g[j], -m1)));
+      for (int i = 0; i < PACKS; ++i) {
+        const P p(tid + i * W * 64, a.d);
+#pragma unroll
+        for (int j = 0; j < N; ++j) sum[0] = WHOLE ? sum[0] + x[i][j] : fmaf(x[i][j], p.own(j), sum[0]);
       }
-      store<E>(out, p, y);
-    }
-  }
-  const int64_t ld = (a.d + 3) / 4 * 4;
-  float* parts = a.parts + slot * ld;
+      row_sum<W, 1>(sum, lds, turn);
+      const float mean = sum[0] * over_d;
+      // sums of (x - mean)^2, dH and dH (x - mean)
+      float s[3] = {0.f, 0.f, 0.f};
 #pragma unroll
-  for (int i = 0; i < PACKS; ++i) {
-    const Place<N> p(tid + i * W * 64, a.d);
-    if (p.end == 0) continue;
-    store_f32<N>(parts, p, dg[i]);
-    if (a.dbeta) store_f32<N>(parts + a.slots * ld, p, db[i]);
-  }
+      for (int i = 0; i < PACKS; ++i) {
+        const P p(tid + i * W * 64, a.d);
+        if (p.end == 0) continue;
+        float g[N];
+        load_f32<N>(a.gamma, p, g);
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+          const float c = WHOLE ? x[i][j] - mean : (x[i][j] - mean) * p.own(j), h = dy[i][j] * g[j];
+          s[0] = fmaf(c, c, s[0]);
+          s[1] = WHOLE ? s[1] + h : fmaf(h, p.own(j), s[1]);
+          s[2] = fmaf(h, c, s[2]);
+        }
+      }
+      row_sum<W, 3>(s, lds, turn);
+      const float r = 1.f / sqrtf(fmaf(s[0], over_d, a.eps));
+      const float m1 = s[1] * over_d, m2 = s[2] * over_d * r;
+      E* out = static_cast<E*>(a.out) + t * a.ld_out;
+#pragma unroll
+      for (int i = 0; i < PACKS; ++i) {
+        const P p(tid + i * W * 64, a.d);
+        if (p.end == 0) continue;
+        float g[N], y[N];
+        load_f32<N>(a.gamma, p, g);
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+          const float h = (x[i][j] - mean) * r, d = dy[i][j];
+          dg[i][j] = fmaf(d, h, dg[i][j]);
+          db[i][j] += d;
+          y[j] = r * (fmaf(-h, m2, fmaf(d, g[j], -m1)));
+        }
+        store<E>(out, p, y);
+      }
+#pragma unroll
+      for (int i = 0; i < PACKS; ++i) {
+        x[i] = next_x[i];
+        dy[i] = next_dy[i];
+      }
+    }
+    const int64_t ld = (a.d + 3) / 4 * 4;
+    float* sums = a.parts + (part + group) * ld;
+#pragma unroll
+    for (int i = 0; i < PACKS; ++i) {
+      const P p(tid + i * W * 64, a.d);
+      if (p.end == 0) continue;
+      store_f32<N>(sums, p, dg[i]);
+      if (a.dbeta) store_f32<N>(sums + (static_cast<int64_t>(a.parts_of_rows) + a.n) * ld, p, db[i]);
+    }
+  });
 }
 
-// A thread takes one pack of columns and every 256 / lanes-th row of its chunk.
+// A thread takes one pack of columns and every 256 / lanes-th row, four of them
+// at once.
 template <typename E>
 __global__ __launch_bounds__(256) void k_linear_grad(LinearGradArgs a, int lanes) {
   constexpr int N = Pack<E>::N;
   __shared__ float lds[256][N + 1];
-  const uint32_t slot = blockIdx.x;
-  const LmChunk chunk = lm_chunk(a.offsets, a.n, a.T, a.rows, slot, threadIdx.x % 64);
-  if (chunk.empty()) return;
-  const int64_t last = std::min<int64_t>(chunk.end, static_cast<int64_t>(chunk.first) + a.rows);
-  const int step = 256 / lanes;
-  const Place<N> p(static_cast<int>(blockIdx.y) * lanes + static_cast<int>(threadIdx.x) % lanes, a.C);
-  float sum[N];
+  const int step = 256 / lanes, tid = threadIdx.x;
+  const Place<N> p(static_cast<int>(blockIdx.y) * lanes + tid % lanes, a.C);
+  const E* dY = static_cast<const E*>(a.dY);
+  const E* Z = static_cast<const E*>(a.Z);
+  E* dZ = static_cast<E*>(a.dZ);
+  pieces(a.offsets, a.n, a.T, a.rows, blockIdx.x, [&](int group, int64_t first, int64_t last) {
+    float sum[N];
 #pragma unroll
-  for (int j = 0; j < N; ++j) sum[j] = 0.f;
-  if (p.end)
-    for (int64_t t = chunk.first + static_cast<int>(threadIdx.x) / lanes; t < last; t += step) {
-      const Pack<E> dy = load<E>(static_cast<const E*>(a.dY) + t * a.ld_dY, p);
-      float y[N];
+    for (int j = 0; j < N; ++j) sum[j] = 0.f;
+    if (p.end)
+      for (int64_t t = first + tid / lanes; t < last; t += 4 * step) {
+        Pack<E> dy[4], z[4];
 #pragma unroll
-      for (int j = 0; j < N; ++j) y[j] = dy[j];
-      if (a.Z) {
-        const Pack<E> z = load<E>(static_cast<const E*>(a.Z) + t * a.ld_Z, p);
+        for (int k = 0; k < 4; ++k)
+          if (t + k * step < last) {
+            dy[k] = load<E>(dY + (t + k * step) * a.ld_dY, p);
+            if (Z) z[k] = load<E>(Z + (t + k * step) * a.ld_Z, p);
+          }
 #pragma unroll
-        for (int j = 0; j < N; ++j) y[j] *= lm_act_slope(z[j], a.act);
+        for (int k = 0; k < 4; ++k)
+          if (t + k * step < last) {
+            float y[N];
+#pragma unroll
+            for (int j = 0; j < N; ++j) y[j] = Z ? dy[k][j] * lm_act_slope(z[k][j], a.act) : dy[k][j];
+            if (dZ) store<E>(dZ + (t + k * step) * a.ld_dZ, p, y);
+#pragma unroll
+            for (int j = 0; j < N; ++j) sum[j] += y[j];
+          }
       }
-      if (a.dZ) store<E>(static_cast<E*>(a.dZ) + t * a.ld_dZ, p, y);
+    if (!a.dbias) return;
+    for (int s = 128; s >= lanes; s /= 2) {
+      if (tid >= s && tid < 2 * s)
 #pragma unroll
-      for (int j = 0; j < N; ++j) sum[j] += y[j];
+        for (int j = 0; j < N; ++j) lds[tid][j] = sum[j];
+      __syncthreads();
+      if (tid < s)
+#pragma unroll
+        for (int j = 0; j < N; ++j) sum[j] += lds[tid + s][j];
     }
-  if (!a.dbias) return;
-  for (int s = 128; s >= lanes; s /= 2) {
-    const int tid = threadIdx.x;
-    if (tid >= s && tid < 2 * s)
-#pragma unroll
-      for (int j = 0; j < N; ++j) lds[tid][j] = sum[j];
+    if (tid < lanes && p.end) store_f32<N>(a.parts + (blockIdx.x + group) * ((a.C + 3) / 4 * int64_t{4}), p, sum);
     __syncthreads();
-    if (tid < s)
-#pragma unroll
-      for (int j = 0; j < N; ++j) sum[j] += lds[tid + s][j];
-  }
-  if (static_cast<int>(threadIdx.x) < lanes && p.end) {
-    const int64_t ld = (a.C + 3) / 4 * 4;
-    store_f32<N>(a.parts + slot * ld, p, sum);
-  }
+  });
 }
 
-// Sums of a group's chunks: 16 threads for four columns, each takes every 16th
-// chunk.
-struct ChunkSum {
+// Sums over the pieces of a group: 16 threads for four columns, each takes
+// every 16th piece.
+struct PieceSum {
   int n, d;
   int64_t T;
   const int32_t* offsets;
@@ -323,16 +386,18 @@ struct ChunkSum {
   float* out[2];
   int64_t ld_out[2];
 };
-__global__ __launch_bounds__(256) void k_chunk_sum(ChunkSum a) {
+__global__ __launch_bounds__(256) void k_piece_sum(PieceSum a) {
   __shared__ lm_f32x4 lds[16][17];
   const int which = blockIdx.z, q = threadIdx.x % 16, part = threadIdx.x / 16;
-  const int64_t ld = (a.d + 3) / 4 * 4;
-  const uint32_t o0 = static_cast<uint32_t>(lm_offset(a.offsets, 0, a.T));
+  const int64_t ld = (a.d + 3) / 4 * 4, o0 = lm_offset(a.offsets, 0, a.T);
   for (int i = blockIdx.y; i < a.n; i += gridDim.y) {
     const int64_t first = lm_offset(a.offsets, i, a.T), end = lm_offset(a.offsets, i + 1, a.T);
-    const uint32_t from = std::min(lm_first_slot(a.offsets, i, a.T, o0, a.rows), a.slots);
-    const uint32_t count =
-        end > first ? std::min(static_cast<uint32_t>((end - first + a.rows - 1) / a.rows), a.slots - from) : 0;
+    uint32_t from = 0, count = 0;
+    if (end > first && first >= o0) {
+      const uint32_t p0 = static_cast<uint32_t>((first - o0) / a.rows), p1 = static_cast<uint32_t>((end - 1 - o0) / a.rows);
+      from = std::min(p0 + i, a.slots);
+      count = std::min(p1 - p0 + 1, a.slots - from);
+    }
     const int c = (static_cast<int>(blockIdx.x) * 16 + q) * 4;
     lm_f32x4 x = {0.f, 0.f, 0.f, 0.f};
     if (c < a.d) {
@@ -354,16 +419,11 @@ __global__ __launch_bounds__(256) void k_chunk_sum(ChunkSum a) {
   }
 }
 
-int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
-
 int norm_waves(int d) { return d <= 1024 ? 1 : d <= 4096 ? 4 : 16; }
 
-uint32_t norm_rows(int64_t T, int d) {
-  const int w = norm_waves(d);
-  const int64_t teams = w == 1 ? 4096 : w == 4 ? 1024 : 512;
-  // (a launch holds fewer than 2^32 threads)
-  return static_cast<uint32_t>(std::max({std::min<int64_t>(64, T / teams), int64_t{8}, T >> 21}));
-}
+// Rows of a part: as many parts as run at once (two workgroups a CU, or 2048
+// waves), and each with four rows at least for every sum that it leaves.
+uint32_t norm_rows(int64_t T, int d) { return static_cast<uint32_t>(std::max<int64_t>(4, ceil_div(T, norm_waves(d) == 1 ? 2048 : 512))); }
 
 int linear_lanes(int packs) {
   int lanes = 64;
@@ -373,25 +433,31 @@ int linear_lanes(int packs) {
 
 uint32_t linear_rows(int64_t T, int C) {
   const int64_t tiles = ceil_div(C, 512);
-  return static_cast<uint32_t>(std::min<int64_t>(256, std::max<int64_t>(16, T * tiles / 1024)));
+  return static_cast<uint32_t>(std::max<int64_t>(16, ceil_div(T * tiles, 1024)));
 }
 
-uint32_t slots_of(int n, int64_t T, uint32_t rows) { return static_cast<uint32_t>(T / rows + n); }
+uint32_t parts_of(int64_t T, uint32_t rows) { return static_cast<uint32_t>(ceil_div(T, rows)); }
+uint32_t slots_of(int n, int64_t T, uint32_t rows) { return parts_of(T, rows) + n; }
 
-void launch_chunk_sum(const ChunkSum& c, hipStream_t s) {
+void launch_piece_sum(const PieceSum& c, hipStream_t s) {
   const dim3 grid(static_cast<uint32_t>(ceil_div(c.d, 64)), std::min(c.n, 1024), c.out[1] ? 2 : 1);
-  k_chunk_sum<<<grid, 256, 0, s>>>(c);
+  k_piece_sum<<<grid, 256, 0, s>>>(c);
 }
 
-template <typename E, int W, int PACKS>
-void norm_variant(const NormArgs& a, bool grad, hipStream_t s) {
+template <typename E, int W, int PACKS, bool WHOLE>
+void norm_launch(const NormArgs& a, bool grad, hipStream_t s) {
   constexpr int TEAMS = W == 1 ? 4 : 1, THREADS = W == 1 ? 256 : 64 * W;
   if (grad) {
-    k_norm_grad<E, W, PACKS><<<static_cast<uint32_t>(ceil_div(a.slots, TEAMS)), THREADS, 0, s>>>(a);
+    k_norm_grad<E, W, PACKS, WHOLE><<<static_cast<uint32_t>(ceil_div(a.parts_of_rows, TEAMS)), THREADS, 0, s>>>(a);
   } else {
-    const int64_t most = W == 16 ? 1024 : 4096;
-    k_norm<E, W, PACKS><<<static_cast<uint32_t>(std::min(most, ceil_div(a.T, TEAMS))), THREADS, 0, s>>>(a);
+    const int64_t most = W == 16 ? 512 : 2048;
+    k_norm<E, W, PACKS, WHOLE><<<static_cast<uint32_t>(std::min(most, ceil_div(a.T, TEAMS))), THREADS, 0, s>>>(a);
   }
+}
+template <typename E, int W, int PACKS>
+void norm_variant(const NormArgs& a, bool grad, hipStream_t s) {
+  if (a.d % Pack<E>::N == 0) norm_launch<E, W, PACKS, true>(a, grad, s);
+  else norm_launch<E, W, PACKS, false>(a, grad, s);
 }
 
 template <typename E>
@@ -431,9 +497,9 @@ hipError_t launch_layer_norm(const NormArgs& a, hipStream_t s) {
 
 hipError_t launch_layer_norm_grad(NormArgs a, hipStream_t s) {
   a.rows = norm_rows(a.T, a.d);
-  a.slots = slots_of(a.n, a.T, a.rows);
+  a.parts_of_rows = parts_of(a.T, a.rows);
   if (a.T > 0) norm(a, true, s);
-  launch_chunk_sum(ChunkSum{a.n, a.d, a.T, a.offsets, a.rows, a.slots, a.parts, {a.dgamma, a.dbeta},
+  launch_piece_sum(PieceSum{a.n, a.d, a.T, a.offsets, a.rows, slots_of(a.n, a.T, a.rows), a.parts, {a.dgamma, a.dbeta},
                             {a.ld_dgamma, a.ld_dbeta}}, s);
   return hipGetLastError();
 }
@@ -444,17 +510,16 @@ int64_t linear_grad_workspace(int n, int64_t T, int C) {
 
 hipError_t launch_linear_grad(LinearGradArgs a, hipStream_t s) {
   a.rows = linear_rows(a.T, a.C);
-  a.slots = slots_of(a.n, a.T, a.rows);
   if (a.T > 0) {
     const int packs = static_cast<int>(ceil_div(a.C, a.dtype == DBW_F32 ? 4 : 8));
     const int lanes = linear_lanes(packs);
-    const dim3 grid(a.slots, static_cast<uint32_t>(ceil_div(packs, lanes)));
+    const dim3 grid(parts_of(a.T, a.rows), static_cast<uint32_t>(ceil_div(packs, lanes)));
     if (a.dtype == DBW_F32) k_linear_grad<float><<<grid, 256, 0, s>>>(a, lanes);
     else if (a.dtype == DBW_BF16) k_linear_grad<__bf16><<<grid, 256, 0, s>>>(a, lanes);
     else k_linear_grad<_Float16><<<grid, 256, 0, s>>>(a, lanes);
   }
   if (a.dbias)
-    launch_chunk_sum(ChunkSum{a.n, a.C, a.T, a.offsets, a.rows, a.slots, a.parts, {a.dbias, nullptr}, {a.ld_dbias, 0}}, s);
+    launch_piece_sum(PieceSum{a.n, a.C, a.T, a.offsets, a.rows, slots_of(a.n, a.T, a.rows), a.parts, {a.dbias, nullptr}, {a.ld_dbias, 0}}, s);
   return hipGetLastError();
 }
 

@@ -220,8 +220,8 @@ struct NormArgs {
   int64_t ld_dgamma;
   float* dbeta;         // nullable
   int64_t ld_dbeta;
-  float* parts;         // workspace [2][slots][d]
-  uint32_t rows, slots; // rows of a chunk, chunks (set by the launch)
+  float* parts;         // workspace [2][parts_of_rows + n][d]: sums over pieces of the groups
+  uint32_t rows, parts_of_rows;   // rows of a part (set by the launch)
 };
 constexpr int kNormMost = 16384;
 int64_t norm_workspace(int n, int64_t T, int d);
@@ -241,8 +241,8 @@ struct LinearGradArgs {
   int64_t ld_dZ;
   float* dbias;         // nullable
   int64_t ld_dbias;
-  float* parts;         // workspace [slots][C]
-  uint32_t rows, slots;
+  float* parts;         // workspace [parts of the rows + n][C]
+  uint32_t rows;
 };
 int64_t linear_grad_workspace(int n, int64_t T, int C);
 hipError_t launch_linear_grad(LinearGradArgs a, hipStream_t s);
@@ -297,7 +297,7 @@ struct AttentionArgs {
   float* delta;         // workspace [2][heads][T]: dO . O, and lse log2(e)
   uint32_t slots;       // tiles of a head's queries or keys (set by the launch)
 };
-constexpr int kAttentionRows = 128;   // queries, or keys, of a workgroup
+constexpr int kAttentionKeys = 64;   // the fewest rows of a workgroup (512 threads)
 hipError_t launch_attention(AttentionArgs a, hipStream_t s);
 hipError_t launch_attention_grad(AttentionArgs a, hipStream_t s);
 
