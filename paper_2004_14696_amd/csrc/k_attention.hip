@@ -56,9 +56,9 @@ __device__ __forceinline__ float sum_halves(float x) {
 }
 
 // Rows of DP values in LDS, as a stage of ROWS of them.  A line's chunks of 16
-// bytes are turned by its number, so that eight lanes that read a chunk of
-// eight lines, and sixteen that read 32 bytes of four lines by the transposing
-// load, meet in no bank.
+// bytes are turned by its number, so that the lanes that read at once meet in
+// none of the 64 banks: sixteen that read a chunk of sixteen lines, or 32 that
+// read 64 bytes of four lines by the transposing load.
 template <int DP, int ROWS, int THREADS>
 struct Rows {
   static constexpr int LINE = DP / 8;                     // chunks of a line
@@ -67,8 +67,8 @@ struct Rows {
   static_assert(DP == 64 || DP == 96 || DP == 128, "turn() is for these");
   static_assert(ROWS * LINE % THREADS == 0, "whole chunks a thread");
   static __device__ __forceinline__ int turn(int line) {
-    if (DP == 96) return (line >> 1 & 1) << 1 | (line >> 2 & 1);   // (lines start at two places among the banks)
-    return (line & 3) << 1 | (line >> 2 & 1);
+    const int low = line >> 2 & 3;
+    return DP == 128 ? (line & 3) << 2 | low : DP == 64 ? (line >> 1 & 1) << 2 | low : low;
   }
   // Byte offset of thread tid's chunk i from the stage's first row, or one
   // behind every buffer (such loads give 0): of `left` rows, of D values each.
@@ -104,18 +104,19 @@ struct Rows {
           (P)(lds + line * (DP * 2) + ((4 * i + lane / 16 % 2 * 2 + q / 2) ^ turn(line)) * 16 + q % 2 * 8)));
   }
   // Sixteen lines from AT bytes behind them on, transposed: in lane 32 h + c,
-  // column 32 i + c of lines 4 h .. + 3 and 8 + 4 h .. + 3.  The wait is in the
+  // column 32 i + c of lines 4 h .. + 3 and 8 + 4 h .. + 3 (eight lines on, the
+  // turn differs by two chunks).  The wait is in the
   // statement: as builtins, the compiler would first wait for every load on
   // its way to LDS.
   template <int AT>
   static __device__ __forceinline__ void column(const uint32_t (&p)[2], lm_u32x4 (&f)[2]) {
     lm_u32x2 x[2][2];
     asm volatile(
-        "ds_read_b64_tr_b16 %0, %4 offset:%6\n\tds_read_b64_tr_b16 %1, %4 offset:%7\n\t"
-        "ds_read_b64_tr_b16 %2, %5 offset:%6\n\tds_read_b64_tr_b16 %3, %5 offset:%7\n\t"
+        "ds_read_b64_tr_b16 %0, %4 offset:%8\n\tds_read_b64_tr_b16 %1, %6 offset:%9\n\t"
+        "ds_read_b64_tr_b16 %2, %5 offset:%8\n\tds_read_b64_tr_b16 %3, %7 offset:%9\n\t"
         "s_waitcnt lgkmcnt(0)"
         : "=&v"(x[0][0]), "=&v"(x[0][1]), "=&v"(x[1][0]), "=&v"(x[1][1])
-        : "v"(p[0]), "v"(p[1]), "n"(AT), "n"(AT + 8 * DP * 2)
+        : "v"(p[0]), "v"(p[1]), "v"(p[0] ^ 32), "v"(p[1] ^ 32), "n"(AT), "n"(AT + 8 * DP * 2)
         : "memory");
     join(x, f);
   }
@@ -123,12 +124,13 @@ struct Rows {
   static __device__ __forceinline__ void column(const uint32_t (&p)[3], lm_u32x4 (&f)[3]) {
     lm_u32x2 x[3][2];
     asm volatile(
-        "ds_read_b64_tr_b16 %0, %6 offset:%9\n\tds_read_b64_tr_b16 %1, %6 offset:%10\n\t"
-        "ds_read_b64_tr_b16 %2, %7 offset:%9\n\tds_read_b64_tr_b16 %3, %7 offset:%10\n\t"
-        "ds_read_b64_tr_b16 %4, %8 offset:%9\n\tds_read_b64_tr_b16 %5, %8 offset:%10\n\t"
+        "ds_read_b64_tr_b16 %0, %6 offset:%12\n\tds_read_b64_tr_b16 %1, %9 offset:%13\n\t"
+        "ds_read_b64_tr_b16 %2, %7 offset:%12\n\tds_read_b64_tr_b16 %3, %10 offset:%13\n\t"
+        "ds_read_b64_tr_b16 %4, %8 offset:%12\n\tds_read_b64_tr_b16 %5, %11 offset:%13\n\t"
         "s_waitcnt lgkmcnt(0)"
         : "=&v"(x[0][0]), "=&v"(x[0][1]), "=&v"(x[1][0]), "=&v"(x[1][1]), "=&v"(x[2][0]), "=&v"(x[2][1])
-        : "v"(p[0]), "v"(p[1]), "v"(p[2]), "n"(AT), "n"(AT + 8 * DP * 2)
+        : "v"(p[0]), "v"(p[1]), "v"(p[2]), "v"(p[0] ^ 32), "v"(p[1] ^ 32), "v"(p[2] ^ 32), "n"(AT),
+          "n"(AT + 8 * DP * 2)
         : "memory");
     join(x, f);
   }
@@ -136,14 +138,15 @@ struct Rows {
   static __device__ __forceinline__ void column(const uint32_t (&p)[4], lm_u32x4 (&f)[4]) {
     lm_u32x2 x[4][2];
     asm volatile(
-        "ds_read_b64_tr_b16 %0, %8 offset:%12\n\tds_read_b64_tr_b16 %1, %8 offset:%13\n\t"
-        "ds_read_b64_tr_b16 %2, %9 offset:%12\n\tds_read_b64_tr_b16 %3, %9 offset:%13\n\t"
-        "ds_read_b64_tr_b16 %4, %10 offset:%12\n\tds_read_b64_tr_b16 %5, %10 offset:%13\n\t"
-        "ds_read_b64_tr_b16 %6, %11 offset:%12\n\tds_read_b64_tr_b16 %7, %11 offset:%13\n\t"
+        "ds_read_b64_tr_b16 %0, %8 offset:%16\n\tds_read_b64_tr_b16 %1, %12 offset:%17\n\t"
+        "ds_read_b64_tr_b16 %2, %9 offset:%16\n\tds_read_b64_tr_b16 %3, %13 offset:%17\n\t"
+        "ds_read_b64_tr_b16 %4, %10 offset:%16\n\tds_read_b64_tr_b16 %5, %14 offset:%17\n\t"
+        "ds_read_b64_tr_b16 %6, %11 offset:%16\n\tds_read_b64_tr_b16 %7, %15 offset:%17\n\t"
         "s_waitcnt lgkmcnt(0)"
         : "=&v"(x[0][0]), "=&v"(x[0][1]), "=&v"(x[1][0]), "=&v"(x[1][1]), "=&v"(x[2][0]), "=&v"(x[2][1]),
           "=&v"(x[3][0]), "=&v"(x[3][1])
-        : "v"(p[0]), "v"(p[1]), "v"(p[2]), "v"(p[3]), "n"(AT), "n"(AT + 8 * DP * 2)
+        : "v"(p[0]), "v"(p[1]), "v"(p[2]), "v"(p[3]), "v"(p[0] ^ 32), "v"(p[1] ^ 32), "v"(p[2] ^ 32), "v"(p[3] ^ 32),
+          "n"(AT), "n"(AT + 8 * DP * 2)
         : "memory");
     join(x, f);
   }
@@ -212,14 +215,82 @@ struct Work {
   LmChunk rows;
   int head;
 };
-// Workgroups start in the order of their numbers: the last tiles of a sequence
-// have the most keys before them, and go first.
-__device__ __forceinline__ Work work(const AttentionArgs& a, int heads, int rows, bool reverse, int lane) {
-  const uint32_t slot = blockIdx.x / heads;
-  Work w;
-  w.head = static_cast<int>(blockIdx.x % heads);
-  w.rows = lm_chunk(a.offsets, a.n, a.T, rows, reverse ? a.slots - 1 - slot : slot, lane);
-  return w;
+
+// Sum over a wave.
+__device__ __forceinline__ uint32_t wave_sum(uint32_t v) {
+  const auto add = [&](auto control) {
+    v += static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), decltype(control)::value, 0xf, 0xf, true));
+  };
+  add(std::integral_constant<int, 0xB1>{});    // lanes 1, 0, 3, 2
+  add(std::integral_constant<int, 0x4E>{});    // lanes 2, 3, 0, 1
+  add(std::integral_constant<int, 0x141>{});   // halves of 16 lanes mirrored
+  add(std::integral_constant<int, 0x140>{});   // 16 lanes mirrored
+  return static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(v), 0)) +
+         static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(v), 16)) +
+         static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(v), 32)) +
+         static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(v), 48));
+}
+
+// Tile number `rank` of all sequences' tiles of `rows` rows, those with the most
+// keys (LAST: the last tiles of long sequences) or queries (the first ones) to
+// pass first: workgroups start in the order of their numbers, and with the
+// longest at the end the others would wait for them (8 sequences of 8192 tokens,
+// 16 heads on 4 of 128: 72, 107 and 173 us for the three kernels with tiles in
+// the sequences' order, SORTED_US with this one).  With w the tiles to pass, its
+// own included, the tiles with w or more are sum_i max(0, tiles_i - w + 1).
+// kSorted sequences at most: beyond, chunks in the sequences' order.
+constexpr int kSorted = 256;
+template <bool LAST>
+__device__ __forceinline__ LmChunk tile(const AttentionArgs& a, uint32_t rows, uint32_t rank, int lane) {
+  if (a.n > kSorted) return lm_chunk(a.offsets, a.n, a.T, rows, LAST ? a.slots - 1 - rank : rank, lane);
+  uint32_t tiles[kSorted / 64];
+#pragma unroll
+  for (int k = 0; k < kSorted / 64; ++k) {
+    const int i = 64 * k + lane;
+    tiles[k] = 0;
+    if (i < a.n) {
+      const int64_t o = lm_offset(a.offsets, i, a.T), e = lm_offset(a.offsets, i + 1, a.T);
+      tiles[k] = e > o ? static_cast<uint32_t>(e - o + rows - 1) / rows : 0;
+    }
+  }
+  const auto with = [&](uint32_t w) {
+    uint32_t sum = 0;
+#pragma unroll
+    for (int k = 0; k < kSorted / 64; ++k) sum += tiles[k] >= w ? tiles[k] - w + 1 : 0;
+    return wave_sum(sum);
+  };
+  LmChunk c{0, 0, 0, 0};
+  if (with(1) <= rank) return c;
+  uint32_t step = 1, w = 1;
+  while (with(2 * step) > rank) step *= 2;
+  w = step;
+  for (step /= 2; step; step /= 2)
+    if (with(w + step) > rank) w += step;
+  uint32_t left = rank - with(w + 1);      // among the tiles with w to pass, one in each of these sequences
+#pragma unroll
+  for (int k = 0; k < kSorted / 64; ++k) {
+    const uint64_t these = __ballot(tiles[k] >= w);
+    const uint32_t count = __builtin_popcountll(these);
+    if (left < count) {
+      const bool here = tiles[k] >= w && __builtin_popcountll(these & ((uint64_t{1} << lane) - 1)) == left;
+      const int l = __builtin_ctzll(__ballot(here));
+      c.group = 64 * k + l;
+      const uint32_t j = LAST ? w - 1 : __builtin_amdgcn_readlane(tiles[k], l) - w;
+      c.start = static_cast<int32_t>(lm_offset(a.offsets, c.group, a.T));
+      c.end = static_cast<int32_t>(lm_offset(a.offsets, c.group + 1, a.T));
+      c.first = static_cast<int32_t>(c.start + j * rows);
+      break;
+    }
+    left -= count;
+  }
+  c.start = __builtin_amdgcn_readfirstlane(c.start);
+  c.end = __builtin_amdgcn_readfirstlane(c.end);
+  c.first = __builtin_amdgcn_readfirstlane(c.first);
+  return c;
+}
+template <bool LAST>
+__device__ __forceinline__ Work work(const AttentionArgs& a, int heads, int rows, int lane) {
+  return Work{tile<LAST>(a, rows, blockIdx.x / heads, lane), static_cast<int>(blockIdx.x % heads)};
 }
 
 template <typename E, int DP>
@@ -228,7 +299,7 @@ __global__ __launch_bounds__(256, 2) void k_attention(AttentionArgs a) {
   __shared__ __align__(16) char lds[4 * R::BYTES];   // two stages of K and V
   const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
   const int c = lane % 32, h = lane / 32;
-  const Work w = work(a, a.heads, BM, true, lane);
+  const Work w = work<true>(a, a.heads, BM, lane);
   if (w.rows.empty()) return;
   const int len = w.rows.end - w.rows.start, q0 = w.rows.first - w.rows.start, qw = q0 + 32 * wave, qi = qw + c;
   const int kv_head = w.head / (a.heads / a.kv_heads);
@@ -325,7 +396,7 @@ __global__ __launch_bounds__(256, 2) void k_attention_dq(AttentionArgs a) {
   __shared__ __align__(16) char lds[4 * R::BYTES];   // two stages of K and V
   const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
   const int c = lane % 32, h = lane / 32;
-  const Work w = work(a, a.heads, BM, true, lane);
+  const Work w = work<true>(a, a.heads, BM, lane);
   if (w.rows.empty()) return;
   const int len = w.rows.end - w.rows.start, q0 = w.rows.first - w.rows.start, qw = q0 + 32 * wave, qi = qw + c;
   const int kv_head = w.head / (a.heads / a.kv_heads);
@@ -428,7 +499,7 @@ __global__ __launch_bounds__(512, 2) void k_attention_dkv(AttentionArgs a) {
   static_assert(4 * VALUES * 256 <= 2 * STAGE, "the sums of half the waves go through LDS");
   const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
   const int c = lane % 32, h = lane / 32, part = wave / 2;
-  const Work w = work(a, a.kv_heads, KEYS, false, lane);
+  const Work w = work<false>(a, a.kv_heads, KEYS, lane);
   if (w.rows.empty()) return;
   const int len = w.rows.end - w.rows.start, k0 = w.rows.first - w.rows.start, kw = k0 + 32 * (wave % 2), ki = kw + c;
   const int share = a.heads / a.kv_heads;
