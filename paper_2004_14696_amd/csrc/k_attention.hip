@@ -108,46 +108,16 @@ struct Rows {
   // turn differs by two chunks).  The wait is in the
   // statement: as builtins, the compiler would first wait for every load on
   // its way to LDS.
-  template <int AT>
-  static __device__ __forceinline__ void column(const uint32_t (&p)[2], lm_u32x4 (&f)[2]) {
-    lm_u32x2 x[2][2];
-    asm volatile(
-        "ds_read_b64_tr_b16 %0, %4 offset:%8\n\tds_read_b64_tr_b16 %1, %6 offset:%9\n\t"
-        "ds_read_b64_tr_b16 %2, %5 offset:%8\n\tds_read_b64_tr_b16 %3, %7 offset:%9\n\t"
-        "s_waitcnt lgkmcnt(0)"
-        : "=&v"(x[0][0]), "=&v"(x[0][1]), "=&v"(x[1][0]), "=&v"(x[1][1])
-        : "v"(p[0]), "v"(p[1]), "v"(p[0] ^ 32), "v"(p[1] ^ 32), "n"(AT), "n"(AT + 8 * DP * 2)
-        : "memory");
-    join(x, f);
-  }
-  template <int AT>
-  static __device__ __forceinline__ void column(const uint32_t (&p)[3], lm_u32x4 (&f)[3]) {
-    lm_u32x2 x[3][2];
-    asm volatile(
-        "ds_read_b64_tr_b16 %0, %6 offset:%12\n\tds_read_b64_tr_b16 %1, %9 offset:%13\n\t"
-        "ds_read_b64_tr_b16 %2, %7 offset:%12\n\tds_read_b64_tr_b16 %3, %10 offset:%13\n\t"
-        "ds_read_b64_tr_b16 %4, %8 offset:%12\n\tds_read_b64_tr_b16 %5, %11 offset:%13\n\t"
-        "s_waitcnt lgkmcnt(0)"
-        : "=&v"(x[0][0]), "=&v"(x[0][1]), "=&v"(x[1][0]), "=&v"(x[1][1]), "=&v"(x[2][0]), "=&v"(x[2][1])
-        : "v"(p[0]), "v"(p[1]), "v"(p[2]), "v"(p[0] ^ 32), "v"(p[1] ^ 32), "v"(p[2] ^ 32), "n"(AT),
-          "n"(AT + 8 * DP * 2)
-        : "memory");
-    join(x, f);
-  }
-  template <int AT>
-  static __device__ __forceinline__ void column(const uint32_t (&p)[4], lm_u32x4 (&f)[4]) {
-    lm_u32x2 x[4][2];
-    asm volatile(
-        "ds_read_b64_tr_b16 %0, %8 offset:%16\n\tds_read_b64_tr_b16 %1, %12 offset:%17\n\t"
-        "ds_read_b64_tr_b16 %2, %9 offset:%16\n\tds_read_b64_tr_b16 %3, %13 offset:%17\n\t"
-        "ds_read_b64_tr_b16 %4, %10 offset:%16\n\tds_read_b64_tr_b16 %5, %14 offset:%17\n\t"
-        "ds_read_b64_tr_b16 %6, %11 offset:%16\n\tds_read_b64_tr_b16 %7, %15 offset:%17\n\t"
-        "s_waitcnt lgkmcnt(0)"
-        : "=&v"(x[0][0]), "=&v"(x[0][1]), "=&v"(x[1][0]), "=&v"(x[1][1]), "=&v"(x[2][0]), "=&v"(x[2][1]),
-          "=&v"(x[3][0]), "=&v"(x[3][1])
-        : "v"(p[0]), "v"(p[1]), "v"(p[2]), "v"(p[3]), "v"(p[0] ^ 32), "v"(p[1] ^ 32), "v"(p[2] ^ 32), "v"(p[3] ^ 32),
-          "n"(AT), "n"(AT + 8 * DP * 2)
-        : "memory");
+  template <int AT, int N>
+  static __device__ __forceinline__ void column(const uint32_t (&p)[N], lm_u32x4 (&f)[N]) {
+    typedef short S4 __attribute__((ext_vector_type(4)));
+    typedef __attribute__((address_space(3))) S4* P;
+    lm_u32x2 x[N][2];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      x[i][0] = __builtin_bit_cast(lm_u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(p[i] + AT)));
+      x[i][1] = __builtin_bit_cast(lm_u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)((p[i] ^ 32) + AT + 8 * DP * 2)));
+    }
     join(x, f);
   }
   template <int N>
