@@ -55,6 +55,11 @@ __device__ __forceinline__ float sum_halves(float x) {
   return __builtin_bit_cast(float, a) + __builtin_bit_cast(float, b);
 }
 
+// Two waves share a SIMD.
+__device__ __forceinline__ void one_first() {
+  if (__builtin_amdgcn_s_getreg(3 << 11 | 4) & 1) __builtin_amdgcn_s_setprio(2);
+}
+
 // Rows of DP values in LDS, as a stage of ROWS of them.  A line's chunks of 16
 // bytes are turned by its number, so that the lanes that read at once meet in
 // none of the 64 banks: sixteen that read a chunk of sixteen lines, or 32 that
@@ -177,8 +182,8 @@ __device__ __forceinline__ lm_u32x4 terms(const f32x16& x, int u) {
 
 __device__ __forceinline__ int place(int r, int h) { return 8 * (r / 4) + 4 * h + r % 4; }
 
-constexpr int BM = 128, BN = 64;   // queries of a workgroup, keys of a stage
-constexpr int KEYS = kAttentionKeys, STEP = 128;          // for dK and dV: keys of a workgroup, queries of a stage
+constexpr int BM = 128, BN = 64;       // queries of a workgroup, keys of a stage
+constexpr int KEYS = kAttentionKeys;   // for dK and dV: keys of a workgroup
 
 // What a workgroup works on: rows first .. of a sequence [start, end) and a head.
 struct Work {
@@ -269,6 +274,7 @@ __global__ __launch_bounds__(256, 2) void k_attention(AttentionArgs a) {
   __shared__ __align__(16) char lds[4 * R::BYTES];   // two stages of K and V
   const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
   const int c = lane % 32, h = lane / 32;
+  one_first();
   const Work w = work<true>(a, a.heads, BM, lane);
   if (w.rows.empty()) return;
   const int len = w.rows.end - w.rows.start, q0 = w.rows.first - w.rows.start, qw = q0 + 32 * wave, qi = qw + c;
@@ -366,6 +372,7 @@ __global__ __launch_bounds__(256, 2) void k_attention_dq(AttentionArgs a) {
   __shared__ __align__(16) char lds[4 * R::BYTES];   // two stages of K and V
   const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
   const int c = lane % 32, h = lane / 32;
+  one_first();
   const Work w = work<true>(a, a.heads, BM, lane);
   if (w.rows.empty()) return;
   const int len = w.rows.end - w.rows.start, q0 = w.rows.first - w.rows.start, qw = q0 + 32 * wave, qi = qw + c;
@@ -455,20 +462,22 @@ __global__ __launch_bounds__(256, 2) void k_attention_dq(AttentionArgs a) {
   write_rows<E, DP>(at(a.dQ, row, w.head), a.dQ.token, len - qw, a.D, lane, dq, a.scale);
 }
 
-// Eight waves: two groups of 32 keys, and each the four groups of 32 queries of
-// a stage, whose sums are joined at the end.
-template <typename E, int DP>
-__global__ __launch_bounds__(512, 2) void k_attention_dkv(AttentionArgs a) {
-  typedef Rows<DP, STEP, 512> R;
-  typedef Rows<DP, KEYS, 512> RV;
+// Two groups of 32 keys, and each the G groups of 32 queries of a stage: 2 G
+// waves, whose sums are joined at the end.
+template <typename E, int DP, int G>
+__global__ __launch_bounds__(128 * G, 2) void k_attention_dkv(AttentionArgs a) {
+  constexpr int STEP = 32 * G, THREADS = 128 * G;
+  typedef Rows<DP, STEP, THREADS> R;
+  typedef Rows<DP, KEYS, THREADS> RV;
   // with 128 values a head, registers hold the keys but not the values beside the sums
   constexpr bool V_IN_LDS = DP == 128;
-  constexpr int STAGE = 2 * R::BYTES + 8 * 256;      // Q, dO, and of each query: delta, lse (twice: every wave loads)
+  constexpr int STAGE = 2 * R::BYTES + 2 * G * 256;      // Q, dO, and of each query: delta, lse (twice: every wave loads)
   constexpr int VALUES = DP / 32 * 2 * 16;           // sums of a lane
   __shared__ __align__(16) char lds[2 * STAGE + (V_IN_LDS ? KEYS * DP * 2 : 0)];
-  static_assert(4 * VALUES * 256 <= 2 * STAGE, "the sums of half the waves go through LDS");
+  static_assert(G * VALUES * 256 <= 2 * STAGE, "the sums of half the waves go through LDS");
   const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
   const int c = lane % 32, h = lane / 32, part = wave / 2;
+  one_first();
   const Work w = work<false>(a, a.kv_heads, KEYS, lane);
   if (w.rows.empty()) return;
   const int len = w.rows.end - w.rows.start, k0 = w.rows.first - w.rows.start, kw = k0 + 32 * (wave % 2), ki = kw + c;
@@ -507,8 +516,8 @@ __global__ __launch_bounds__(512, 2) void k_attention_dkv(AttentionArgs a) {
     R::load(at(a.Q, from, head), a.Q.token, left, a.D, to, wave, lane, off_q);
     R::load(at(a.dO, from, head), a.dO.token, left, a.D, to + R::BYTES, wave, lane, off_d);
     typedef __attribute__((address_space(3))) void* P;
-    const int i = wave % 2 * 64 + lane;
-    const float* x = a.delta + (wave / 2 % 2 * a.heads + head) * a.T + from;
+    const int i = wave % (G / 2) * 64 + lane;
+    const float* x = a.delta + (wave / (G / 2) % 2 * a.heads + head) * a.T + from;
     __builtin_amdgcn_raw_ptr_buffer_load_lds(make_rsrc(x, static_cast<uint32_t>(kMaxBufferBytes)),
                                              (P)(to + 2 * R::BYTES + wave * 256), 4,
                                              i < left ? static_cast<uint32_t>(i * 4) : kOutOfRange, 0, 0, 0);
@@ -544,7 +553,7 @@ __global__ __launch_bounds__(512, 2) void k_attention_dkv(AttentionArgs a) {
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
       const lm_f32x4 delta = *reinterpret_cast<const lm_f32x4*>(stats + 32 * g);
-      const lm_f32x4 lse2 = *reinterpret_cast<const lm_f32x4*>(stats + 512 + 32 * g);
+      const lm_f32x4 lse2 = *reinterpret_cast<const lm_f32x4*>(stats + STEP * 4 + 32 * g);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const int r = 4 * g + j;
@@ -572,9 +581,9 @@ __global__ __launch_bounds__(512, 2) void k_attention_dkv(AttentionArgs a) {
     product(std::integral_constant<int, 0>{});
     product(std::integral_constant<int, 1>{});
   }
-  // the sums of waves 4 to 7 join those of 0 to 3, and then 2 and 3 those of 0 and 1
+  // the sums of the upper half of the waves join the lower half's, until two are left
 #pragma unroll
-  for (int from = 4; from >= 2; from /= 2) {
+  for (int from = G; from >= 2; from /= 2) {
     wait_step<0>();
     if (wave >= from && wave < 2 * from) {
       float* to = reinterpret_cast<float*>(lds) + (wave - from) * VALUES * 64 + lane;
@@ -614,7 +623,8 @@ void launch_typed(AttentionArgs a, bool grad, hipStream_t s) {
   }
   k_attention_dq<E, DP><<<a.slots * a.heads, 256, 0, s>>>(a);
   a.slots = slots_of(a, KEYS);
-  k_attention_dkv<E, DP><<<a.slots * a.kv_heads, 512, 0, s>>>(a);
+  constexpr int G = DP == 128 ? 4 : 2;
+  k_attention_dkv<E, DP, G><<<a.slots * a.kv_heads, 128 * G, 0, s>>>(a);
 }
 template <typename E>
 void launch_wide(const AttentionArgs& a, bool grad, hipStream_t s) {
