@@ -55,11 +55,6 @@ __device__ __forceinline__ float sum_halves(float x) {
   return __builtin_bit_cast(float, a) + __builtin_bit_cast(float, b);
 }
 
-// Two waves share a SIMD.
-__device__ __forceinline__ void one_first() {
-  if (__builtin_amdgcn_s_getreg(3 << 11 | 4) & 1) __builtin_amdgcn_s_setprio(2);
-}
-
 // Rows of DP values in LDS, as a stage of ROWS of them.  A line's chunks of 16
 // bytes are turned by its number, so that the lanes that read at once meet in
 // none of the 64 banks: sixteen that read a chunk of sixteen lines, or 32 that
@@ -191,21 +186,6 @@ struct Work {
   int head;
 };
 
-// Sum over a wave.
-__device__ __forceinline__ uint32_t wave_sum(uint32_t v) {
-  const auto add = [&](auto control) {
-    v += static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), decltype(control)::value, 0xf, 0xf, true));
-  };
-  add(std::integral_constant<int, 0xB1>{});    // lanes 1, 0, 3, 2
-  add(std::integral_constant<int, 0x4E>{});    // lanes 2, 3, 0, 1
-  add(std::integral_constant<int, 0x141>{});   // halves of 16 lanes mirrored
-  add(std::integral_constant<int, 0x140>{});   // 16 lanes mirrored
-  return static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(v), 0)) +
-         static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(v), 16)) +
-         static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(v), 32)) +
-         static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(v), 48));
-}
-
 // Tile number `rank` of all sequences' tiles of `rows` rows, those with the most
 // keys (LAST: the last tiles of long sequences) or queries (the first ones) to
 // pass first: workgroups start in the order of their numbers, and with the
@@ -232,7 +212,7 @@ __device__ __forceinline__ LmChunk tile(const AttentionArgs& a, uint32_t rows, u
     uint32_t sum = 0;
 #pragma unroll
     for (int k = 0; k < kSorted / 64; ++k) sum += tiles[k] >= w ? tiles[k] - w + 1 : 0;
-    return wave_sum(sum);
+    return lm_wave_sum(sum);
   };
   LmChunk c{0, 0, 0, 0};
   if (with(1) <= rank) return c;
@@ -274,7 +254,7 @@ __global__ __launch_bounds__(256, 2) void k_attention(AttentionArgs a) {
   __shared__ __align__(16) char lds[4 * R::BYTES];   // two stages of K and V
   const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
   const int c = lane % 32, h = lane / 32;
-  one_first();
+  lm_one_first();
   const Work w = work<true>(a, a.heads, BM, lane);
   if (w.rows.empty()) return;
   const int len = w.rows.end - w.rows.start, q0 = w.rows.first - w.rows.start, qw = q0 + 32 * wave, qi = qw + c;
@@ -372,7 +352,7 @@ __global__ __launch_bounds__(256, 2) void k_attention_dq(AttentionArgs a) {
   __shared__ __align__(16) char lds[4 * R::BYTES];   // two stages of K and V
   const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
   const int c = lane % 32, h = lane / 32;
-  one_first();
+  lm_one_first();
   const Work w = work<true>(a, a.heads, BM, lane);
   if (w.rows.empty()) return;
   const int len = w.rows.end - w.rows.start, q0 = w.rows.first - w.rows.start, qw = q0 + 32 * wave, qi = qw + c;
@@ -477,7 +457,7 @@ __global__ __launch_bounds__(128 * G, 2) void k_attention_dkv(AttentionArgs a) {
   static_assert(G * VALUES * 256 <= 2 * STAGE, "the sums of half the waves go through LDS");
   const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
   const int c = lane % 32, h = lane / 32, part = wave / 2;
-  one_first();
+  lm_one_first();
   const Work w = work<false>(a, a.kv_heads, KEYS, lane);
   if (w.rows.empty()) return;
   const int len = w.rows.end - w.rows.start, k0 = w.rows.first - w.rows.start, kw = k0 + 32 * (wave % 2), ki = kw + c;

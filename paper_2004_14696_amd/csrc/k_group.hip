@@ -393,29 +393,63 @@ __device__ __forceinline__ void store4(O* p, const f32x4& x, int left) {
   }
 }
 
-// Four columns of one row, from their sums z: n and m count from the tile's
+template <int N>
+__device__ __forceinline__ void act_all(f32x4 (&z)[N], int act) {
+  const auto all = [&](auto which) {
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) z[j][r] = lm_act(z[j][r], decltype(which)::value);
+  };
+  if (act == DBW_ACT_RELU) all(std::integral_constant<int, DBW_ACT_RELU>{});
+  if (act == DBW_ACT_GELU) all(std::integral_constant<int, DBW_ACT_GELU>{});
+  if (act == DBW_ACT_SILU) all(std::integral_constant<int, DBW_ACT_SILU>{});
+}
+
+// Four columns of one row, from their sums z with the bias: n and m count from the tile's
 // first column and row.
 template <typename E, typename O>
 __device__ __forceinline__ void finish4(const Epilogue& e, O* out, int64_t ldo, int m, int n, int left, f32x4 z) {
-  if (e.bias) z += load4<float>(e.bias + n, left);
   if (e.pre) store4<E>(static_cast<E*>(e.pre) + m * e.ld_pre + n, z, left);
-  if (e.act != DBW_ACT_NONE)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) z[j] = lm_act(z[j], e.act);
+  f32x4 y[1] = {z};
+  act_all(y, e.act);
+  z = y[0];
   if (e.residual) z += load4<O>(static_cast<const O*>(e.residual) + m * e.ld_residual + n, left);
   store4<O>(out + m * ldo + n, z, left);
 }
 
-// A wave's outputs with an epilogue: the sums go through LDS as they are, so
-// that a lane finishes four columns of a row and memory takes whole lines.
+// A wave's outputs with an epilogue but no residual: 16 rows at a time, the
+// epilogue where the sums are, and out through LDS in the outputs' types.
+template <typename E, typename O, int WM, int WN, int LDS>
+__device__ __forceinline__ void write_acted(const f32x4 (&acc)[WM / 16][WN / 16], const Tile& t, const Epilogue& e,
+                                            int m0, int n0, char* lds, int lane) {
+  constexpr int TN = WN / 16;
+  Tile pre = t;
+  pre.out = e.pre;
+  pre.ldo = e.ld_pre;
+#pragma unroll
+  for (int p = 0; p < WM / 16; ++p) {
+    f32x4 z[1][TN];
+#pragma unroll
+    for (int j = 0; j < TN; ++j) z[0][j] = acc[p][j];
+    if (e.pre) write_out<E, 16, WN, LDS, false>(z, pre, m0 + 16 * p, n0, lds, lane);
+    act_all(z[0], e.act);
+    write_out<O, 16, WN, LDS, false>(z, t, m0 + 16 * p, n0, lds, lane);
+  }
+}
+
+// A wave's outputs with a residual: the sums go through LDS as they are, so
+// that a lane finishes four columns of a row and memory takes whole lines of
+// the residual too.
 template <typename E, typename O, int WM, int WN, int LDS>
 __device__ __forceinline__ void write_finished(const f32x4 (&acc)[WM / 16][WN / 16], const Tile& t, const Epilogue& e,
                                                int m0, int n0, char* lds, int lane) {
   constexpr int BYTES = WN * 4, CH = BYTES / 16;
   constexpr int TILES = LDS / BYTES / 16 >= WM / 16 ? WM / 16 : LDS / BYTES >= 64 ? 4 : LDS / BYTES >= 32 ? 2 : 1;
   constexpr int ROWS = 16 * TILES;
-  static_assert(ROWS * BYTES <= LDS && WM % ROWS == 0 && ROWS * CH % 64 == 0, "whole passes");
+  static_assert(ROWS * BYTES <= LDS && WM % ROWS == 0 && 64 % CH == 0 && ROWS * CH % 64 == 0, "whole passes");
   const int c = lane % 16, g = lane / 16;
+  const int q = lane % CH, n = n0 + q * 4;   // the same columns of every row
 #pragma unroll
   for (int p = 0; p < WM / ROWS; ++p) {
 #pragma unroll
@@ -428,9 +462,8 @@ __device__ __forceinline__ void write_finished(const f32x4 (&acc)[WM / 16][WN / 
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll 4
     for (int i = 0; i < ROWS * CH / 64; ++i) {
-      const int row = (i * 64 + lane) / CH, q = (i * 64 + lane) % CH;
+      const int row = (i * 64 + lane) / CH, m = m0 + p * ROWS + row;
       const f32x4 z = *reinterpret_cast<const f32x4*>(lds + row * BYTES + (q ^ (row & (CH - 1) & 15)) * 16);
-      const int m = m0 + p * ROWS + row, n = n0 + q * 4;
       if (m < t.rows && n < t.cols) finish4<E, O>(e, static_cast<O*>(t.out), t.ldo, m, n, t.cols - n, z);
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -450,11 +483,18 @@ __device__ __forceinline__ void product(const Tile& t, const Epilogue& e, bool o
   const E* a = static_cast<const E*>(t.a);
   const E* b = static_cast<const E*>(t.b);
 
+  // sums start at the bias, if there is one: nothing waits for it then
   f32x4 acc[TM][TN];
 #pragma unroll
-  for (int i = 0; i < TM; ++i)
+  for (int j = 0; j < TN; ++j) {
+    f32x4 first = {0.f, 0.f, 0.f, 0.f};
+    if constexpr (EPILOGUE) {
+      const int n = n0 + 16 * j + lane / 16 * 4;
+      if (e.bias && !parts && n < t.cols) first = load4<float>(e.bias + n, t.cols - n);
+    }
 #pragma unroll
-    for (int j = 0; j < TN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < TM; ++i) acc[i][j] = first;
+  }
 
   const auto multiply = [&](const char* stages, auto slot) {
     constexpr int AT = decltype(slot)::value * STAGE;
@@ -536,7 +576,13 @@ __device__ __forceinline__ void product(const Tile& t, const Epilogue& e, bool o
   constexpr int LDS = (WIDE ? STAGES : 2) * STAGE / (THREADS / 64);   // bytes a wave
   char* mine = lds + wave * LDS;
   if constexpr (EPILOGUE)
-    if (!parts) {
+    if (!parts && !e.residual) {
+      if (out_f32)
+        write_acted<E, float, WM, WN, LDS>(acc, t, e, m0, n0, mine, lane);
+      else
+        write_acted<E, E, WM, WN, LDS>(acc, t, e, m0, n0, mine, lane);
+      return;
+    } else if (!parts) {
       if (out_f32)
         write_finished<E, float, WM, WN, LDS>(acc, t, e, m0, n0, mine, lane);
       else
@@ -754,6 +800,7 @@ __global__ __launch_bounds__(256) void k_group_finish(GroupArgs g, const float* 
     }
     if (e.residual) e.residual = static_cast<const O*>(e.residual) + row * e.ld_residual;
     if (e.pre) e.pre = static_cast<E*>(e.pre) + row * e.ld_pre;
+    if (e.bias) z += load4<float>(e.bias + n, left);
     finish4<E, O>(e, static_cast<O*>(g.out) + row * g.ld_C, 0, 0, n, left, z);
   }
 }

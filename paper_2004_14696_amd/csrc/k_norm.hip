@@ -123,9 +123,7 @@ __device__ __forceinline__ void store_f32(float* w, const P& p, const float (&x)
 template <int W, int K>
 __device__ __forceinline__ void row_sum(float (&v)[K], float* lds, int& turn) {
 #pragma unroll
-  for (int d = 32; d; d /= 2)
-#pragma unroll
-    for (int k = 0; k < K; ++k) v[k] += __shfl_xor(v[k], d);
+  for (int k = 0; k < K; ++k) v[k] = lm_wave_sum(v[k]);
   if constexpr (W > 1) {
     float* mine = lds + turn * (K * W);
     turn ^= 1;
@@ -444,37 +442,47 @@ void launch_piece_sum(const PieceSum& c, hipStream_t s) {
   k_piece_sum<<<grid, 256, 0, s>>>(c);
 }
 
-template <typename E, int W, int PACKS, bool WHOLE>
-void norm_launch(const NormArgs& a, bool grad, hipStream_t s) {
+template <typename E, int W, int PACKS>
+void forward(const NormArgs& a, hipStream_t s) {
   constexpr int TEAMS = W == 1 ? 4 : 1, THREADS = W == 1 ? 256 : 64 * W;
-  if (grad) {
-    k_norm_grad<E, W, PACKS, WHOLE><<<static_cast<uint32_t>(ceil_div(a.parts_of_rows, TEAMS)), THREADS, 0, s>>>(a);
-  } else {
-    const int64_t most = W == 16 ? 512 : 2048;
-    k_norm<E, W, PACKS, WHOLE><<<static_cast<uint32_t>(std::min(most, ceil_div(a.T, TEAMS))), THREADS, 0, s>>>(a);
-  }
+  const uint32_t grid = static_cast<uint32_t>(std::min<int64_t>(W == 16 ? 512 : 2048, ceil_div(a.T, TEAMS)));
+  if (a.d % Pack<E>::N == 0) k_norm<E, W, PACKS, true><<<grid, THREADS, 0, s>>>(a);
+  else k_norm<E, W, PACKS, false><<<grid, THREADS, 0, s>>>(a);
 }
 template <typename E, int W, int PACKS>
-void norm_variant(const NormArgs& a, bool grad, hipStream_t s) {
-  if (a.d % Pack<E>::N == 0) norm_launch<E, W, PACKS, true>(a, grad, s);
-  else norm_launch<E, W, PACKS, false>(a, grad, s);
+void backward(const NormArgs& a, hipStream_t s) {
+  constexpr int TEAMS = W == 1 ? 4 : 1, THREADS = W == 1 ? 256 : 64 * W;
+  const uint32_t grid = static_cast<uint32_t>(ceil_div(a.parts_of_rows, TEAMS));
+  if (a.d % Pack<E>::N == 0) k_norm_grad<E, W, PACKS, true><<<grid, THREADS, 0, s>>>(a);
+  else k_norm_grad<E, W, PACKS, false><<<grid, THREADS, 0, s>>>(a);
 }
 
 template <typename E>
 void norm_typed(const NormArgs& a, bool grad, hipStream_t s) {
   constexpr int N = Pack<E>::N;
+  if (!grad) {
+    // a wave to a row as far as its registers hold one: no barriers
+    const int packs = static_cast<int>(ceil_div(a.d, N * 64));
+    if (packs <= 1) return forward<E, 1, 1>(a, s);
+    if (packs <= 2) return forward<E, 1, 2>(a, s);
+    if (packs <= 4) return forward<E, 1, 4>(a, s);
+    if (packs <= 8) return forward<E, 1, 8>(a, s);
+    if (packs <= 16) return forward<E, 4, 4>(a, s);
+    if (packs <= 32) return forward<E, 4, 8>(a, s);
+    return forward<E, 16, 4>(a, s);
+  }
   const int w = norm_waves(a.d);
   const int packs = static_cast<int>(ceil_div(a.d, N * 64 * w));
   if constexpr (N == 4) {
     if (packs > 2) {
-      if (w == 1) return norm_variant<E, 1, 4>(a, grad, s);
-      if (w == 4) return norm_variant<E, 4, 4>(a, grad, s);
-      return norm_variant<E, 16, 4>(a, grad, s);
+      if (w == 1) return backward<E, 1, 4>(a, s);
+      if (w == 4) return backward<E, 4, 4>(a, s);
+      return backward<E, 16, 4>(a, s);
     }
   }
-  if (w == 1) return packs > 1 ? norm_variant<E, 1, 2>(a, grad, s) : norm_variant<E, 1, 1>(a, grad, s);
-  if (w == 4) return packs > 1 ? norm_variant<E, 4, 2>(a, grad, s) : norm_variant<E, 4, 1>(a, grad, s);
-  return packs > 1 ? norm_variant<E, 16, 2>(a, grad, s) : norm_variant<E, 16, 1>(a, grad, s);
+  if (w == 1) return packs > 1 ? backward<E, 1, 2>(a, s) : backward<E, 1, 1>(a, s);
+  if (w == 4) return packs > 1 ? backward<E, 4, 2>(a, s) : backward<E, 4, 1>(a, s);
+  return packs > 1 ? backward<E, 16, 2>(a, s) : backward<E, 16, 1>(a, s);
 }
 
 void norm(const NormArgs& a, bool grad, hipStream_t s) {

@@ -6,6 +6,7 @@
 
 #include <cstdint>
 #include <string>
+#include <type_traits>
 
 #include "dbw.h"
 
@@ -126,6 +127,35 @@ __host__ __device__ inline uint32_t adam_index(int64_t index) {
   return static_cast<uint32_t>(i) * 0x6A09E667u + static_cast<uint32_t>(i >> 32) * 0xBB67AE85u;
 }
 
+// Sums over the 64 lanes of a wave, in every lane: four steps within 16 lanes,
+// and the four 16s.
+template <int CONTROL>
+__device__ __forceinline__ uint32_t lm_moved(uint32_t v) {
+  return static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), CONTROL, 0xf, 0xf, true));
+}
+__device__ __forceinline__ uint32_t lm_lane(uint32_t v, int lane) {
+  return static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(v), lane));
+}
+__device__ __forceinline__ uint32_t lm_wave_sum(uint32_t v) {
+  v += lm_moved<0xB1>(v);    // lanes 1, 0, 3, 2
+  v += lm_moved<0x4E>(v);    // lanes 2, 3, 0, 1
+  v += lm_moved<0x141>(v);   // halves of 16 lanes mirrored
+  v += lm_moved<0x140>(v);   // 16 lanes mirrored
+  return lm_lane(v, 0) + lm_lane(v, 16) + lm_lane(v, 32) + lm_lane(v, 48);
+}
+__device__ __forceinline__ float lm_wave_sum(float v) {
+  const auto moved = [&](auto control) {
+    return __builtin_bit_cast(float, lm_moved<decltype(control)::value>(__builtin_bit_cast(uint32_t, v)));
+  };
+  v += moved(std::integral_constant<int, 0xB1>{});
+  v += moved(std::integral_constant<int, 0x4E>{});
+  v += moved(std::integral_constant<int, 0x141>{});
+  v += moved(std::integral_constant<int, 0x140>{});
+  const uint32_t u = __builtin_bit_cast(uint32_t, v);
+  return (__builtin_bit_cast(float, lm_lane(u, 0)) + __builtin_bit_cast(float, lm_lane(u, 16))) +
+         (__builtin_bit_cast(float, lm_lane(u, 32)) + __builtin_bit_cast(float, lm_lane(u, 48)));
+}
+
 // ---------------------------------------------------------------------------
 // Rows of ragged groups in chunks of `rows` rows: chunk number `slot` belongs
 // to the group i with the largest (offsets[i] - offsets[0]) / rows + i that is
@@ -175,14 +205,12 @@ __device__ __forceinline__ LmChunk lm_chunk(const int32_t* offsets, int n, int64
 // Activations: z sigmoid(s(z)) with s = 2 (a z + b z^3) or z, or simpler ones.
 constexpr float kLog2E = 1.44269504088896341f;
 constexpr float kGeluA = 0.797884560802865356f, kGeluB = 0.0356774081363001f;   // sqrt(2/pi), 0.044715 sqrt(2/pi)
-__device__ __forceinline__ float lm_sigmoid(float s) {
-  return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-kLog2E * s));
-}
 __device__ __forceinline__ float lm_act(float z, int act) {
   if (act == DBW_ACT_RELU) return z < 0.f ? 0.f : z;   // (a NaN stays)
-  if (act == DBW_ACT_GELU) return z * lm_sigmoid(2.f * z * fmaf(kGeluB * z, z, kGeluA));
-  if (act == DBW_ACT_SILU) return z * lm_sigmoid(z);
-  return z;
+  if (act == DBW_ACT_NONE) return z;
+  // exp(-s) as a power of two, with the factors joined
+  const float s = act == DBW_ACT_GELU ? z * fmaf(-2.f * kLog2E * kGeluB, z * z, -2.f * kLog2E * kGeluA) : -kLog2E * z;
+  return z * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(s));
 }
 // p + z p (1 - p) s'(z) with p = sigmoid(s): 1 - p as e / (1 + e), so that it keeps
 // its digits where p is near 1 (1 - p by subtraction left 1e-5 of GELU's slope at
@@ -198,6 +226,13 @@ __device__ __forceinline__ float lm_act_slope(float z, int act) {
   const float ds = gelu ? 2.f * fmaf(3.f * kGeluB * z, z, kGeluA) : 1.f;
   const float e = __builtin_amdgcn_exp2f(-kLog2E * s), p = __builtin_amdgcn_rcpf(1.f + e);
   return fmaf(z * p * (e * p), ds, p);
+}
+
+// Where two waves share a SIMD, one of them goes first in everything, so that
+// the other multiplies while it does not, and the other way around: waves that
+// take turns stay in step, and the matrix cores wait for both at once.
+__device__ __forceinline__ void lm_one_first() {
+  if (__builtin_amdgcn_s_getreg(3 << 11 | 4) & 1) __builtin_amdgcn_s_setprio(2);   // by the wave's place in its SIMD
 }
 
 // ---------------------------------------------------------------------------
