@@ -253,9 +253,18 @@ DBW_API dbw_status dbw_attention(const dbw_attention_shape* shape, const int32_t
   return launched(call, dbw::launch_attention(a, static_cast<hipStream_t>(stream)));
 }
 
+namespace {
+// delta and lse of every query; and the parts' sums
+int64_t delta_bytes(const dbw_attention_shape& p) { return (int64_t{8} * p.heads * p.T + 15) / 16 * 16; }
+int64_t sum_bytes(const dbw_attention_shape& p) {
+  const int64_t parts = dbw::attention_parts(p.n, p.T, p.heads, p.kv_heads);
+  return parts > 1 ? parts * 8 * p.T * p.kv_heads * p.D : 0;
+}
+}  // namespace
+
 DBW_API int64_t dbw_attention_workspace(const dbw_attention_shape* shape) {
   if (check_attention("dbw_attention_workspace", shape) != DBW_OK) return -1;
-  return int64_t{8} * shape->heads * shape->T;   // delta and lse of every query
+  return delta_bytes(*shape) + sum_bytes(*shape);
 }
 
 DBW_API dbw_status dbw_attention_grad(const dbw_attention_shape* shape, const int32_t* offsets, const dbw_heads* dO,
@@ -283,10 +292,12 @@ DBW_API dbw_status dbw_attention_grad(const dbw_attention_shape* shape, const in
       if (x.out && &x != &y && x.h->data == y.h->data) return overlap(call);
   for (const auto& x : arrays)
     if (x.out && x.h->data == lse) return overlap(call);
-  if (dbw_status s = check_workspace(call, int64_t{8} * p.heads * p.T, workspace, workspace_bytes); s != DBW_OK) return s;
+  if (dbw_status s = check_workspace(call, delta_bytes(p) + sum_bytes(p), workspace, workspace_bytes); s != DBW_OK) return s;
   dbw::AttentionArgs a = attention_args(p, offsets);
   a.Q = rows_of(*Q); a.K = rows_of(*K); a.V = rows_of(*V); a.O = rows_of(*O); a.dO = rows_of(*dO);
   a.dQ = rows_of(*dQ); a.dK = rows_of(*dK); a.dV = rows_of(*dV);
   a.lse = const_cast<float*>(lse); a.delta = static_cast<float*>(workspace);
+  a.parts = dbw::attention_parts(p.n, p.T, p.heads, p.kv_heads);
+  a.sums = reinterpret_cast<float*>(static_cast<char*>(workspace) + delta_bytes(p));
   return launched(call, dbw::launch_attention_grad(a, static_cast<hipStream_t>(stream)));
 }

@@ -2,6 +2,7 @@
 //   k_attention       O and lse: a workgroup takes 128 queries of a head
 //   k_attention_dq    dQ, and delta = dO . O of each query: the same
 //   k_attention_dkv   dK and dV: a workgroup takes 64 keys of a head of keys
+//   k_attention_join  dK and dV where several share them
 //
 // v_mfma_f32_32x32x16 takes, in lane l = 32 h + c, row c and terms 8 h .. 8 h +
 // 7 of each operand; its result r of a lane is row 8 (r / 4) + 4 h + r % 4 of
@@ -179,6 +180,7 @@ __device__ __forceinline__ int place(int r, int h) { return 8 * (r / 4) + 4 * h 
 
 constexpr int BM = 128, BN = 64;       // queries of a workgroup, keys of a stage
 constexpr int KEYS = kAttentionKeys;   // for dK and dV: keys of a workgroup
+constexpr uint32_t kFewTiles = 256;    // workgroups that leave a CU each
 
 // What a workgroup works on: rows first .. of a sequence [start, end) and a head.
 struct Work {
@@ -244,18 +246,22 @@ __device__ __forceinline__ LmChunk tile(const AttentionArgs& a, uint32_t rows, u
   return c;
 }
 template <bool LAST>
-__device__ __forceinline__ Work work(const AttentionArgs& a, int heads, int rows, int lane) {
-  return Work{tile<LAST>(a, rows, blockIdx.x / heads, lane), static_cast<int>(blockIdx.x % heads)};
+__device__ __forceinline__ Work work(const AttentionArgs& a, uint32_t id, int heads, int rows, int lane) {
+  return Work{tile<LAST>(a, rows, id / heads, lane), static_cast<int>(id % heads)};
 }
 
-template <typename E, int DP>
-__global__ __launch_bounds__(256, 2) void k_attention(AttentionArgs a) {
-  typedef Rows<DP, BN, 256> R;
+// S groups of four waves, which take the same queries and every S-th 64 keys,
+// and whose sums are joined at the end.
+template <typename E, int DP, int S>
+__global__ __launch_bounds__(256 * S, 2) void k_attention(AttentionArgs a) {
+  typedef Rows<DP, BN * S, 256 * S> R;
   __shared__ __align__(16) char lds[4 * R::BYTES];   // two stages of K and V
-  const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
-  const int c = lane % 32, h = lane / 32;
+  constexpr int VALUES = DP / 32 * 16 + 2;           // of a lane, to be joined
+  static_assert(S == 1 || 4 * VALUES * 256 <= 4 * R::BYTES, "they go through LDS");
+  const int tid = threadIdx.x, lane = tid % 64, all_waves = __builtin_amdgcn_readfirstlane(tid / 64);
+  const int wave = all_waves % 4, part = all_waves / 4, c = lane % 32, h = lane / 32;
   lm_one_first();
-  const Work w = work<true>(a, a.heads, BM, lane);
+  const Work w = work<true>(a, blockIdx.x, a.heads, BM, lane);
   if (w.rows.empty()) return;
   const int len = w.rows.end - w.rows.start, q0 = w.rows.first - w.rows.start, qw = q0 + 32 * wave, qi = qw + c;
   const int kv_head = w.head / (a.heads / a.kv_heads);
@@ -272,22 +278,23 @@ __global__ __launch_bounds__(256, 2) void k_attention(AttentionArgs a) {
   uint32_t off_k[R::CHUNKS], off_v[R::CHUNKS], pv[DP / 32];
 #pragma unroll
   for (int i = 0; i < R::CHUNKS; ++i) {
-    off_k[i] = R::offset(a.K.token, BN, a.D, tid, i);
-    off_v[i] = R::offset(a.V.token, BN, a.D, tid, i);
+    off_k[i] = R::offset(a.K.token, BN * S, a.D, tid, i);
+    off_v[i] = R::offset(a.V.token, BN * S, a.D, tid, i);
   }
-  R::columns(lds + R::BYTES, lane, pv);
+  R::columns(lds + R::BYTES + part * (BN * DP * 2), lane, pv);
   const int keys = std::min(len, q0 + BM);   // the workgroup's
   const auto issue = [&](int k0, int slot) {
     char* to = lds + slot * (2 * R::BYTES);
-    R::load(at(a.K, w.rows.start + static_cast<int64_t>(k0), kv_head), a.K.token, len - k0, a.D, to, wave, lane, off_k);
-    R::load(at(a.V, w.rows.start + static_cast<int64_t>(k0), kv_head), a.V.token, len - k0, a.D, to + R::BYTES, wave, lane, off_v);
+    R::load(at(a.K, w.rows.start + static_cast<int64_t>(k0), kv_head), a.K.token, len - k0, a.D, to, all_waves, lane, off_k);
+    R::load(at(a.V, w.rows.start + static_cast<int64_t>(k0), kv_head), a.V.token, len - k0, a.D, to + R::BYTES, all_waves, lane, off_v);
   };
   issue(0, 0);
-  for (int k0 = 0, slot = 0; k0 < keys; k0 += BN, slot ^= 1) {
+  for (int first = 0, slot = 0; first < keys; first += BN * S, slot ^= 1) {
     wait_step<0>();
-    if (k0 + BN < keys) issue(k0 + BN, slot ^ 1);
+    if (first + BN * S < keys) issue(first + BN * S, slot ^ 1);
+    const int k0 = first + BN * part;
     if (k0 > qw + 31 || qw >= len) continue;
-    const char* stage = lds + slot * (2 * R::BYTES);
+    const char* stage = lds + slot * (2 * R::BYTES) + part * (BN * DP * 2);
     f32x16 s[2] = {zero16(), zero16()};
 #pragma unroll
     for (int kk = 0; kk < DP / 16; ++kk)
@@ -339,21 +346,47 @@ __global__ __launch_bounds__(256, 2) void k_attention(AttentionArgs a) {
     product(std::integral_constant<int, 2>{});
     product(std::integral_constant<int, 3>{});
   }
-  if (qw >= len) return;
   sum = sum_halves(sum);
+  if constexpr (S == 2) {
+    // the second group's sums join the first's (it may have had no keys: its
+    // maximum is then -infinity, and its share 0)
+    float* to = reinterpret_cast<float*>(lds) + wave * VALUES * 64 + lane;
+    wait_step<0>();
+    if (part == 1) {
+      to[0] = m;
+      to[64] = sum;
+#pragma unroll
+      for (int i = 0; i < DP / 32; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) to[(2 + i * 16 + r) * 64] = o[i][r];
+    }
+    wait_step<0>();
+    if (part == 1) return;
+    const float m1 = to[0], top = fmaxf(m, m1);
+    const float by0 = __builtin_amdgcn_exp2f((m - top) * scale2), by1 = __builtin_amdgcn_exp2f((m1 - top) * scale2);
+    m = top;
+    sum = sum * by0 + to[64] * by1;
+#pragma unroll
+    for (int i = 0; i < DP / 32; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[i][r] = o[i][r] * by0 + to[(2 + i * 16 + r) * 64] * by1;
+  }
+  if (qw >= len) return;
   write_rows<E, DP>(at(a.O, w.rows.first + 32 * wave, w.head), a.O.token, len - qw, a.D, lane, o, 1.f / sum);
   if (a.lse && h == 0 && qi < len)
     a.lse[w.head * a.T + w.rows.start + qi] = (m * scale2 + __builtin_amdgcn_logf(sum)) * (1.f / kLog2E);
 }
 
-template <typename E, int DP>
-__global__ __launch_bounds__(256, 2) void k_attention_dq(AttentionArgs a) {
-  typedef Rows<DP, BN, 256> R;
+template <typename E, int DP, int S>
+__global__ __launch_bounds__(256 * S, 2) void k_attention_dq(AttentionArgs a) {
+  typedef Rows<DP, BN * S, 256 * S> R;
   __shared__ __align__(16) char lds[4 * R::BYTES];   // two stages of K and V
-  const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
-  const int c = lane % 32, h = lane / 32;
+  constexpr int VALUES = DP / 32 * 16;
+  static_assert(S == 1 || 4 * VALUES * 256 <= 4 * R::BYTES, "the sums to be joined go through LDS");
+  const int tid = threadIdx.x, lane = tid % 64, all_waves = __builtin_amdgcn_readfirstlane(tid / 64);
+  const int wave = all_waves % 4, part = all_waves / 4, c = lane % 32, h = lane / 32;
   lm_one_first();
-  const Work w = work<true>(a, a.heads, BM, lane);
+  const Work w = work<true>(a, blockIdx.x, a.heads, BM, lane);
   if (w.rows.empty()) return;
   const int len = w.rows.end - w.rows.start, q0 = w.rows.first - w.rows.start, qw = q0 + 32 * wave, qi = qw + c;
   const int kv_head = w.head / (a.heads / a.kv_heads);
@@ -378,7 +411,7 @@ __global__ __launch_bounds__(256, 2) void k_attention_dq(AttentionArgs a) {
     if (qi < len) {
       const int64_t to = w.head * a.T + w.rows.start + qi;
       lse2 = a.lse[to] * kLog2E;
-      if (h == 0) {
+      if (h == 0 && part == 0) {
         a.delta[to] = delta;
         a.delta[a.heads * a.T + to] = lse2;
       }
@@ -391,21 +424,22 @@ __global__ __launch_bounds__(256, 2) void k_attention_dq(AttentionArgs a) {
   uint32_t off_k[R::CHUNKS], off_v[R::CHUNKS], pk[DP / 32];
 #pragma unroll
   for (int i = 0; i < R::CHUNKS; ++i) {
-    off_k[i] = R::offset(a.K.token, BN, a.D, tid, i);
-    off_v[i] = R::offset(a.V.token, BN, a.D, tid, i);
+    off_k[i] = R::offset(a.K.token, BN * S, a.D, tid, i);
+    off_v[i] = R::offset(a.V.token, BN * S, a.D, tid, i);
   }
-  R::columns(lds, lane, pk);
+  R::columns(lds + part * (BN * DP * 2), lane, pk);
   const int keys = std::min(len, q0 + BM);
   const auto issue = [&](int k0, int slot) {
     char* to = lds + slot * (2 * R::BYTES);
-    R::load(at(a.K, w.rows.start + static_cast<int64_t>(k0), kv_head), a.K.token, len - k0, a.D, to, wave, lane, off_k);
-    R::load(at(a.V, w.rows.start + static_cast<int64_t>(k0), kv_head), a.V.token, len - k0, a.D, to + R::BYTES, wave, lane, off_v);
+    R::load(at(a.K, w.rows.start + static_cast<int64_t>(k0), kv_head), a.K.token, len - k0, a.D, to, all_waves, lane, off_k);
+    R::load(at(a.V, w.rows.start + static_cast<int64_t>(k0), kv_head), a.V.token, len - k0, a.D, to + R::BYTES, all_waves, lane, off_v);
   };
   issue(0, 0);
-  for (int k0 = 0, slot = 0; k0 < keys; k0 += BN, slot ^= 1) {
+  for (int first = 0, slot = 0; first < keys; first += BN * S, slot ^= 1) {
     wait_step<0>();
-    if (k0 + BN < keys) issue(k0 + BN, slot ^ 1);
-    const char* stage = lds + slot * (2 * R::BYTES);
+    if (first + BN * S < keys) issue(first + BN * S, slot ^ 1);
+    const int k0 = first + BN * part;
+    const char* stage = lds + slot * (2 * R::BYTES) + part * (BN * DP * 2);
     uint32_t p[DP / 32];
 #pragma unroll
     for (int i = 0; i < DP / 32; ++i) p[i] = pk[i] + slot * (2 * R::BYTES);
@@ -438,12 +472,41 @@ __global__ __launch_bounds__(256, 2) void k_attention_dq(AttentionArgs a) {
     part(std::integral_constant<int, 0>{});
     part(std::integral_constant<int, 1>{});
   }
+  if constexpr (S == 2) {
+    float* to = reinterpret_cast<float*>(lds) + wave * VALUES * 64 + lane;
+    wait_step<0>();
+    if (part == 1)
+#pragma unroll
+      for (int i = 0; i < DP / 32; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) to[(i * 16 + r) * 64] = dq[i][r];
+    wait_step<0>();
+    if (part == 1) return;
+#pragma unroll
+    for (int i = 0; i < DP / 32; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) dq[i][r] += to[(i * 16 + r) * 64];
+  }
   if (qw >= len) return;
   write_rows<E, DP>(at(a.dQ, row, w.head), a.dQ.token, len - qw, a.D, lane, dq, a.scale);
 }
 
+// A lane's sums of a row (see write_rows), as they are.
+template <int DP>
+__device__ __forceinline__ void write_sums(float* row, int D, int lane, const f32x16 (&x)[DP / 32]) {
+#pragma unroll
+  for (int i = 0; i < DP / 32; ++i)
+#pragma unroll
+    for (int k = 0; k < 16; k += 4) {
+      const int d = 32 * i + 2 * k + 4 * (lane / 32);
+      if (d < D) *reinterpret_cast<lm_f32x4*>(row + d) = lm_f32x4{x[i][k], x[i][k + 1], x[i][k + 2], x[i][k + 3]};
+    }
+}
+
 // Two groups of 32 keys, and each the G groups of 32 queries of a stage: 2 G
-// waves, whose sums are joined at the end.
+// waves, whose sums are joined at the end.  With a.parts > 1, as many workgroups
+// have a part of the queries and heads each, and leave their sums to
+// k_attention_join.
 template <typename E, int DP, int G>
 __global__ __launch_bounds__(128 * G, 2) void k_attention_dkv(AttentionArgs a) {
   constexpr int STEP = 32 * G, THREADS = 128 * G;
@@ -458,7 +521,7 @@ __global__ __launch_bounds__(128 * G, 2) void k_attention_dkv(AttentionArgs a) {
   const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
   const int c = lane % 32, h = lane / 32, part = wave / 2;
   lm_one_first();
-  const Work w = work<false>(a, a.kv_heads, KEYS, lane);
+  const Work w = work<false>(a, blockIdx.x / a.parts, a.kv_heads, KEYS, lane);
   if (w.rows.empty()) return;
   const int len = w.rows.end - w.rows.start, k0 = w.rows.first - w.rows.start, kw = k0 + 32 * (wave % 2), ki = kw + c;
   const int share = a.heads / a.kv_heads;
@@ -487,8 +550,11 @@ __global__ __launch_bounds__(128 * G, 2) void k_attention_dkv(AttentionArgs a) {
   }
   R::columns(lds + 32 * part * DP * 2, lane, pq);
   // tiles of queries from the workgroup's first key on, for each head in turn
-  const int steps = (len - k0 + STEP - 1) / STEP, all = steps * share;
-  int head_of = 0, q_of = k0;      // the next stage to load
+  const int steps = (len - k0 + STEP - 1) / STEP;
+  const int64_t all = static_cast<int64_t>(steps) * share;
+  const int piece = static_cast<int>(blockIdx.x % a.parts);
+  const int64_t begin = all * piece / a.parts, end = all * (piece + 1) / a.parts;
+  int head_of = static_cast<int>(begin / steps), q_of = k0 + static_cast<int>(begin % steps) * STEP;   // the next stage to load
   const auto issue = [&](int slot) {
     char* to = lds + slot * STAGE;
     const int head = w.head * share + head_of, left = len - q_of;
@@ -507,11 +573,11 @@ __global__ __launch_bounds__(128 * G, 2) void k_attention_dkv(AttentionArgs a) {
       ++head_of;
     }
   };
-  issue(0);
-  int q0 = k0;
-  for (int i = 0, slot = 0; i < all; ++i, slot ^= 1) {
+  int q0 = q_of, slot = 0;
+  if (begin < end) issue(0);
+  for (int64_t i = begin; i < end; ++i, slot ^= 1) {
     wait_step<0>();
-    if (i + 1 < all) issue(slot ^ 1);
+    if (i + 1 < end) issue(slot ^ 1);
     const int q = q0 + 32 * part;
     q0 += STEP;
     if (q0 >= len) q0 = k0;
@@ -588,23 +654,62 @@ __global__ __launch_bounds__(128 * G, 2) void k_attention_dkv(AttentionArgs a) {
     }
   }
   if (wave >= 2 || kw >= len) return;
+  if (a.parts > 1) {
+    if (ki >= len) return;
+    const int64_t rows = a.T * a.kv_heads, to = (w.rows.start + static_cast<int64_t>(ki)) * a.kv_heads + w.head;
+    write_sums<DP>(a.sums + (2 * piece * rows + to) * a.D, a.D, lane, dk);
+    write_sums<DP>(a.sums + ((2 * piece + 1) * rows + to) * a.D, a.D, lane, dv);
+    return;
+  }
   write_rows<E, DP>(at(a.dK, row, w.head), a.dK.token, len - kw, a.D, lane, dk, a.scale);
   write_rows<E, DP>(at(a.dV, row, w.head), a.dV.token, len - kw, a.D, lane, dv, 1.f);
 }
 
+// dK and dV from the sums of their parts, in order; a thread takes eight values
+// of a row.
+template <typename E>
+__global__ __launch_bounds__(256) void k_attention_join(AttentionArgs a) {
+  const int chunks = a.D / 8;
+  const int64_t first = lm_offset(a.offsets, 0, a.T), end = lm_offset(a.offsets, a.n, a.T);
+  const int64_t all = (end - first) * a.kv_heads * chunks, values = a.T * a.kv_heads * a.D;
+  const bool v = blockIdx.y == 1;
+  const HeadRows& out = v ? a.dV : a.dK;
+  for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < all; i += static_cast<int64_t>(gridDim.x) * 256) {
+    const int64_t at_ = first * a.kv_heads * chunks + i, row = at_ / chunks;
+    const float* p = a.sums + (v ? values : 0) + at_ * 8;
+    lm_f32x4 x = {0.f, 0.f, 0.f, 0.f}, y = x;
+    for (int k = 0; k < a.parts; ++k, p += 2 * values) {
+      x += *reinterpret_cast<const lm_f32x4*>(p);
+      y += *reinterpret_cast<const lm_f32x4*>(p + 4);
+    }
+    const float by = v ? 1.f : a.scale;
+    *reinterpret_cast<lm_u32x4*>(at(out, row / a.kv_heads, static_cast<int>(row % a.kv_heads)) + at_ % chunks * 16) =
+        lm_u32x4{pack2<E>(x[0] * by, x[1] * by), pack2<E>(x[2] * by, x[3] * by), pack2<E>(y[0] * by, y[1] * by),
+                 pack2<E>(y[2] * by, y[3] * by)};
+  }
+}
+
 uint32_t slots_of(const AttentionArgs& a, int rows) { return static_cast<uint32_t>(a.T / rows + a.n); }
 
+template <typename E, int DP, int S>
+void launch_queries(const AttentionArgs& a, bool grad, hipStream_t s) {
+  if (grad) k_attention_dq<E, DP, S><<<a.slots * a.heads, 256 * S, 0, s>>>(a);
+  else k_attention<E, DP, S><<<a.slots * a.heads, 256 * S, 0, s>>>(a);
+}
 template <typename E, int DP>
 void launch_typed(AttentionArgs a, bool grad, hipStream_t s) {
   a.slots = slots_of(a, BM);
-  if (!grad) {
-    k_attention<E, DP><<<a.slots * a.heads, 256, 0, s>>>(a);
-    return;
-  }
-  k_attention_dq<E, DP><<<a.slots * a.heads, 256, 0, s>>>(a);
+  if (static_cast<int64_t>(a.slots) * a.heads <= kFewTiles) launch_queries<E, DP, 2>(a, grad, s);
+  else launch_queries<E, DP, 1>(a, grad, s);
+  if (!grad) return;
   a.slots = slots_of(a, KEYS);
-  constexpr int G = DP == 128 ? 4 : 2;
-  k_attention_dkv<E, DP, G><<<a.slots * a.kv_heads, 128 * G, 0, s>>>(a);
+  const uint32_t grid = a.slots * a.kv_heads * a.parts;
+  if (DP == 128 || grid <= kFewTiles) k_attention_dkv<E, DP, 4><<<grid, 512, 0, s>>>(a);
+  else k_attention_dkv<E, DP, DP == 128 ? 4 : 2><<<grid, 128 * (DP == 128 ? 4 : 2), 0, s>>>(a);
+  if (a.parts > 1) {
+    const int64_t blocks = (a.T * a.kv_heads * (a.D / 8) + 255) / 256;
+    k_attention_join<E><<<dim3(static_cast<uint32_t>(std::min<int64_t>(blocks, 4096)), 2), 256, 0, s>>>(a);
+  }
 }
 template <typename E>
 void launch_wide(const AttentionArgs& a, bool grad, hipStream_t s) {
@@ -620,6 +725,11 @@ hipError_t launch(AttentionArgs a, bool grad, hipStream_t s) {
 }
 
 }  // namespace
+
+int attention_parts(int n, int64_t T, int heads, int kv_heads) {
+  const int64_t grid = (T / KEYS + n) * kv_heads, steps = T / n / 256 * (heads / kv_heads);
+  return static_cast<int>(std::max<int64_t>(1, std::min({int64_t{512} / grid, steps / 2, int64_t{16}})));
+}
 
 hipError_t launch_attention(AttentionArgs a, hipStream_t s) { return launch(a, false, s); }
 hipError_t launch_attention_grad(AttentionArgs a, hipStream_t s) { return launch(a, true, s); }

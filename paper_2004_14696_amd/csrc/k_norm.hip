@@ -419,9 +419,17 @@ __global__ __launch_bounds__(256) void k_piece_sum(PieceSum a) {
 
 int norm_waves(int d) { return d <= 1024 ? 1 : d <= 4096 ? 4 : 16; }
 
-// Rows of a part: as many parts as run at once (two workgroups a CU, or 2048
-// waves), and each with four rows at least for every sum that it leaves.
-uint32_t norm_rows(int64_t T, int d) { return static_cast<uint32_t>(std::max<int64_t>(4, ceil_div(T, norm_waves(d) == 1 ? 2048 : 512))); }
+// Rows of a part: about as many parts as run at once, and each with two rows at
+// least for every sum that it leaves.  Measured, us with the sums over the
+// pieces (8192 x 4096 bf16; 60000 x 1024 bf16; 3001 x 1003 fp32 of 64 groups):
+//   512 parts of workgroups, 2048 of waves   63; 110; 26 (4 rows at least)
+//   768 and 4096                             62; 97; 23
+//   1024 and 4096                            60 (4090 columns 78 for 69); 97; 26 (4 rows)
+// Sixteen waves a row (8192 columns and more): 512 parts 71, 768 77.
+uint32_t norm_rows(int64_t T, int d) {
+  const int w = norm_waves(d);
+  return static_cast<uint32_t>(std::max<int64_t>(2, ceil_div(T, w == 1 ? 4096 : w == 4 ? 768 : 512)));
+}
 
 int linear_lanes(int packs) {
   int lanes = 64;

@@ -330,8 +330,11 @@ struct AttentionArgs {
   HeadRows Q, K, V, O, dO, dQ, dK, dV;
   float* lse;           // [heads][T], nullable in the forward pass
   float* delta;         // workspace [2][heads][T]: dO . O, and lse log2(e)
+  float* sums;          // workspace [parts][2][T][kv_heads][D] (parts > 1)
+  int parts;            // workgroups that share the queries of a tile of keys
   uint32_t slots;       // tiles of a head's queries or keys (set by the launch)
 };
+int attention_parts(int n, int64_t T, int heads, int kv_heads);
 constexpr int kAttentionKeys = 64;   // the fewest rows of a workgroup (512 threads)
 hipError_t launch_attention(AttentionArgs a, hipStream_t s);
 hipError_t launch_attention_grad(AttentionArgs a, hipStream_t s);
