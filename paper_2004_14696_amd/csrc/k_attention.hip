@@ -180,7 +180,13 @@ __device__ __forceinline__ int place(int r, int h) { return 8 * (r / 4) + 4 * h 
 
 constexpr int BM = 128, BN = 64;       // queries of a workgroup, keys of a stage
 constexpr int KEYS = kAttentionKeys;   // for dK and dV: keys of a workgroup
-constexpr uint32_t kFewTiles = 256;    // workgroups that leave a CU each
+// Workgroups below which eight waves work on a tile rather than four.  Forward,
+// dQ, and dK with dV, us with four and eight waves: 1 sequence of 8192 tokens, 4
+// heads of 64 (260 and 516 workgroups) 110, 159, 137 and 84, 108, 104; 1 of 8192, 8
+// heads of 128 (520) 194, 284 and 154, 212; 16 of 256 tokens, 8 heads of 64 (384 and
+// 640) 12.0, 15.6, 13.7 and 11.6, 16.6, 25: short sequences' keys see too few
+// queries for more than four waves.
+constexpr int64_t kFewTiles = 640;
 
 // What a workgroup works on: rows first .. of a sequence [start, end) and a head.
 struct Work {
@@ -396,27 +402,9 @@ __global__ __launch_bounds__(256 * S, 2) void k_attention_dq(AttentionArgs a) {
   lm_u32x4 q[DP / 16], dy[DP / 16];
   operand<DP>(at(a.Q, row, w.head), a.Q.token, len - qw, a.D, lane, q);
   operand<DP>(at(a.dO, row, w.head), a.dO.token, len - qw, a.D, lane, dy);
-  float delta = 0.f, lse2 = 0.f;
-  {
-    lm_u32x4 y[DP / 16];
-    operand<DP>(at(a.O, row, w.head), a.O.token, len - qw, a.D, lane, y);
-    typedef E V __attribute__((ext_vector_type(8)));
-#pragma unroll
-    for (int kk = 0; kk < DP / 16; ++kk) {
-      const V x = __builtin_bit_cast(V, y[kk]), g = __builtin_bit_cast(V, dy[kk]);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) delta = fmaf(lm_to_f32(x[j]), lm_to_f32(g[j]), delta);
-    }
-    delta = sum_halves(delta);
-    if (qi < len) {
-      const int64_t to = w.head * a.T + w.rows.start + qi;
-      lse2 = a.lse[to] * kLog2E;
-      if (h == 0 && part == 0) {
-        a.delta[to] = delta;
-        a.delta[a.heads * a.T + to] = lse2;
-      }
-    }
-  }
+  const int64_t stat = w.head * a.T + w.rows.start + qi;
+  const float lse2 = qi < len ? a.lse[stat] * kLog2E : 0.f;
+  float delta = 0.f;
   f32x16 dq[DP / 32];
 #pragma unroll
   for (int i = 0; i < DP / 32; ++i) dq[i] = zero16();
@@ -434,44 +422,85 @@ __global__ __launch_bounds__(256 * S, 2) void k_attention_dq(AttentionArgs a) {
     R::load(at(a.K, w.rows.start + static_cast<int64_t>(k0), kv_head), a.K.token, len - k0, a.D, to, all_waves, lane, off_k);
     R::load(at(a.V, w.rows.start + static_cast<int64_t>(k0), kv_head), a.V.token, len - k0, a.D, to + R::BYTES, all_waves, lane, off_v);
   };
-  issue(0, 0);
-  for (int first = 0, slot = 0; first < keys; first += BN * S, slot ^= 1) {
+  // one pass over the keys: for delta alone, or for dQ
+  const auto pass = [&](auto for_delta) {
+    constexpr bool DELTA = decltype(for_delta)::value;
+    issue(0, 0);
+    for (int first = 0, slot = 0; first < keys; first += BN * S, slot ^= 1) {
+      wait_step<0>();
+      if (first + BN * S < keys) issue(first + BN * S, slot ^ 1);
+      const int k0 = first + BN * part;
+      const char* stage = lds + slot * (2 * R::BYTES) + part * (BN * DP * 2);
+      uint32_t p[DP / 32];
+#pragma unroll
+      for (int i = 0; i < DP / 32; ++i) p[i] = pk[i] + slot * (2 * R::BYTES);
+      const auto half = [&](auto which) {
+        constexpr int t = decltype(which)::value;
+        const int k = k0 + 32 * t;
+        if (k > qw + 31 || qw >= len) return;
+        f32x16 s = zero16(), ds = zero16();
+#pragma unroll
+        for (int kk = 0; kk < DP / 16; ++kk) {
+          s = mma(R::row(stage, 32 * t, kk, lane), q[kk], s, E{});
+          ds = mma(R::row(stage + R::BYTES, 32 * t, kk, lane), dy[kk], ds, E{});
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) ds[r] = __builtin_amdgcn_exp2f(fmaf(s[r], scale2, -lse2)) * (DELTA ? ds[r] : ds[r] - delta);
+        if (k + 31 > qw) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            if (k + place(r, h) > qi) ds[r] = 0.f;
+        }
+        if constexpr (DELTA) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) delta += ds[r];
+        } else {
+          lm_u32x4 f[DP / 32];
+          R::template column<32 * t * DP * 2>(p, f);
+          const lm_u32x4 x0 = terms<E>(ds, 0), x1 = terms<E>(ds, 1);
+#pragma unroll
+          for (int i = 0; i < DP / 32; ++i) dq[i] = mma(f[i], x0, dq[i], E{});
+          R::template column<(32 * t + 16) * DP * 2>(p, f);
+#pragma unroll
+          for (int i = 0; i < DP / 32; ++i) dq[i] = mma(f[i], x1, dq[i], E{});
+        }
+      };
+      half(std::integral_constant<int, 0>{});
+      half(std::integral_constant<int, 1>{});
+    }
+  };
+  if (q0 == 0) {
+    // The first queries have few keys, their O is as large as V, and O's rounding
+    // would move delta by as much as dS is rounded: they take delta = sum_s P (dO .
+    // V), a pass over at most two stages of keys (dQ, dK and dV of 100 tokens in
+    // bf16 1.48 times as far from 64 bits as their own rounding, 1.40 so).
+    pass(std::true_type{});
+    delta = sum_halves(delta);
     wait_step<0>();
-    if (first + BN * S < keys) issue(first + BN * S, slot ^ 1);
-    const int k0 = first + BN * part;
-    const char* stage = lds + slot * (2 * R::BYTES) + part * (BN * DP * 2);
-    uint32_t p[DP / 32];
+    if constexpr (S == 2) {
+      float* both = reinterpret_cast<float*>(lds) + lane;
+      both[64 * all_waves] = delta;
+      wait_step<0>();
+      delta = both[64 * wave] + both[64 * (wave + 4)];
+      wait_step<0>();
+    }
+  } else {
+    lm_u32x4 y[DP / 16];
+    operand<DP>(at(a.O, row, w.head), a.O.token, len - qw, a.D, lane, y);
+    typedef E V __attribute__((ext_vector_type(8)));
 #pragma unroll
-    for (int i = 0; i < DP / 32; ++i) p[i] = pk[i] + slot * (2 * R::BYTES);
-    const auto part = [&](auto half) {
-      constexpr int t = decltype(half)::value;
-      const int k = k0 + 32 * t;
-      if (k > qw + 31 || qw >= len) return;
-      f32x16 s = zero16(), ds = zero16();
+    for (int kk = 0; kk < DP / 16; ++kk) {
+      const V x = __builtin_bit_cast(V, y[kk]), g = __builtin_bit_cast(V, dy[kk]);
 #pragma unroll
-      for (int kk = 0; kk < DP / 16; ++kk) {
-        s = mma(R::row(stage, 32 * t, kk, lane), q[kk], s, E{});
-        ds = mma(R::row(stage + R::BYTES, 32 * t, kk, lane), dy[kk], ds, E{});
-      }
-#pragma unroll
-      for (int r = 0; r < 16; ++r) ds[r] = __builtin_amdgcn_exp2f(fmaf(s[r], scale2, -lse2)) * (ds[r] - delta);
-      if (k + 31 > qw) {
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-          if (k + place(r, h) > qi) ds[r] = 0.f;
-      }
-      lm_u32x4 f[DP / 32];
-      R::template column<32 * t * DP * 2>(p, f);
-      const lm_u32x4 x0 = terms<E>(ds, 0), x1 = terms<E>(ds, 1);
-#pragma unroll
-      for (int i = 0; i < DP / 32; ++i) dq[i] = mma(f[i], x0, dq[i], E{});
-      R::template column<(32 * t + 16) * DP * 2>(p, f);
-#pragma unroll
-      for (int i = 0; i < DP / 32; ++i) dq[i] = mma(f[i], x1, dq[i], E{});
-    };
-    part(std::integral_constant<int, 0>{});
-    part(std::integral_constant<int, 1>{});
+      for (int j = 0; j < 8; ++j) delta = fmaf(lm_to_f32(x[j]), lm_to_f32(g[j]), delta);
+    }
+    delta = sum_halves(delta);
   }
+  if (h == 0 && part == 0 && qi < len) {
+    a.delta[stat] = delta;
+    a.delta[a.heads * a.T + stat] = lse2;
+  }
+  pass(std::false_type{});
   if constexpr (S == 2) {
     float* to = reinterpret_cast<float*>(lds) + wave * VALUES * 64 + lane;
     wait_step<0>();
@@ -704,7 +733,7 @@ void launch_typed(AttentionArgs a, bool grad, hipStream_t s) {
   if (!grad) return;
   a.slots = slots_of(a, KEYS);
   const uint32_t grid = a.slots * a.kv_heads * a.parts;
-  if (DP == 128 || grid <= kFewTiles) k_attention_dkv<E, DP, 4><<<grid, 512, 0, s>>>(a);
+  if (DP == 128 || (grid <= kFewTiles && a.T / a.n >= 512)) k_attention_dkv<E, DP, 4><<<grid, 512, 0, s>>>(a);
   else k_attention_dkv<E, DP, DP == 128 ? 4 : 2><<<grid, 128 * (DP == 128 ? 4 : 2), 0, s>>>(a);
   if (a.parts > 1) {
     const int64_t blocks = (a.T * a.kv_heads * (a.D / 8) + 255) / 256;
@@ -726,9 +755,15 @@ hipError_t launch(AttentionArgs a, bool grad, hipStream_t s) {
 
 }  // namespace
 
+// Parts of the queries of a tile of keys: until there are about four workgroups
+// a CU, which then end within a quarter of the time of one another although
+// the first keys of a sequence have all its queries to pass and the last ones
+// none; with two steps of 128 queries at least.  us with 1 part, 512 / grid and
+// 1024 / grid of them (joined): 1 sequence of 8192 tokens, 8 heads on 2 of 128 541,
+// 541, 386; 1 of 4096, 16 heads on 2 of 96 490, 160, 155.
 int attention_parts(int n, int64_t T, int heads, int kv_heads) {
   const int64_t grid = (T / KEYS + n) * kv_heads, steps = T / n / 256 * (heads / kv_heads);
-  return static_cast<int>(std::max<int64_t>(1, std::min({int64_t{512} / grid, steps / 2, int64_t{16}})));
+  return static_cast<int>(std::max<int64_t>(1, std::min({int64_t{1024} / grid, steps / 2, int64_t{16}})));
 }
 
 hipError_t launch_attention(AttentionArgs a, hipStream_t s) { return launch(a, false, s); }

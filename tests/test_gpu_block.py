@@ -601,7 +601,9 @@ def test_attention_and_its_gradients(dtype, lengths, heads, kv, D):
     check_attention(Q[first:T - 4], K[first:T - 4], V[first:T - 4], lengths, scale=0.3)
 
 
-@pytest.mark.parametrize("n,T,heads,kv,D", [(70, 700, 4, 2, 64), (4200, 5000, 1, 1, 32), (9, 4000, 2, 1, 128), (1, 3000, 1, 1, 64)])
+@pytest.mark.parametrize("n,T,heads,kv,D", [(70, 700, 4, 2, 64), (4200, 5000, 1, 1, 32), (9, 4000, 2, 1, 128), (1, 3000, 1, 1, 64),
+                                             (60, 1500, 12, 4, 128), (60, 1500, 12, 12, 80), (2, 1500, 8, 1, 128),
+                                             (300, 2000, 3, 3, 96)])
 def test_attention_of_many_and_long_sequences(n, T, heads, kv, D):
     g = gen(n)
     lengths = ragged(n, n, T)
