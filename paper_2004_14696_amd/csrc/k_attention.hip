@@ -383,6 +383,30 @@ __global__ __launch_bounds__(256 * S, 2) void k_attention(AttentionArgs a) {
     a.lse[w.head * a.T + w.rows.start + qi] = (m * scale2 + __builtin_amdgcn_logf(sum)) * (1.f / kLog2E);
 }
 
+// fp16 has no more than 2^-14 at its full precision, and P and dS of long rows lie
+// around 2^-13 of a gradient: they are rounded, and multiplied, 2^kRaise times
+// as large.  Where dS does not fit then (above 64), a wave goes on without.
+// (8192 tokens in a row, gradients 0.02: dQ, dK and dV 1.5 times as far from 64
+// bits as their own rounding without it.)
+template <typename E>
+constexpr int kRaise = std::is_same_v<E, _Float16> ? 10 : 0;
+constexpr float kMostHalf = 65504.f;
+
+// Whether a lane of the wave has a value above what fp16 holds.
+__device__ __forceinline__ bool too_large(const f32x16& x) {
+  float most = 0.f;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) most = fmaxf(most, fabsf(x[r]));
+  return __any(most > kMostHalf);
+}
+template <int N>
+__device__ __forceinline__ void times(f32x16 (&x)[N], float by) {
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) x[i][r] *= by;
+}
+
 template <typename E, int DP, int S>
 __global__ __launch_bounds__(256 * S, 2) void k_attention_dq(AttentionArgs a) {
   typedef Rows<DP, BN * S, 256 * S> R;
@@ -404,7 +428,7 @@ __global__ __launch_bounds__(256 * S, 2) void k_attention_dq(AttentionArgs a) {
   operand<DP>(at(a.dO, row, w.head), a.dO.token, len - qw, a.D, lane, dy);
   const int64_t stat = w.head * a.T + w.rows.start + qi;
   const float lse2 = qi < len ? a.lse[stat] * kLog2E : 0.f;
-  float delta = 0.f;
+  float delta = 0.f, raise = static_cast<float>(kRaise<E>);
   f32x16 dq[DP / 32];
 #pragma unroll
   for (int i = 0; i < DP / 32; ++i) dq[i] = zero16();
@@ -425,6 +449,7 @@ __global__ __launch_bounds__(256 * S, 2) void k_attention_dq(AttentionArgs a) {
   // one pass over the keys: for delta alone, or for dQ
   const auto pass = [&](auto for_delta) {
     constexpr bool DELTA = decltype(for_delta)::value;
+    float shift = (DELTA ? 0.f : raise) - lse2;
     issue(0, 0);
     for (int first = 0, slot = 0; first < keys; first += BN * S, slot ^= 1) {
       wait_step<0>();
@@ -445,7 +470,7 @@ __global__ __launch_bounds__(256 * S, 2) void k_attention_dq(AttentionArgs a) {
           ds = mma(R::row(stage + R::BYTES, 32 * t, kk, lane), dy[kk], ds, E{});
         }
 #pragma unroll
-        for (int r = 0; r < 16; ++r) ds[r] = __builtin_amdgcn_exp2f(fmaf(s[r], scale2, -lse2)) * (DELTA ? ds[r] : ds[r] - delta);
+        for (int r = 0; r < 16; ++r) ds[r] = __builtin_amdgcn_exp2f(fmaf(s[r], scale2, shift)) * (DELTA ? ds[r] : ds[r] - delta);
         if (k + 31 > qw) {
 #pragma unroll
           for (int r = 0; r < 16; ++r)
@@ -455,6 +480,12 @@ __global__ __launch_bounds__(256 * S, 2) void k_attention_dq(AttentionArgs a) {
 #pragma unroll
           for (int r = 0; r < 16; ++r) delta += ds[r];
         } else {
+          if (kRaise<E> && raise > 0.f && too_large(ds)) {
+            times(dq, 1.f / (1 << kRaise<E>));
+            ds *= 1.f / (1 << kRaise<E>);
+            raise = 0.f;
+            shift = -lse2;
+          }
           lm_u32x4 f[DP / 32];
           R::template column<32 * t * DP * 2>(p, f);
           const lm_u32x4 x0 = terms<E>(ds, 0), x1 = terms<E>(ds, 1);
@@ -498,9 +529,10 @@ __global__ __launch_bounds__(256 * S, 2) void k_attention_dq(AttentionArgs a) {
   }
   if (h == 0 && part == 0 && qi < len) {
     a.delta[stat] = delta;
-    a.delta[a.heads * a.T + stat] = lse2;
+    a.delta[a.heads * a.T + stat] = lse2 - kRaise<E>;
   }
   pass(std::false_type{});
+  if (kRaise<E>) times(dq, raise > 0.f ? 1.f / (1 << kRaise<E>) : 1.f);
   if constexpr (S == 2) {
     float* to = reinterpret_cast<float*>(lds) + wave * VALUES * 64 + lane;
     wait_step<0>();
@@ -570,6 +602,7 @@ __global__ __launch_bounds__(128 * G, 2) void k_attention_dkv(AttentionArgs a) {
   f32x16 dk[DP / 32], dv[DP / 32];
 #pragma unroll
   for (int i = 0; i < DP / 32; ++i) dk[i] = dv[i] = zero16();
+  bool raised = kRaise<E> > 0;
 
   uint32_t off_q[R::CHUNKS], off_d[R::CHUNKS], pq[DP / 32];
 #pragma unroll
@@ -641,6 +674,18 @@ __global__ __launch_bounds__(128 * G, 2) void k_attention_dkv(AttentionArgs a) {
       for (int r = 0; r < 16; ++r)
         if (ki > q + place(r, h) || q + place(r, h) >= len) s[r] = ds[r] = 0.f;
     }
+    if constexpr (kRaise<E> > 0) {
+      constexpr float by = 1.f / (1 << kRaise<E>);
+      if (raised && too_large(ds)) {
+        raised = false;
+        times(dk, by);
+        times(dv, by);
+      }
+      if (!raised) {
+        s *= by;
+        ds *= by;
+      }
+    }
     const auto product = [&](auto at_) {
       constexpr int u = decltype(at_)::value;
       lm_u32x4 f[DP / 32];
@@ -655,6 +700,10 @@ __global__ __launch_bounds__(128 * G, 2) void k_attention_dkv(AttentionArgs a) {
     };
     product(std::integral_constant<int, 0>{});
     product(std::integral_constant<int, 1>{});
+  }
+  if (kRaise<E> > 0 && raised) {
+    times(dk, 1.f / (1 << kRaise<E>));
+    times(dv, 1.f / (1 << kRaise<E>));
   }
   // the sums of the upper half of the waves join the lower half's, until two are left
 #pragma unroll

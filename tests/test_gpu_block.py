@@ -654,6 +654,20 @@ def test_attention_of_growing_large_and_equal_scores(dtype):
     check_attention(Q, K, V, [T], dO, scale=1e-6)
 
 
+def test_attention_gradients_of_any_size_in_fp16():
+    # dS from far below the normal range of fp16 to far above 64, in one call
+    g = gen(16)
+    T, D = 300, 64
+    Q, K, V = normal(g, (T, 4, D), F16), normal(g, (T, 2, D), F16), normal(g, (T, 2, D), F16)
+    dO = normal(g, (T, 4, D), F32)
+    dO[:, 0] *= 1e-3
+    dO[:, 1] *= 300.0
+    dO[150:, 2] *= 2000.0
+    dO[100, 3] *= 500.0
+    check_attention(Q, K, V, [T], dO.to(F16))
+    check_attention(Q, K, V, [40, 200, 60], dO.to(F16))
+
+
 def test_attention_keeps_sequences_apart():
     g = gen(7)
     lengths, T = [40, 100, 3, 90], 233
