@@ -11,6 +11,7 @@ from __future__ import annotations
 import ctypes
 import functools
 import os
+import struct
 from ctypes import POINTER, c_double, c_int32, c_int64, c_size_t, c_uint8, c_uint32, c_uint64, c_void_p
 
 import numpy as np
@@ -230,7 +231,7 @@ def load_library(path: str = LIB_PATH):
     lib.dbw_linear_grad.argtypes = [c_int32, c_int64, c_int32, c_int32, c_int32, P, P, c_int64, P, c_int64, P, c_int64,
                                     P, c_int64, P, c_int64, P]
     lib.dbw_linear_grad.restype = st
-    H = POINTER(Heads)
+    H = P    # dbw_heads: a reference, or its bytes
     lib.dbw_attention.argtypes = [POINTER(AttentionShape), P, H, H, H, H, P, P]
     lib.dbw_attention.restype = st
     lib.dbw_attention_workspace.argtypes = [POINTER(AttentionShape)]
@@ -713,32 +714,46 @@ def group_linear_grad(dY, offsets, pre=None, activation="none", dZ=None, dbias=N
     return dY if own else dZ, dbias
 
 
+_pack_heads = struct.Struct("Pqq").pack
+
+
 def _heads_of(t, shape, dtype, dev, name):
-    """dbw_heads of a tensor [T][heads][D] with contiguous D."""
+    """A dbw_heads of a tensor [T][heads][D] with contiguous D, as bytes."""
     if t.device != dev or t.dtype != dtype or t.shape != shape:
         raise ValueError(f"{name} must be {dtype} {tuple(shape)} on {dev}, not {t.dtype} {tuple(t.shape)} on {t.device}")
     token, head, one = t.stride()
-    if one != 1 and shape[2] > 1:
+    T, heads, D = shape
+    if one != 1 and D > 1:
         raise ValueError(f"the last dimension of {name} must be contiguous")
     # a single head, or a single token, has no stride of its own
-    if shape[1] == 1:
-        head = shape[2]
-    if shape[0] == 1:
-        token = (shape[1] - 1) * head + shape[2] if shape[1] * head < 1 << 21 else shape[2]
-    return Heads(t.data_ptr(), token, head)
+    if heads == 1:
+        head = D
+    if T == 1:
+        token = (heads - 1) * head + D if heads * head < 1 << 21 else D
+    return _pack_heads(t.data_ptr(), token, head)
 
 
-def _attention_shape(torch, Q, K, offsets, scale):
+@functools.lru_cache(maxsize=512)
+def _attention_shape(*values):
+    """A dbw_attention_shape, by reference, and its bytes of workspace."""
+    ref = ctypes.byref(AttentionShape(*values))
+    return ref, load_library().dbw_attention_workspace(ref)
+
+
+def _attention(torch, Q, K, offsets, scale):
+    """What attention and its gradient share: the shape of K, the
+    dbw_attention_shape, its workspace, stream and offsets."""
     if Q.dim() != 3 or K.dim() != 3 or offsets.dim() != 1 or offsets.numel() < 2:
         raise ValueError("Q must be [T][heads][D], K and V [T][kv_heads][D] and offsets [n + 1]")
     T, heads, D = Q.shape
-    n, dev = offsets.numel() - 1, Q.device
+    n, dev, kv = offsets.numel() - 1, Q.device, K.shape[1]
     code = _dtype_code(torch, Q.dtype, "Q", _HALVES)
     raw = _stream_of(torch, dev)
     po = _flat(offsets, (n + 1,), torch.int32, dev, "offsets")
     if scale is None:
         scale = D ** -0.5 if D else 1.0
-    return AttentionShape(code, n, heads, K.shape[1], D, T, scale), raw, po
+    ref, need = _attention_shape(code, n, heads, kv, D, T, scale)
+    return (T, kv, D), ref, need, raw, po
 
 
 def attention(Q, K, V, offsets, scale=None, out=None, lse=None, stream=None):
@@ -752,18 +767,17 @@ def attention(Q, K, V, offsets, scale=None, out=None, lse=None, stream=None):
         return _on(stream, Q.device, attention, Q, K, V, offsets, scale, out, lse)
     torch = _torch()
     lib = load_library()
-    shape, raw, po = _attention_shape(torch, Q, K, offsets, scale)
-    dev, dtype, kv = Q.device, Q.dtype, (shape.T, shape.kv_heads, shape.D)
+    kv, shape, _, raw, po = _attention(torch, Q, K, offsets, scale)
+    dev, dtype, q = Q.device, Q.dtype, Q.shape
     if out is None:
-        out = torch.empty(Q.shape, dtype=dtype, device=dev)
+        out = torch.empty(q, dtype=dtype, device=dev)
     if lse is None or lse is True:
-        lse = torch.empty((shape.heads, shape.T), dtype=torch.float32, device=dev)
+        lse = torch.empty((q[1], q[0]), dtype=torch.float32, device=dev)
     elif lse is False:
         lse = None
-    pl = _flat(lse, (shape.heads, shape.T), torch.float32, dev, "lse") if lse is not None else None
-    arrays = [ctypes.byref(_heads_of(t, s, dtype, dev, name)) for t, s, name in
-              ((Q, Q.shape, "Q"), (K, kv, "K"), (V, kv, "V"), (out, Q.shape, "out"))]
-    _call(torch, lib, dev, lib.dbw_attention, ctypes.byref(shape), po, *arrays, pl, raw)
+    pl = _flat(lse, (q[1], q[0]), torch.float32, dev, "lse") if lse is not None else None
+    _call(torch, lib, dev, lib.dbw_attention, shape, po, _heads_of(Q, q, dtype, dev, "Q"), _heads_of(K, kv, dtype, dev, "K"),
+          _heads_of(V, kv, dtype, dev, "V"), _heads_of(out, q, dtype, dev, "out"), pl, raw)
     return out, lse
 
 
@@ -776,17 +790,20 @@ def attention_grad(dO, Q, K, V, O, lse, offsets, scale=None, dQ=None, dK=None, d
         return _on(stream, Q.device, attention_grad, dO, Q, K, V, O, lse, offsets, scale, dQ, dK, dV, workspace)
     torch = _torch()
     lib = load_library()
-    shape, raw, po = _attention_shape(torch, Q, K, offsets, scale)
-    dev, dtype, kv = Q.device, Q.dtype, (shape.T, shape.kv_heads, shape.D)
-    dQ, dK, dV = (torch.empty(s, dtype=dtype, device=dev) if t is None else t
-                  for t, s in ((dQ, Q.shape), (dK, kv), (dV, kv)))
-    pl = _flat(lse, (shape.heads, shape.T), torch.float32, dev, "lse")
-    dO, Q_, K_, V_, O, *grads = (                                                                        # noqa: E741
-        ctypes.byref(_heads_of(t, s, dtype, dev, name)) for t, s, name in
-        ((dO, Q.shape, "dO"), (Q, Q.shape, "Q"), (K, kv, "K"), (V, kv, "V"), (O, Q.shape, "O"), (dQ, Q.shape, "dQ"),
-         (dK, kv, "dK"), (dV, kv, "dV")))
-    pw, nbytes, keep = _workspace(torch, lib.dbw_attention_workspace(ctypes.byref(shape)), dev, workspace)
-    _call(torch, lib, dev, lib.dbw_attention_grad, ctypes.byref(shape), po, dO, Q_, K_, V_, O, pl, *grads, pw, nbytes, raw)
+    kv, shape, need, raw, po = _attention(torch, Q, K, offsets, scale)
+    dev, dtype, q = Q.device, Q.dtype, Q.shape
+    if dQ is None:
+        dQ = torch.empty(q, dtype=dtype, device=dev)
+    if dK is None:
+        dK = torch.empty(kv, dtype=dtype, device=dev)
+    if dV is None:
+        dV = torch.empty(kv, dtype=dtype, device=dev)
+    pl = _flat(lse, (q[1], q[0]), torch.float32, dev, "lse")
+    pw, nbytes, keep = _workspace(torch, need, dev, workspace)
+    _call(torch, lib, dev, lib.dbw_attention_grad, shape, po, _heads_of(dO, q, dtype, dev, "dO"),
+          _heads_of(Q, q, dtype, dev, "Q"), _heads_of(K, kv, dtype, dev, "K"), _heads_of(V, kv, dtype, dev, "V"),
+          _heads_of(O, q, dtype, dev, "O"), pl, _heads_of(dQ, q, dtype, dev, "dQ"), _heads_of(dK, kv, dtype, dev, "dK"),
+          _heads_of(dV, kv, dtype, dev, "dV"), pw, nbytes, raw)
     return dQ, dK, dV
 
 

@@ -273,9 +273,10 @@ __global__ __launch_bounds__(256 * S, 2) void k_attention(AttentionArgs a) {
   const int kv_head = w.head / (a.heads / a.kv_heads);
   const float scale2 = a.scale * kLog2E;
   const float lim = 8.f / scale2;    // a maximum may grow by 2^8 before sums are scaled
+  const int64_t row = w.rows.first + int64_t{32} * wave;
 
   lm_u32x4 q[DP / 16];
-  operand<DP>(at(a.Q, w.rows.first + 32 * wave, w.head), a.Q.token, len - qw, a.D, lane, q);
+  operand<DP>(at(a.Q, row, w.head), a.Q.token, len - qw, a.D, lane, q);
   f32x16 o[DP / 32];
 #pragma unroll
   for (int i = 0; i < DP / 32; ++i) o[i] = zero16();
@@ -378,7 +379,7 @@ __global__ __launch_bounds__(256 * S, 2) void k_attention(AttentionArgs a) {
       for (int r = 0; r < 16; ++r) o[i][r] = o[i][r] * by0 + to[(2 + i * 16 + r) * 64] * by1;
   }
   if (qw >= len) return;
-  write_rows<E, DP>(at(a.O, w.rows.first + 32 * wave, w.head), a.O.token, len - qw, a.D, lane, o, 1.f / sum);
+  write_rows<E, DP>(at(a.O, row, w.head), a.O.token, len - qw, a.D, lane, o, 1.f / sum);
   if (a.lse && h == 0 && qi < len)
     a.lse[w.head * a.T + w.rows.start + qi] = (m * scale2 + __builtin_amdgcn_logf(sum)) * (1.f / kLog2E);
 }
@@ -421,7 +422,7 @@ __global__ __launch_bounds__(256 * S, 2) void k_attention_dq(AttentionArgs a) {
   const int len = w.rows.end - w.rows.start, q0 = w.rows.first - w.rows.start, qw = q0 + 32 * wave, qi = qw + c;
   const int kv_head = w.head / (a.heads / a.kv_heads);
   const float scale2 = a.scale * kLog2E;
-  const int64_t row = w.rows.first + 32 * wave;
+  const int64_t row = w.rows.first + int64_t{32} * wave;
 
   lm_u32x4 q[DP / 16], dy[DP / 16];
   operand<DP>(at(a.Q, row, w.head), a.Q.token, len - qw, a.D, lane, q);
@@ -587,7 +588,7 @@ __global__ __launch_bounds__(128 * G, 2) void k_attention_dkv(AttentionArgs a) {
   const int len = w.rows.end - w.rows.start, k0 = w.rows.first - w.rows.start, kw = k0 + 32 * (wave % 2), ki = kw + c;
   const int share = a.heads / a.kv_heads;
   const float scale2 = a.scale * kLog2E;
-  const int64_t row = w.rows.first + 32 * (wave % 2);
+  const int64_t row = w.rows.first + int64_t{32} * (wave % 2);
 
   lm_u32x4 k[DP / 16], v[V_IN_LDS ? 1 : DP / 16];
   operand<DP>(at(a.K, row, w.head), a.K.token, len - kw, a.D, lane, k);

@@ -476,21 +476,20 @@ void norm_typed(const NormArgs& a, bool grad, hipStream_t s) {
     if (packs <= 4) return forward<E, 1, 4>(a, s);
     if (packs <= 8) return forward<E, 1, 8>(a, s);
     if (packs <= 16) return forward<E, 4, 4>(a, s);
-    if (packs <= 32) return forward<E, 4, 8>(a, s);
-    return forward<E, 16, 4>(a, s);
+    if constexpr (N == 4)
+      if (packs > 32) return forward<E, 16, 4>(a, s);
+    return forward<E, 4, 8>(a, s);
   }
   const int w = norm_waves(a.d);
   const int packs = static_cast<int>(ceil_div(a.d, N * 64 * w));
   if constexpr (N == 4) {
-    if (packs > 2) {
-      if (w == 1) return backward<E, 1, 4>(a, s);
-      if (w == 4) return backward<E, 4, 4>(a, s);
-      return backward<E, 16, 4>(a, s);
-    }
+    if (packs > 2) return w == 1 ? backward<E, 1, 4>(a, s) : w == 4 ? backward<E, 4, 4>(a, s) : backward<E, 16, 4>(a, s);
+    if (w > 1) return w == 4 ? backward<E, 4, 2>(a, s) : backward<E, 16, 2>(a, s);   // (more than one pack each)
+  } else {
+    if (w == 4) return packs > 1 ? backward<E, 4, 2>(a, s) : backward<E, 4, 1>(a, s);
+    if (w == 16) return packs > 1 ? backward<E, 16, 2>(a, s) : backward<E, 16, 1>(a, s);
   }
-  if (w == 1) return packs > 1 ? backward<E, 1, 2>(a, s) : backward<E, 1, 1>(a, s);
-  if (w == 4) return packs > 1 ? backward<E, 4, 2>(a, s) : backward<E, 4, 1>(a, s);
-  return packs > 1 ? backward<E, 16, 2>(a, s) : backward<E, 16, 1>(a, s);
+  return packs > 1 ? backward<E, 1, 2>(a, s) : backward<E, 1, 1>(a, s);
 }
 
 void norm(const NormArgs& a, bool grad, hipStream_t s) {

@@ -946,6 +946,22 @@ def test_calls_on_another_stream_give_the_same_bits():
         assert torch.equal(a, b)
 
 
+def test_calls_without_rows():
+    off, w = offsets_of([0, 0]), torch.ones(64, device="cuda")
+    X, Q = torch.empty((0, 64), dtype=BF16, device="cuda"), torch.empty((0, 4, 16), dtype=BF16, device="cuda")
+    assert pb.layer_norm(X, w, w, off).shape == (0, 64)
+    dX, dg, db = pb.layer_norm_grad(X, X, w, off, dgamma=torch.full((2, 64), 3.0, device="cuda"))
+    assert dX.shape == (0, 64) and bool((dg == 0).all()) and bool((db == 0).all())
+    Y, Z = pb.group_linear(X, torch.zeros((64, 8), dtype=BF16, device="cuda"), off, activation="gelu", pre=True)
+    assert Y.shape == Z.shape == (0, 8)
+    dZ, db = pb.group_linear_grad(X, off, pre=X, activation="gelu")
+    assert dZ.shape == (0, 64) and bool((db == 0).all())
+    assert pb.dropout(X, 0.5, 1, off).shape == (0, 64)
+    O, lse = pb.attention(Q, Q, Q, off)                                                                    # noqa: E741
+    assert O.shape == Q.shape and [x.shape for x in pb.attention_grad(Q, Q, Q, Q, O, lse, off)] == [Q.shape] * 3
+    torch.cuda.synchronize()
+
+
 def test_offsets_that_break_the_rules_stay_inside():
     # results are unspecified; nothing outside the arrays is touched
     g = gen(23)
