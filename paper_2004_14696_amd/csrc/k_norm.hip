@@ -30,21 +30,25 @@ struct Pack {
 // The columns of pack number p of a row of d values.  A row's last pack is its
 // last N values: the first of them may be the pack's before, which computes the
 // same for them; sums over a row leave them out.  Rows of fewer than N values are
-// one pack.  WHOLE: d is a multiple of N.
+// one pack.  WHOLE: d is a multiple of N.  Only where `last` is true may the pack
+// be the row's last one, or behind it.
 template <int N, bool WHOLE = false>
 struct Place {
   int base, end;   // `end` values from base on
   uint32_t mask;   // those of them that are the pack's own
-  __device__ __forceinline__ Place(int p, int d) {
-    base = p * N;
-    end = base < d ? N : 0;
+  bool wide;       // rows have N values at least
+  __device__ __forceinline__ Place(int p, int d, bool last = true) : base(p * N), end(N), wide(true) {
     int skip = 0;
-    if (!WHOLE && end && base + N > d) {
-      if (d >= N) {
-        skip = base + N - d;
-        base = d - N;
-      } else {
-        end = d;
+    if (last) {
+      wide = WHOLE || d >= N;
+      end = base < d ? N : 0;
+      if (!WHOLE && end && base + N > d) {
+        if (d >= N) {
+          skip = base + N - d;
+          base = d - N;
+        } else {
+          end = d;
+        }
       }
     }
     mask = (1u << end) - (1u << skip);
@@ -54,16 +58,18 @@ struct Place {
     return WHOLE ? 1.f : __builtin_bit_cast(float, static_cast<uint32_t>(static_cast<int32_t>(mask << (31 - j)) >> 31) & 0x3f800000u);
   }
   __device__ __forceinline__ bool full() const { return WHOLE || end == N; }
+  __device__ __forceinline__ bool vectors() const { return wide; }
 };
 
+// Loads are the same for packs behind the row's end, which read its start and
+// get zeros: a branch around each would make them wait for one another.
 template <typename E, typename P>
 __device__ __forceinline__ Pack<E> load(const E* row, const P& p) {
   constexpr int N = Pack<E>::N;
   Pack<E> x;
-  x.v = lm_u32x4{0, 0, 0, 0};
-  if (p.end == 0) return x;
-  if (p.full()) {
-    x.v = *reinterpret_cast<const lm_u32x4_any*>(row + p.base);
+  if (p.vectors()) {
+    const lm_u32x4 v = *reinterpret_cast<const lm_u32x4_any*>(row + (p.end ? p.base : 0));
+    x.v = p.end ? v : lm_u32x4{0, 0, 0, 0};
   } else {
     typename Pack<E>::V v;
 #pragma unroll
@@ -93,10 +99,11 @@ __device__ __forceinline__ void store(E* row, const P& p, const float (&y)[Pack<
 // N fp32 values from (to) p.base of a vector of weights.
 template <int N, typename P>
 __device__ __forceinline__ void load_f32(const float* w, const P& p, float (&x)[N]) {
-  if (p.full()) {
+  if (p.vectors()) {
+    const float* at = w + (p.end ? p.base : 0);
 #pragma unroll
     for (int j = 0; j < N; j += 4) {
-      const lm_f32x4 v = *reinterpret_cast<const lm_f32x4_any*>(w + p.base + j);
+      const lm_f32x4 v = *reinterpret_cast<const lm_f32x4_any*>(at + j);
 #pragma unroll
       for (int k = 0; k < 4; ++k) x[j + k] = v[k];
     }
@@ -155,16 +162,32 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_norm(NormArgs a) {
   const auto row = [&](int64_t t, Pack<E>(&x)[PACKS]) {
     const E* p = static_cast<const E*>(a.X) + t * a.ld_X;
 #pragma unroll
-    for (int i = 0; i < PACKS; ++i) x[i] = load<E>(p, P(tid + i * W * 64, a.d));
+    for (int i = 0; i < PACKS; ++i) x[i] = load<E>(p, P(tid + i * W * 64, a.d, i == PACKS - 1));
+  };
+  // the weights stay in registers where they fit
+  constexpr bool HELD = PACKS <= 2;
+  float g[HELD ? PACKS : 1][N], b[HELD ? PACKS : 1][N];
+  const auto weights = [&](int i, float(&g)[N], float(&b)[N]) {
+    const P p(tid + i * W * 64, a.d, i == PACKS - 1);
+    load_f32<N>(a.gamma, p, g);
+    if (a.beta) {
+      load_f32<N>(a.beta, p, b);
+    } else {
+#pragma unroll
+      for (int j = 0; j < N; ++j) b[j] = 0.f;
+    }
   };
   Pack<E> x[PACKS], next[PACKS];
   if (t < end) row(t, x);
+  if constexpr (HELD)
+#pragma unroll
+    for (int i = 0; i < PACKS; ++i) weights(i, g[i], b[i]);
   for (; t < end; t += step) {
     if (t + step < end) row(t + step, next);
     float sum[1] = {0.f};
 #pragma unroll
     for (int i = 0; i < PACKS; ++i) {
-      const P p(tid + i * W * 64, a.d);
+      const P p(tid + i * W * 64, a.d, i == PACKS - 1);
 #pragma unroll
       for (int j = 0; j < N; ++j) sum[0] = WHOLE ? sum[0] + x[i][j] : fmaf(x[i][j], p.own(j), sum[0]);
     }
@@ -173,29 +196,27 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_norm(NormArgs a) {
     float sq[1] = {0.f};
 #pragma unroll
     for (int i = 0; i < PACKS; ++i) {
-      const P p(tid + i * W * 64, a.d);
-      if (p.end == 0) continue;
+      const P p(tid + i * W * 64, a.d, i == PACKS - 1);
+      float part = 0.f;
 #pragma unroll
       for (int j = 0; j < N; ++j) {
         const float c = WHOLE ? x[i][j] - mean : (x[i][j] - mean) * p.own(j);
-        sq[0] = fmaf(c, c, sq[0]);
+        part = fmaf(c, c, part);
       }
+      sq[0] += p.end ? part : 0.f;
     }
     row_sum<W, 1>(sq, lds, turn);
     const float r = 1.f / sqrtf(fmaf(sq[0], over_d, a.eps));
     E* out = static_cast<E*>(a.out) + t * a.ld_out;
 #pragma unroll
     for (int i = 0; i < PACKS; ++i) {
-      const P p(tid + i * W * 64, a.d);
-      if (p.end == 0) continue;
-      float g[N], b[N], y[N];
-      load_f32<N>(a.gamma, p, g);
+      const P p(tid + i * W * 64, a.d, i == PACKS - 1);
+      const int k = HELD ? i : 0;
+      if (!HELD) weights(i, g[0], b[0]);
+      float y[N];
 #pragma unroll
-      for (int j = 0; j < N; ++j) b[j] = 0.f;
-      if (a.beta) load_f32<N>(a.beta, p, b);
-#pragma unroll
-      for (int j = 0; j < N; ++j) y[j] = fmaf((x[i][j] - mean) * r, g[j], b[j]);
-      store<E>(out, p, y);
+      for (int j = 0; j < N; ++j) y[j] = fmaf((x[i][j] - mean) * r, g[k][j], b[k][j]);
+      if (p.end) store<E>(out, p, y);
     }
 #pragma unroll
     for (int i = 0; i < PACKS; ++i) x[i] = next[i];
@@ -247,11 +268,14 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_norm_grad(NormArgs a)
     const E* q = static_cast<const E*>(a.dY) + t * a.ld_dY;
 #pragma unroll
     for (int i = 0; i < PACKS; ++i) {
-      const P at(tid + i * W * 64, a.d);
+      const P at(tid + i * W * 64, a.d, i == PACKS - 1);
       x[i] = load<E>(p, at);
       dy[i] = load<E>(q, at);
     }
   };
+  float g[PACKS][N];
+#pragma unroll
+  for (int i = 0; i < PACKS; ++i) load_f32<N>(a.gamma, P(tid + i * W * 64, a.d, i == PACKS - 1), g[i]);
   pieces(a.offsets, a.n, a.T, a.rows, part, [&](int group, int64_t first, int64_t last) {
 #pragma unroll
     for (int i = 0; i < PACKS; ++i)
@@ -264,7 +288,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_norm_grad(NormArgs a)
       float sum[1] = {0.f};
 #pragma unroll
       for (int i = 0; i < PACKS; ++i) {
-        const P p(tid + i * W * 64, a.d);
+        const P p(tid + i * W * 64, a.d, i == PACKS - 1);
 #pragma unroll
         for (int j = 0; j < N; ++j) sum[0] = WHOLE ? sum[0] + x[i][j] : fmaf(x[i][j], p.own(j), sum[0]);
       }
@@ -274,17 +298,16 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_norm_grad(NormArgs a)
       float s[3] = {0.f, 0.f, 0.f};
 #pragma unroll
       for (int i = 0; i < PACKS; ++i) {
-        const P p(tid + i * W * 64, a.d);
-        if (p.end == 0) continue;
-        float g[N];
-        load_f32<N>(a.gamma, p, g);
+        const P p(tid + i * W * 64, a.d, i == PACKS - 1);
+        float part = 0.f;
 #pragma unroll
         for (int j = 0; j < N; ++j) {
-          const float c = WHOLE ? x[i][j] - mean : (x[i][j] - mean) * p.own(j), h = dy[i][j] * g[j];
-          s[0] = fmaf(c, c, s[0]);
+          const float c = WHOLE ? x[i][j] - mean : (x[i][j] - mean) * p.own(j), h = dy[i][j] * g[i][j];
+          part = fmaf(c, c, part);
           s[1] = WHOLE ? s[1] + h : fmaf(h, p.own(j), s[1]);
           s[2] = fmaf(h, c, s[2]);
         }
+        s[0] += p.end ? part : 0.f;   // (dY is 0 behind the end)
       }
       row_sum<W, 3>(s, lds, turn);
       const float r = 1.f / sqrtf(fmaf(s[0], over_d, a.eps));
@@ -292,18 +315,16 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_norm_grad(NormArgs a)
       E* out = static_cast<E*>(a.out) + t * a.ld_out;
 #pragma unroll
       for (int i = 0; i < PACKS; ++i) {
-        const P p(tid + i * W * 64, a.d);
-        if (p.end == 0) continue;
-        float g[N], y[N];
-        load_f32<N>(a.gamma, p, g);
+        const P p(tid + i * W * 64, a.d, i == PACKS - 1);
+        float y[N];
 #pragma unroll
         for (int j = 0; j < N; ++j) {
           const float h = (x[i][j] - mean) * r, d = dy[i][j];
           dg[i][j] = fmaf(d, h, dg[i][j]);
           db[i][j] += d;
-          y[j] = r * (fmaf(-h, m2, fmaf(d, g[j], -m1)));
+          y[j] = r * (fmaf(-h, m2, fmaf(d, g[i][j], -m1)));
         }
-        store<E>(out, p, y);
+        if (p.end) store<E>(out, p, y);
       }
 #pragma unroll
       for (int i = 0; i < PACKS; ++i) {
@@ -315,7 +336,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_norm_grad(NormArgs a)
     float* sums = a.parts + (part + group) * ld;
 #pragma unroll
     for (int i = 0; i < PACKS; ++i) {
-      const P p(tid + i * W * 64, a.d);
+      const P p(tid + i * W * 64, a.d, i == PACKS - 1);
       if (p.end == 0) continue;
       store_f32<N>(sums, p, dg[i]);
       if (a.dbeta) store_f32<N>(sums + (static_cast<int64_t>(a.parts_of_rows) + a.n) * ld, p, db[i]);
@@ -450,19 +471,24 @@ void launch_piece_sum(const PieceSum& c, hipStream_t s) {
   k_piece_sum<<<grid, 256, 0, s>>>(c);
 }
 
-template <typename E, int W, int PACKS>
-void forward(const NormArgs& a, hipStream_t s) {
+// The kernels with `packs` packs a thread, of FROM to TO.
+template <typename E, int W, int FROM, int TO>
+void forward(const NormArgs& a, int packs, hipStream_t s) {
+  if constexpr (FROM < TO)
+    if (packs > FROM) return forward<E, W, FROM + 1, TO>(a, packs, s);
   constexpr int TEAMS = W == 1 ? 4 : 1, THREADS = W == 1 ? 256 : 64 * W;
   const uint32_t grid = static_cast<uint32_t>(std::min<int64_t>(W == 16 ? 512 : 2048, ceil_div(a.T, TEAMS)));
-  if (a.d % Pack<E>::N == 0) k_norm<E, W, PACKS, true><<<grid, THREADS, 0, s>>>(a);
-  else k_norm<E, W, PACKS, false><<<grid, THREADS, 0, s>>>(a);
+  if (a.d % Pack<E>::N == 0) k_norm<E, W, FROM, true><<<grid, THREADS, 0, s>>>(a);
+  else k_norm<E, W, FROM, false><<<grid, THREADS, 0, s>>>(a);
 }
-template <typename E, int W, int PACKS>
-void backward(const NormArgs& a, hipStream_t s) {
+template <typename E, int W, int FROM, int TO>
+void backward(const NormArgs& a, int packs, hipStream_t s) {
+  if constexpr (FROM < TO)
+    if (packs > FROM) return backward<E, W, FROM + 1, TO>(a, packs, s);
   constexpr int TEAMS = W == 1 ? 4 : 1, THREADS = W == 1 ? 256 : 64 * W;
   const uint32_t grid = static_cast<uint32_t>(ceil_div(a.parts_of_rows, TEAMS));
-  if (a.d % Pack<E>::N == 0) k_norm_grad<E, W, PACKS, true><<<grid, THREADS, 0, s>>>(a);
-  else k_norm_grad<E, W, PACKS, false><<<grid, THREADS, 0, s>>>(a);
+  if (a.d % Pack<E>::N == 0) k_norm_grad<E, W, FROM, true><<<grid, THREADS, 0, s>>>(a);
+  else k_norm_grad<E, W, FROM, false><<<grid, THREADS, 0, s>>>(a);
 }
 
 template <typename E>
@@ -471,25 +497,16 @@ void norm_typed(const NormArgs& a, bool grad, hipStream_t s) {
   if (!grad) {
     // a wave to a row as far as its registers hold one: no barriers
     const int packs = static_cast<int>(ceil_div(a.d, N * 64));
-    if (packs <= 1) return forward<E, 1, 1>(a, s);
-    if (packs <= 2) return forward<E, 1, 2>(a, s);
-    if (packs <= 4) return forward<E, 1, 4>(a, s);
-    if (packs <= 8) return forward<E, 1, 8>(a, s);
-    if (packs <= 16) return forward<E, 4, 4>(a, s);
+    if (packs <= 8) return forward<E, 1, 1, 8>(a, packs, s);
     if constexpr (N == 4)
-      if (packs > 32) return forward<E, 16, 4>(a, s);
-    return forward<E, 4, 8>(a, s);
+      if (packs > 32) return forward<E, 16, 3, 4>(a, (packs + 15) / 16, s);
+    return forward<E, 4, 3, 8>(a, (packs + 3) / 4, s);
   }
-  const int w = norm_waves(a.d);
-  const int packs = static_cast<int>(ceil_div(a.d, N * 64 * w));
-  if constexpr (N == 4) {
-    if (packs > 2) return w == 1 ? backward<E, 1, 4>(a, s) : w == 4 ? backward<E, 4, 4>(a, s) : backward<E, 16, 4>(a, s);
-    if (w > 1) return w == 4 ? backward<E, 4, 2>(a, s) : backward<E, 16, 2>(a, s);   // (more than one pack each)
-  } else {
-    if (w == 4) return packs > 1 ? backward<E, 4, 2>(a, s) : backward<E, 4, 1>(a, s);
-    if (w == 16) return packs > 1 ? backward<E, 16, 2>(a, s) : backward<E, 16, 1>(a, s);
-  }
-  return packs > 1 ? backward<E, 1, 2>(a, s) : backward<E, 1, 1>(a, s);
+  const int w = norm_waves(a.d), packs = static_cast<int>(ceil_div(a.d, N * 64 * w));
+  constexpr int LEAST = N == 4 ? 2 : 1, MOST = N == 4 ? 4 : 2;    // (more than 1024, or 4096, values)
+  if (w == 1) return backward<E, 1, 1, MOST>(a, packs, s);
+  if (w == 4) return backward<E, 4, LEAST, MOST>(a, packs, s);
+  return backward<E, 16, LEAST, MOST>(a, packs, s);
 }
 
 void norm(const NormArgs& a, bool grad, hipStream_t s) {
