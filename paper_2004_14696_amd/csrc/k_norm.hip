@@ -165,7 +165,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_norm(NormArgs a) {
     for (int i = 0; i < PACKS; ++i) x[i] = load<E>(p, P(tid + i * W * 64, a.d, i == PACKS - 1));
   };
   // the weights stay in registers where they fit
-  constexpr bool HELD = PACKS <= 2;
+  constexpr bool HELD = PACKS * N <= 32;
   float g[HELD ? PACKS : 1][N], b[HELD ? PACKS : 1][N];
   const auto weights = [&](int i, float(&g)[N], float(&b)[N]) {
     const P p(tid + i * W * 64, a.d, i == PACKS - 1);
@@ -497,10 +497,11 @@ void norm_typed(const NormArgs& a, bool grad, hipStream_t s) {
   if (!grad) {
     // a wave to a row as far as its registers hold one: no barriers
     const int packs = static_cast<int>(ceil_div(a.d, N * 64));
-    if (packs <= 8) return forward<E, 1, 1, 8>(a, packs, s);
+    constexpr int MOST = N == 4 ? 8 : 4;
+    if (packs <= MOST) return forward<E, 1, 1, MOST>(a, packs, s);
     if constexpr (N == 4)
       if (packs > 32) return forward<E, 16, 3, 4>(a, (packs + 15) / 16, s);
-    return forward<E, 4, 3, 8>(a, (packs + 3) / 4, s);
+    return forward<E, 4, N == 4 ? 3 : 2, 8>(a, (packs + 3) / 4, s);
   }
   const int w = norm_waves(a.d), packs = static_cast<int>(ceil_div(a.d, N * 64 * w));
   constexpr int LEAST = N == 4 ? 2 : 1, MOST = N == 4 ? 4 : 2;    // (more than 1024, or 4096, values)
