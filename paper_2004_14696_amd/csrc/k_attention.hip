@@ -14,6 +14,29 @@
 // V^T P^T without any exchange, when V's transposing loads take the same keys.
 // The gradients do the same with K^T, and, with keys for queries, with Q^T and
 // dO^T.
+//
+// A pass over the keys keeps the running maximum and sum of a query; sums are
+// scaled only when a maximum has grown by 2^8 (a wave then spends 64 products on
+// it; on random rows, in the first stages alone).  The gradients form S and dO V^T
+// once for dQ and once for dK and dV, seven products for five: dK and dV, and dQ,
+// are then sums of one workgroup in a fixed order, without atomics or arrays of T x T
+// (a workgroup for keys that adds to dQ would need fp32 atomics whose order is
+// not fixed).
+//
+// What bounds it.  Long sequences: the matrix cores at the clock they hold under
+// load; 1 sequence of 16384 tokens, 8 heads on 2 of 128, forward 547 to 576 us, 955 to
+// 1005 TFLOP/s (a library product 1244), dQ 775 us, 1060 TFLOP/s, dK and dV 1334 us, 825
+// TFLOP/s.  Vector work, 150 instructions and 32 exponentials for 32 products, runs
+// beside the products of the other wave of a SIMD only in part (cores busy 60% of
+// the cycles).  Ragged batches: the tiles on the diagonal, start and end of each
+// workgroup, and the last of them; 8 sequences, 8192 tokens, 16 heads on 4 of 128: 60,
+// 87 and 133 us, 680, 700 and 610 TFLOP/s, cores busy 32 to 38%.  Short sequences: the chain
+// from offsets to keys to products, some 5 us a workgroup (50 sequences, 5000 tokens,
+// 12 heads of 80, fp16: 15, 26 and 28 us).  LDS is read without conflicts (with lines
+// turned for 32 banks half of its cycles were), its reads are builtins so that the
+// compiler places their waits.  Tried, no gain: the priority of waves raised for
+// products.  Not tried: softmax of one stage beside the products of the next
+// within a wave, for which 256 registers do not hold 128 values a head.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -199,7 +222,7 @@ struct Work {
 // pass first: workgroups start in the order of their numbers, and with the
 // longest at the end the others would wait for them (8 sequences of 8192 tokens,
 // 16 heads on 4 of 128: 72, 107 and 173 us for the three kernels with tiles in
-// the sequences' order, SORTED_US with this one).  With w the tiles to pass, its
+// the sequences' order, 64, 95 and 142 with this one and LDS free of conflicts).  With w the tiles to pass, its
 // own included, the tiles with w or more are sum_i max(0, tiles_i - w + 1).
 // kSorted sequences at most: beyond, chunks in the sequences' order.
 constexpr int kSorted = 256;

@@ -1,5 +1,10 @@
 // Dropout with the residual's addition; the mask is drawn again wherever it is
-// needed, from a counter: eight values of a row take one Philox4x32-10 block.
+// needed, from a counter: eight values of a row take one Philox4x32-10 block, 16
+// bits each.
+//
+// Bound by memory: 16384 x 4096 bf16 with a residual 73 us, 5.5 TB/s.  The 20
+// products of 32 by 32 bits of a block, 16 cycles each, are a quarter of the time that
+// memory takes for a wave's 512 values; with 32 bits a value they would be half.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
