@@ -426,7 +426,7 @@ def _on(stream, dev, function, *args, **kw):
 
 def _call(torch, lib, dev, function, *args):
     """function(*args) with `dev` as the current device; raises its error."""
-    if torch.cuda.current_device() == dev.index:
+    if torch._C._cuda_getDevice() == dev.index:     # (with a tensor on a GPU, torch's runtime is set up)
         st = function(*args)
     else:
         with torch.cuda.device(dev):
