@@ -615,8 +615,10 @@ dbw_status dbw_linear_grad(int32_t n, int64_t T, int32_t C, int32_t dtype, int32
  * Products take bf16 or fp16 and sum in fp32; the exponentials are rounded to
  * dtype for the second product, and summed unrounded.  Arrays are DEVICE
  * [T][heads or kv_heads][D] of dtype, the D values contiguous; lse is DEVICE
- * float [heads][T], or NULL.  NaN and infinities of a row may reach all rows of
- * its sequence. */
+ * float [heads][T], or NULL.  Q . K and S have to be finite in fp32, and may be
+ * of any size there; a weight's relative error is that of its S, the rounding of
+ * a sum of D products in fp32.  NaN and infinities of a row may reach all rows
+ * of its sequence. */
 typedef struct {
   void* data;             /* 16-byte aligned                                 */
   int64_t token, head;    /* elements from a token, or a head, to the next:

@@ -210,6 +210,15 @@ constexpr int KEYS = kAttentionKeys;   // for dK and dV: keys of a workgroup
 // 640) 12.0, 15.6, 13.7 and 11.6, 16.6, 25: short sequences' keys see too few
 // queries for more than four waves.
 constexpr int64_t kFewTiles = 640;
+// Largest size of a maximum, as an exponent of 2, up to which exponents are
+// formed as S scale log2(e) - x with a rounded x = m scale log2(e), in one
+// instruction: x is off by 2^-15 then.  Beyond, that would tell: 2^-4 at 2^21,
+// where a row's terms have different x; above 2^28 fp16 cannot hold P, and above
+// 2^31 exponentials are infinite or all 0.  A wave with such a row subtracts
+// before it scales, (S - m) scale log2(e), in one instruction more.  The times of
+// ordinary rows are the same with and without (16384 tokens 541 us).
+constexpr float kFar = 1024.f;
+constexpr float kLn2 = 0.693147180559945309f;
 
 // What a workgroup works on: rows first .. of a sequence [start, end) and a head.
 struct Work {
@@ -296,6 +305,7 @@ __global__ __launch_bounds__(256 * S, 2) void k_attention(AttentionArgs a) {
   const int kv_head = w.head / (a.heads / a.kv_heads);
   const float scale2 = a.scale * kLog2E;
   const float lim = 8.f / scale2;    // a maximum may grow by 2^8 before sums are scaled
+  bool far = false;                  // whether a maximum of the wave's lies beyond kFar
   const int64_t row = w.rows.first + int64_t{32} * wave;
 
   lm_u32x4 q[DP / 16];
@@ -351,7 +361,7 @@ __global__ __launch_bounds__(256 * S, 2) void k_attention(AttentionArgs a) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[t][r]);
     mx = max_halves(mx);
-    if (__any(mx > m + lim)) {
+    if (__any(mx - m > lim)) {   // (a sum m + lim rounds by more than lim where m is large)
       const float top = fmaxf(m, mx), by = __builtin_amdgcn_exp2f((m - top) * scale2);
       m = top;
       sum *= by;
@@ -359,8 +369,15 @@ __global__ __launch_bounds__(256 * S, 2) void k_attention(AttentionArgs a) {
       for (int i = 0; i < DP / 32; ++i)
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[i][r] *= by;
+      far = __any(!(fabsf(m * scale2) <= kFar));
     }
-    const float m2 = m * scale2;
+    if (far) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[t][r] -= m;
+    }
+    const float m2 = far ? 0.f : m * scale2;
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -412,7 +429,7 @@ __global__ __launch_bounds__(256 * S, 2) void k_attention(AttentionArgs a) {
   if (qw >= len) return;
   write_rows<E, DP>(at(a.O, row, w.head), a.O.token, len - qw, a.D, lane, o, 1.f / sum);
   if (a.lse && h == 0 && qi < len)
-    a.lse[w.head * a.T + w.rows.start + qi] = (m * scale2 + __builtin_amdgcn_logf(sum)) * (1.f / kLog2E);
+    a.lse[w.head * a.T + w.rows.start + qi] = fmaf(m, a.scale, __builtin_amdgcn_logf(sum) * kLn2);
 }
 
 // fp16 has no more than 2^-14 at its full precision, and P and dS of long rows lie
