@@ -616,8 +616,8 @@ dbw_status dbw_linear_grad(int32_t n, int64_t T, int32_t C, int32_t dtype, int32
  * dtype for the second product, and summed unrounded.  Arrays are DEVICE
  * [T][heads or kv_heads][D] of dtype, the D values contiguous; lse is DEVICE
  * float [heads][T], or NULL.  Q . K and S have to be finite in fp32, and may be
- * of any size there; a weight's relative error is that of its S, the rounding of
- * a sum of D products in fp32.  NaN and infinities of a row may reach all rows
+ * of any size there; a weight is off by the factor exp(error of S), S being a
+ * sum of D products in fp32.  NaN and infinities of a row may reach all rows
  * of its sequence. */
 typedef struct {
   void* data;             /* 16-byte aligned                                 */
@@ -641,7 +641,9 @@ dbw_status dbw_attention(const dbw_attention_shape* shape, const int32_t* offset
  *   dS[t][s] = P[t][s] (dO[t] . V[s] - dO[t] . O[t]),
  *   dQ[t] = scale sum_s dS[t][s] K[s],   dK[s] = scale sum_t dS[t][s] Q[t]
  * with dK and dV summed over the heads that share them, in a fixed order.  P
- * and dS are rounded to dtype for the products.  workspace: at least
+ * and dS are rounded to dtype for the products.  Where |lse| is above 709 for a
+ * row, its 128 take maximum and sum from Q and K again, as lse does not hold
+ * exp(S - lse) to its last digits there.  workspace: at least
  * dbw_attention_workspace bytes (-1 for a shape out of range). */
 int64_t dbw_attention_workspace(const dbw_attention_shape* shape);
 dbw_status dbw_attention_grad(const dbw_attention_shape* shape, const int32_t* offsets, const dbw_heads* dO,

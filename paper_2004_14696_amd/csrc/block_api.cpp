@@ -254,8 +254,8 @@ DBW_API dbw_status dbw_attention(const dbw_attention_shape* shape, const int32_t
 }
 
 namespace {
-// delta and lse of every query; and the parts' sums
-int64_t delta_bytes(const dbw_attention_shape& p) { return (int64_t{8} * p.heads * p.T + 15) / 16 * 16; }
+// delta, lse and maximum of every query; and the parts' sums
+int64_t delta_bytes(const dbw_attention_shape& p) { return (int64_t{12} * p.heads * p.T + 15) / 16 * 16; }
 int64_t sum_bytes(const dbw_attention_shape& p) {
   const int64_t parts = dbw::attention_parts(p.n, p.T, p.heads, p.kv_heads);
   return parts > 1 ? parts * 8 * p.T * p.kv_heads * p.D : 0;

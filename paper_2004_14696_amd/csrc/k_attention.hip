@@ -88,6 +88,12 @@ struct Rows {
   static constexpr int LINE = DP / 8;                     // chunks of a line
   static constexpr int CHUNKS = ROWS * LINE / THREADS;    // a thread
   static constexpr int BYTES = ROWS * DP * 2;
+  // With 128 values, a thread's chunks lie whole periods of turn() apart: one offset
+  // does, with a scalar one, and four registers fewer keep dK and dV's loop free of
+  // scratch (8192 tokens, 16 heads on 4, fp16: 173 -> 152 us; with 64 values registers
+  // suffice, and the scalar ones would not).
+  static constexpr bool EVEN = DP == 128 && THREADS / LINE % 16 == 0;
+  static constexpr int OFFSETS = EVEN ? 1 : CHUNKS;
   static_assert(DP == 64 || DP == 96 || DP == 128, "turn() is for these");
   static_assert(ROWS * LINE % THREADS == 0, "whole chunks a thread");
   static __device__ __forceinline__ int turn(int line) {
@@ -101,11 +107,13 @@ struct Rows {
     return line < left && chunk * 8 < D ? static_cast<uint32_t>(line * token * 2 + chunk * 16) : kOutOfRange;
   }
   static __device__ __forceinline__ void load(const char* p, int64_t token, int left, int D, char* lds, int wave,
-                                              int lane, const uint32_t (&off)[CHUNKS]) {
+                                              int lane, const uint32_t (&off)[OFFSETS]) {
     const __amdgpu_buffer_rsrc_t r = make_rsrc(p, static_cast<uint32_t>(kMaxBufferBytes));
     if (left >= ROWS) {
+      const uint32_t step = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(token) * (THREADS / LINE * 2));
 #pragma unroll
-      for (int i = 0; i < CHUNKS; ++i) load_lds(r, lds + (i * (THREADS / 64) + wave) * 1024, off[i]);
+      for (int i = 0; i < CHUNKS; ++i)
+        load_lds(r, lds + (i * (THREADS / 64) + wave) * 1024, off[EVEN ? 0 : i], EVEN ? i * step : 0);
     } else {
 #pragma unroll
       for (int i = 0; i < CHUNKS; ++i)
@@ -216,7 +224,9 @@ constexpr int64_t kFewTiles = 640;
 // where a row's terms have different x; above 2^28 fp16 cannot hold P, and above
 // 2^31 exponentials are infinite or all 0.  A wave with such a row subtracts
 // before it scales, (S - m) scale log2(e), in one instruction more.  The times of
-// ordinary rows are the same with and without (16384 tokens 541 us).
+// ordinary rows are the same with and without (16384 tokens 541 us).  The
+// gradients have lse alone, and dQ's kernel forms maximum and sum again for 128
+// queries of which one is beyond; all others pay 0 to 1.5% for the choice.
 constexpr float kFar = 1024.f;
 constexpr float kLn2 = 0.693147180559945309f;
 
@@ -315,9 +325,9 @@ __global__ __launch_bounds__(256 * S, 2) void k_attention(AttentionArgs a) {
   for (int i = 0; i < DP / 32; ++i) o[i] = zero16();
   float m = -INFINITY, sum = 0.f;
 
-  uint32_t off_k[R::CHUNKS], off_v[R::CHUNKS], pv[DP / 32];
+  uint32_t off_k[R::OFFSETS], off_v[R::OFFSETS], pv[DP / 32];
 #pragma unroll
-  for (int i = 0; i < R::CHUNKS; ++i) {
+  for (int i = 0; i < R::OFFSETS; ++i) {
     off_k[i] = R::offset(a.K.token, BN * S, a.D, tid, i);
     off_v[i] = R::offset(a.V.token, BN * S, a.D, tid, i);
   }
@@ -475,16 +485,23 @@ __global__ __launch_bounds__(256 * S, 2) void k_attention_dq(AttentionArgs a) {
   lm_u32x4 q[DP / 16], dy[DP / 16];
   operand<DP>(at(a.Q, row, w.head), a.Q.token, len - qw, a.D, lane, q);
   operand<DP>(at(a.dO, row, w.head), a.dO.token, len - qw, a.D, lane, dy);
-  const int64_t stat = w.head * a.T + w.rows.start + qi;
-  const float lse2 = qi < len ? a.lse[stat] * kLog2E : 0.f;
+  const int64_t stats = w.head * a.T + w.rows.start, stat = stats + qi;
+  // P = exp2((S - m) scale2 - lse2), with m = 0 unless a row of the workgroup's is
+  // far from 0: lse, of one rounding, does not tell P there (see kFar), and maximum
+  // and sum are formed again
+  float all_lse[BM / 64];
+#pragma unroll
+  for (int i = 0; i < BM / 64; ++i) all_lse[i] = a.lse[stats + std::min(q0 + 64 * i + lane, len - 1)];
+  const float own_lse = a.lse[stats + std::min(qi, len - 1)];
+  float m = 0.f, lse2 = qi < len ? own_lse * kLog2E : 0.f;
   float delta = 0.f, raise = static_cast<float>(kRaise<E>);
   f32x16 dq[DP / 32];
 #pragma unroll
   for (int i = 0; i < DP / 32; ++i) dq[i] = zero16();
 
-  uint32_t off_k[R::CHUNKS], off_v[R::CHUNKS], pk[DP / 32];
+  uint32_t off_k[R::OFFSETS], off_v[R::OFFSETS], pk[DP / 32];
 #pragma unroll
-  for (int i = 0; i < R::CHUNKS; ++i) {
+  for (int i = 0; i < R::OFFSETS; ++i) {
     off_k[i] = R::offset(a.K.token, BN * S, a.D, tid, i);
     off_v[i] = R::offset(a.V.token, BN * S, a.D, tid, i);
   }
@@ -495,11 +512,18 @@ __global__ __launch_bounds__(256 * S, 2) void k_attention_dq(AttentionArgs a) {
     R::load(at(a.K, w.rows.start + static_cast<int64_t>(k0), kv_head), a.K.token, len - k0, a.D, to, all_waves, lane, off_k);
     R::load(at(a.V, w.rows.start + static_cast<int64_t>(k0), kv_head), a.V.token, len - k0, a.D, to + R::BYTES, all_waves, lane, off_v);
   };
-  // one pass over the keys: for delta alone, or for dQ
-  const auto pass = [&](auto for_delta) {
-    constexpr bool DELTA = decltype(for_delta)::value;
-    float shift = (DELTA ? 0.f : raise) - lse2;
-    issue(0, 0);
+  issue(0, 0);
+  bool in_reach = true;
+#pragma unroll
+  for (int i = 0; i < BM / 64; ++i) in_reach &= fabsf(all_lse[i]) * kLog2E <= kFar;
+  const bool far = !__all(in_reach);
+  // one pass over the keys, the first stage on its way: for maximum and sum, for
+  // delta alone, or for dQ
+  enum Pass { SUM, DELTA, GRAD };
+  const auto pass = [&](auto what, auto far_) {
+    constexpr int WHAT = decltype(what)::value;
+    constexpr bool FAR = decltype(far_)::value;
+    float shift = (WHAT == DELTA ? 0.f : raise) - lse2;
     for (int first = 0, slot = 0; first < keys; first += BN * S, slot ^= 1) {
       wait_step<0>();
       if (first + BN * S < keys) issue(first + BN * S, slot ^ 1);
@@ -516,16 +540,32 @@ __global__ __launch_bounds__(256 * S, 2) void k_attention_dq(AttentionArgs a) {
 #pragma unroll
         for (int kk = 0; kk < DP / 16; ++kk) {
           s = mma(R::row(stage, 32 * t, kk, lane), q[kk], s, E{});
-          ds = mma(R::row(stage + R::BYTES, 32 * t, kk, lane), dy[kk], ds, E{});
+          if constexpr (WHAT != SUM) ds = mma(R::row(stage + R::BYTES, 32 * t, kk, lane), dy[kk], ds, E{});
         }
+        if constexpr (WHAT == SUM) {
+          float top = m;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) ds[r] = __builtin_amdgcn_exp2f(fmaf(s[r], scale2, shift)) * (DELTA ? ds[r] : ds[r] - delta);
+          for (int r = 0; r < 16; ++r) {
+            if (k + place(r, h) > qi) s[r] = -INFINITY;
+            top = fmaxf(top, s[r]);
+          }
+          top = max_halves(top);
+          delta *= __builtin_amdgcn_exp2f((m - top) * scale2);
+#pragma unroll
+          for (int r = 0; r < 16; ++r) delta += __builtin_amdgcn_exp2f((s[r] - top) * scale2);
+          m = top;
+          return;
+        }
+        if constexpr (FAR) s -= m;
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          ds[r] = __builtin_amdgcn_exp2f(fmaf(s[r], scale2, shift)) * (WHAT == DELTA ? ds[r] : ds[r] - delta);
         if (k + 31 > qw) {
 #pragma unroll
           for (int r = 0; r < 16; ++r)
             if (k + place(r, h) > qi) ds[r] = 0.f;
         }
-        if constexpr (DELTA) {
+        if constexpr (WHAT == DELTA) {
 #pragma unroll
           for (int r = 0; r < 16; ++r) delta += ds[r];
         } else {
@@ -549,12 +589,34 @@ __global__ __launch_bounds__(256 * S, 2) void k_attention_dq(AttentionArgs a) {
       half(std::integral_constant<int, 1>{});
     }
   };
+  if (far) {
+    m = -INFINITY;
+    pass(std::integral_constant<int, SUM>{}, std::true_type{});
+    float sum = sum_halves(delta);
+    wait_step<0>();
+    if constexpr (S == 2) {
+      // (the second group may have had no keys)
+      float* both = reinterpret_cast<float*>(lds) + lane;
+      both[64 * all_waves] = m;
+      both[64 * (all_waves + 8)] = sum;
+      wait_step<0>();
+      const float m0 = both[64 * wave], m1 = both[64 * (wave + 4)];
+      m = fmaxf(m0, m1);
+      sum = both[64 * (wave + 8)] * __builtin_amdgcn_exp2f((m0 - m) * scale2) +
+            both[64 * (wave + 12)] * __builtin_amdgcn_exp2f((m1 - m) * scale2);
+      wait_step<0>();
+    }
+    issue(0, 0);
+    lse2 = __builtin_amdgcn_logf(sum);
+    delta = 0.f;
+  }
   if (q0 == 0) {
     // The first queries have few keys, their O is as large as V, and O's rounding
     // would move delta by as much as dS is rounded: they take delta = sum_s P (dO .
     // V), a pass over at most two stages of keys (dQ, dK and dV of 100 tokens in
     // bf16 1.48 times as far from 64 bits as their own rounding, 1.40 so).
-    pass(std::true_type{});
+    if (far) pass(std::integral_constant<int, DELTA>{}, std::true_type{});
+    else pass(std::integral_constant<int, DELTA>{}, std::false_type{});
     delta = sum_halves(delta);
     wait_step<0>();
     if constexpr (S == 2) {
@@ -564,6 +626,7 @@ __global__ __launch_bounds__(256 * S, 2) void k_attention_dq(AttentionArgs a) {
       delta = both[64 * wave] + both[64 * (wave + 4)];
       wait_step<0>();
     }
+    issue(0, 0);
   } else {
     lm_u32x4 y[DP / 16];
     operand<DP>(at(a.O, row, w.head), a.O.token, len - qw, a.D, lane, y);
@@ -576,11 +639,14 @@ __global__ __launch_bounds__(256 * S, 2) void k_attention_dq(AttentionArgs a) {
     }
     delta = sum_halves(delta);
   }
+  if (far) pass(std::integral_constant<int, GRAD>{}, std::true_type{});
+  else pass(std::integral_constant<int, GRAD>{}, std::false_type{});
   if (h == 0 && part == 0 && qi < len) {
+    const int64_t all = a.heads * a.T;
     a.delta[stat] = delta;
-    a.delta[a.heads * a.T + stat] = lse2 - kRaise<E>;
+    a.delta[all + stat] = lse2 - kRaise<E>;
+    a.delta[2 * all + stat] = -m;
   }
-  pass(std::false_type{});
   if (kRaise<E>) times(dq, raise > 0.f ? 1.f / (1 << kRaise<E>) : 1.f);
   if constexpr (S == 2) {
     float* to = reinterpret_cast<float*>(lds) + wave * VALUES * 64 + lane;
@@ -624,7 +690,7 @@ __global__ __launch_bounds__(128 * G, 2) void k_attention_dkv(AttentionArgs a) {
   typedef Rows<DP, KEYS, THREADS> RV;
   // with 128 values a head, registers hold the keys but not the values beside the sums
   constexpr bool V_IN_LDS = DP == 128;
-  constexpr int STAGE = 2 * R::BYTES + 2 * G * 256;      // Q, dO, and of each query: delta, lse (twice: every wave loads)
+  constexpr int STAGE = 2 * R::BYTES + 2 * G * 256;      // Q, dO, and of each query: delta, lse, maximum (twice: every wave loads)
   constexpr int VALUES = DP / 32 * 2 * 16;           // sums of a lane
   __shared__ __align__(16) char lds[2 * STAGE + (V_IN_LDS ? KEYS * DP * 2 : 0)];
   static_assert(G * VALUES * 256 <= 2 * STAGE, "the sums of half the waves go through LDS");
@@ -641,9 +707,9 @@ __global__ __launch_bounds__(128 * G, 2) void k_attention_dkv(AttentionArgs a) {
   lm_u32x4 k[DP / 16], v[V_IN_LDS ? 1 : DP / 16];
   operand<DP>(at(a.K, row, w.head), a.K.token, len - kw, a.D, lane, k);
   if constexpr (V_IN_LDS) {
-    uint32_t off[RV::CHUNKS];
+    uint32_t off[RV::OFFSETS];
 #pragma unroll
-    for (int i = 0; i < RV::CHUNKS; ++i) off[i] = RV::offset(a.V.token, KEYS, a.D, tid, i);
+    for (int i = 0; i < RV::OFFSETS; ++i) off[i] = RV::offset(a.V.token, KEYS, a.D, tid, i);
     RV::load(at(a.V, w.rows.first, w.head), a.V.token, len - k0, a.D, lds + 2 * STAGE, wave, lane, off);
   } else {
     operand<DP>(at(a.V, row, w.head), a.V.token, len - kw, a.D, lane, v);
@@ -653,9 +719,9 @@ __global__ __launch_bounds__(128 * G, 2) void k_attention_dkv(AttentionArgs a) {
   for (int i = 0; i < DP / 32; ++i) dk[i] = dv[i] = zero16();
   bool raised = kRaise<E> > 0;
 
-  uint32_t off_q[R::CHUNKS], off_d[R::CHUNKS], pq[DP / 32];
+  uint32_t off_q[R::OFFSETS], off_d[R::OFFSETS], pq[DP / 32];
 #pragma unroll
-  for (int i = 0; i < R::CHUNKS; ++i) {
+  for (int i = 0; i < R::OFFSETS; ++i) {
     off_q[i] = R::offset(a.Q.token, STEP, a.D, tid, i);
     off_d[i] = R::offset(a.dO.token, STEP, a.D, tid, i);
   }
@@ -674,7 +740,8 @@ __global__ __launch_bounds__(128 * G, 2) void k_attention_dkv(AttentionArgs a) {
     R::load(at(a.dO, from, head), a.dO.token, left, a.D, to + R::BYTES, wave, lane, off_d);
     typedef __attribute__((address_space(3))) void* P;
     const int i = wave % (G / 2) * 64 + lane;
-    const float* x = a.delta + (wave / (G / 2) % 2 * a.heads + head) * a.T + from;
+    const int which = wave < G ? wave / (G / 2) : 2;
+    const float* x = a.delta + (which * a.heads + head) * a.T + from;
     __builtin_amdgcn_raw_ptr_buffer_load_lds(make_rsrc(x, static_cast<uint32_t>(kMaxBufferBytes)),
                                              (P)(to + 2 * R::BYTES + wave * 256), 4,
                                              i < left ? static_cast<uint32_t>(i * 4) : kOutOfRange, 0, 0, 0);
@@ -697,7 +764,14 @@ __global__ __launch_bounds__(128 * G, 2) void k_attention_dkv(AttentionArgs a) {
     uint32_t p[DP / 32];
 #pragma unroll
     for (int j = 0; j < DP / 32; ++j) p[j] = pq[j] + slot * STAGE;
-    f32x16 s = zero16(), ds = zero16();
+    const char* stats = stage + 2 * R::BYTES + (32 * part + 4 * h) * 4;
+    f32x16 s, ds = zero16();   // s: Q . K - m, a sum from -m on (0 for ordinary rows)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const lm_f32x4 m = *reinterpret_cast<const lm_f32x4*>(stats + STEP * 8 + 32 * g);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) s[4 * g + j] = m[j];
+    }
 #pragma unroll
     for (int kk = 0; kk < DP / 16; ++kk) {
       s = mma(R::row(stage, 32 * part, kk, lane), k[kk], s, E{});
@@ -706,7 +780,6 @@ __global__ __launch_bounds__(128 * G, 2) void k_attention_dkv(AttentionArgs a) {
       else x = v[kk];
       ds = mma(R::row(stage + R::BYTES, 32 * part, kk, lane), x, ds, E{});
     }
-    const char* stats = stage + 2 * R::BYTES + (32 * part + 4 * h) * 4;
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
       const lm_f32x4 delta = *reinterpret_cast<const lm_f32x4*>(stats + 32 * g);

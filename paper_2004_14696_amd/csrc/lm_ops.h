@@ -329,7 +329,9 @@ struct AttentionArgs {
   const int32_t* offsets;
   HeadRows Q, K, V, O, dO, dQ, dK, dV;
   float* lse;           // [heads][T], nullable in the forward pass
-  float* delta;         // workspace [2][heads][T]: dO . O, and lse log2(e)
+  // workspace [3][heads][T]: dO . O; lse log2(e) and 0, or, where that is large for one
+  // of 128 rows, the logarithm (of 2) of sum exp(S - maximum) and the maximum of Q . K
+  float* delta;
   float* sums;          // workspace [parts][2][T][kv_heads][D] (parts > 1)
   int parts;            // workgroups that share the queries of a tile of keys
   uint32_t slots;       // tiles of a head's queries or keys (set by the launch)

@@ -10,10 +10,11 @@
 
 namespace dbw {
 
-// 16 bytes a lane from r + off to the wave's 1 KiB at `to`.
-__device__ __forceinline__ void load_lds(__amdgpu_buffer_rsrc_t r, char* to, uint32_t off) {
+// 16 bytes a lane from r + off + more (the same for all lanes) to the wave's 1 KiB
+// at `to`.
+__device__ __forceinline__ void load_lds(__amdgpu_buffer_rsrc_t r, char* to, uint32_t off, uint32_t more = 0) {
   typedef __attribute__((address_space(3))) void* P;
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (P)to, 16, off, 0, 0, 0);
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (P)to, 16, off, static_cast<int>(more), 0, 0);
 }
 
 // Waits until at most `loads` of this wave's loads are outstanding and all its

@@ -184,3 +184,64 @@ def test_attention_of_scores_that_grow_past_the_limit():
         steps = torch.arange(T, device="cuda") // 16 * 64
         K[:, 0, 0], K[:, 1, 0] = steps.to(dtype), (steps - 1000).clamp(min=-960).to(dtype)
         check(Q, K, normal(g, (T, 2, D), dtype), [T], scale=0.125)
+
+
+# -- gradients -------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("D,lengths,heads,kv", FAR)
+def test_attention_gradients_of_scores_far_from_zero(dtype, D, lengths, heads, kv):
+    Q, K, V, dO = far_from_zero(D, dtype, lengths, heads, kv)
+    check(Q, K, V, lengths, scale=0.125, dO=dO)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("D,lengths,heads,kv", LARGE)
+def test_attention_gradients_of_large_values(dtype, D, lengths, heads, kv):
+    Q, K, V, dO = large(D, dtype, lengths, heads, kv)
+    # (keys and queries of 20480 times dS of 1 are beyond fp16: dO of 2^-12 brings dQ and dK to its range)
+    check(Q, K, V, lengths, dO=dO if dtype == BF16 else (dO * 2.0 ** -12).to(dtype))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("scale", [1e5, 1e10, 1e20])
+@pytest.mark.parametrize("D", [64, 128])
+def test_attention_gradients_of_a_large_scale(dtype, scale, D):
+    T = 200
+    for sign in (1, 3):
+        Q, K, V, dO = ordered(D, dtype, T, sign)
+        off = offsets_of([T])
+        O, lse = pb.attention(Q, K, V, off, scale=scale)                                                   # noqa: E741
+        dQ, dK, dV = pb.attention_grad(dO, Q, K, V, O, lse, off, scale=scale)
+        # weights are 1 and 0: P (dO . V - dO . O) is 0 exactly, its sums of whole numbers being exact
+        assert bool((dQ == 0).all()) and bool((dK == 0).all())
+        ref = torch.zeros((T, D), dtype=torch.float64, device="cuda")
+        for h in range(2):
+            k = K[:, 0, 1].double() * (1 - 2 * h)
+            ref.index_add_(0, k.cummax(0).indices, dO[:, h].double())
+        close(dV[:, 0], ref, rounded(ref, dtype), "dV")
+
+
+def test_attention_gradients_of_scores_that_grow_past_the_limit():
+    g = gen(32)
+    T, D = 500, 64
+    for dtype in (BF16, F16):
+        Q, K = whole(g, (T, 2, D), 2, dtype), whole(g, (T, 2, D), 2, dtype)
+        Q[:, :, 0] = 8
+        steps = torch.arange(T, device="cuda") // 16 * 64
+        K[:, 0, 0], K[:, 1, 0] = steps.to(dtype), (steps - 1000).clamp(min=-960).to(dtype)
+        check(Q, K, normal(g, (T, 2, D), dtype), [T], scale=0.125, dO=normal(g, (T, 2, D), dtype, 0.5))
+
+
+def test_attention_gradients_at_the_limits_of_the_exponents():
+    # |lse| of 2^10 powers of two from both sides, in one tile and in one batch
+    g = gen(33)
+    T, D, limit = 400, 64, 1024 * math.log(2)
+    Q, K = whole(g, (T, 4, D), 2, BF16), whole(g, (T, 4, D), 2, BF16)
+    K[:, :, 0] = 16
+    base = (limit / 0.125 / 16) * (1 + torch.linspace(-0.04, 0.04, T, device="cuda").view(-1, 1))
+    Q[:, :, 0] = (base * torch.tensor([1, -1, 1, 0.25], device="cuda")).to(BF16)
+    V, dO = normal(g, (T, 4, D), BF16), normal(g, (T, 4, D), BF16, 0.5)
+    got = check(Q, K, V, [T], scale=0.125, dO=dO)
+    low, high = got["lse"][0].abs() < limit, got["lse"][0].abs() > limit
+    assert bool(low.any()) and bool(high.any())
+    check(Q, K, V, [100, 200, 100], scale=0.125, dO=dO)
