@@ -89,9 +89,10 @@ struct Rows {
   static constexpr int CHUNKS = ROWS * LINE / THREADS;    // a thread
   static constexpr int BYTES = ROWS * DP * 2;
   // With 128 values, a thread's chunks lie whole periods of turn() apart: one offset
-  // does, with a scalar one, and four registers fewer keep dK and dV's loop free of
-  // scratch (8192 tokens, 16 heads on 4, fp16: 173 -> 152 us; with 64 values registers
-  // suffice, and the scalar ones would not).
+  // does, with a scalar one.  With it, and with line(), dK and dV's loop has no
+  // scratch, whose loads wait for the next stage (8 sequences, 8192 tokens, 16 heads on 4:
+  // 145 -> 143 us in bf16, 172 -> 142 in fp16).  With 64 values registers suffice, and the
+  // scalar ones would not.
   static constexpr bool EVEN = DP == 128 && THREADS / LINE % 16 == 0;
   static constexpr int OFFSETS = EVEN ? 1 : CHUNKS;
   static_assert(DP == 64 || DP == 96 || DP == 128, "turn() is for these");
@@ -124,6 +125,19 @@ struct Rows {
   static __device__ __forceinline__ lm_u32x4 row(const char* lds, int first, int kk, int lane) {
     const int c = lane % 32, h = lane / 32;
     return *reinterpret_cast<const lm_u32x4*>(lds + (first + c) * (DP * 2) + ((2 * kk + h) ^ turn(c)) * 16);
+  }
+  // The same from the address of a lane's chunk 0, where lines are 256 bytes from a
+  // multiple of that on: chunks' numbers join by exclusive or, and one register
+  // holds what would be eight.
+  static __device__ __forceinline__ uint32_t line(const char* lds, int first, int lane) {
+    const int c = lane % 32, h = lane / 32;
+    typedef __attribute__((address_space(3))) const char* P;
+    return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((P)(lds + (first + c) * (DP * 2) + (h ^ turn(c)) * 16)));
+  }
+  static __device__ __forceinline__ lm_u32x4 row(uint32_t line, int kk) {
+    static_assert(DP == 128, "an exclusive or stays in the line");
+    typedef __attribute__((address_space(3))) const lm_u32x4* P;
+    return *(P)(line ^ kk * 32);
   }
   // Addresses of a lane for column(): of the columns 32 i + 16 (lane / 16 % 2)
   // + 4 q .. + 3 of line 4 h + r, with r and q from lane % 16 = 4 r + q.
@@ -226,7 +240,8 @@ constexpr int64_t kFewTiles = 640;
 // before it scales, (S - m) scale log2(e), in one instruction more.  The times of
 // ordinary rows are the same with and without (16384 tokens 541 us).  The
 // gradients have lse alone, and dQ's kernel forms maximum and sum again for 128
-// queries of which one is beyond; all others pay 0 to 1.5% for the choice.
+// queries of which one is beyond; all others pay up to 2% of the
+// gradients' time for the choice.
 constexpr float kFar = 1024.f;
 constexpr float kLn2 = 0.693147180559945309f;
 
@@ -645,7 +660,7 @@ __global__ __launch_bounds__(256 * S, 2) void k_attention_dq(AttentionArgs a) {
     const int64_t all = a.heads * a.T;
     a.delta[stat] = delta;
     a.delta[all + stat] = lse2 - kRaise<E>;
-    a.delta[2 * all + stat] = -m;
+    a.delta[2 * all + stat] = m;
   }
   if (kRaise<E>) times(dq, raise > 0.f ? 1.f / (1 << kRaise<E>) : 1.f);
   if constexpr (S == 2) {
@@ -692,7 +707,7 @@ __global__ __launch_bounds__(128 * G, 2) void k_attention_dkv(AttentionArgs a) {
   constexpr bool V_IN_LDS = DP == 128;
   constexpr int STAGE = 2 * R::BYTES + 2 * G * 256;      // Q, dO, and of each query: delta, lse, maximum (twice: every wave loads)
   constexpr int VALUES = DP / 32 * 2 * 16;           // sums of a lane
-  __shared__ __align__(16) char lds[2 * STAGE + (V_IN_LDS ? KEYS * DP * 2 : 0)];
+  __shared__ __align__(256) char lds[2 * STAGE + (V_IN_LDS ? KEYS * DP * 2 : 0)];
   static_assert(G * VALUES * 256 <= 2 * STAGE, "the sums of half the waves go through LDS");
   const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
   const int c = lane % 32, h = lane / 32, part = wave / 2;
@@ -726,6 +741,11 @@ __global__ __launch_bounds__(128 * G, 2) void k_attention_dkv(AttentionArgs a) {
     off_d[i] = R::offset(a.dO.token, STEP, a.D, tid, i);
   }
   R::columns(lds + 32 * part * DP * 2, lane, pq);
+  uint32_t line_q = 0, line_v = 0;
+  if constexpr (V_IN_LDS) {
+    line_q = R::line(lds, 32 * part, lane);
+    line_v = RV::line(lds + 2 * STAGE, 32 * (wave % 2), lane);
+  }
   // tiles of queries from the workgroup's first key on, for each head in turn
   const int steps = (len - k0 + STEP - 1) / STEP;
   const int64_t all = static_cast<int64_t>(steps) * share;
@@ -765,20 +785,32 @@ __global__ __launch_bounds__(128 * G, 2) void k_attention_dkv(AttentionArgs a) {
 #pragma unroll
     for (int j = 0; j < DP / 32; ++j) p[j] = pq[j] + slot * STAGE;
     const char* stats = stage + 2 * R::BYTES + (32 * part + 4 * h) * 4;
-    f32x16 s, ds = zero16();   // s: Q . K - m, a sum from -m on (0 for ordinary rows)
+    // whether one of 32 queries has a maximum, which is subtracted from whole sums: these
+    // are then the same bits here as where the maximum is from
+    const bool far = __any(*reinterpret_cast<const float*>(stage + 2 * R::BYTES + STEP * 8 + (32 * part + c) * 4) != 0.f);
+    f32x16 s = zero16(), ds = zero16();
+    if constexpr (V_IN_LDS) {
+      const uint32_t at_q = line_q + slot * STAGE;
+      asm("" : "+v"(line_v));   // (the addresses from it are not to be kept)
 #pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      const lm_f32x4 m = *reinterpret_cast<const lm_f32x4*>(stats + STEP * 8 + 32 * g);
+      for (int kk = 0; kk < DP / 16; ++kk) {
+        s = mma(R::row(at_q, kk), k[kk], s, E{});
+        ds = mma(R::row(at_q + R::BYTES, kk), RV::row(line_v, kk), ds, E{});
+      }
+    } else {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) s[4 * g + j] = m[j];
+      for (int kk = 0; kk < DP / 16; ++kk) {
+        s = mma(R::row(stage, 32 * part, kk, lane), k[kk], s, E{});
+        ds = mma(R::row(stage + R::BYTES, 32 * part, kk, lane), v[kk], ds, E{});
+      }
     }
+    if (far) {
 #pragma unroll
-    for (int kk = 0; kk < DP / 16; ++kk) {
-      s = mma(R::row(stage, 32 * part, kk, lane), k[kk], s, E{});
-      lm_u32x4 x;
-      if constexpr (V_IN_LDS) x = RV::row(lds + 2 * STAGE, 32 * (wave % 2), kk, lane);
-      else x = v[kk];
-      ds = mma(R::row(stage + R::BYTES, 32 * part, kk, lane), x, ds, E{});
+      for (int g = 0; g < 4; ++g) {
+        const lm_f32x4 m = *reinterpret_cast<const lm_f32x4*>(stats + STEP * 8 + 32 * g);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[4 * g + j] -= m[j];
+      }
     }
 #pragma unroll
     for (int g = 0; g < 4; ++g) {

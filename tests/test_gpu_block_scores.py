@@ -245,3 +245,44 @@ def test_attention_gradients_at_the_limits_of_the_exponents():
     low, high = got["lse"][0].abs() < limit, got["lse"][0].abs() > limit
     assert bool(low.any()) and bool(high.any())
     check(Q, K, V, [100, 200, 100], scale=0.125, dO=dO)
+
+
+@pytest.mark.parametrize("dtype,size", [(F16, 6000.0), (BF16, 1e5), (BF16, 1e15)])
+@pytest.mark.parametrize("D,lengths,heads,kv", [(64, [400], 2, 1), (128, [150, 0, 333], 4, 2), (128, [400, 0, 700], 64, 16),
+                                                (64, [400, 0, 700], 64, 16)])
+def test_attention_and_its_gradients_where_sums_round(dtype, size, D, lengths, heads, kv):
+    """Values of which Q . K rounds by far more than 1: every pass has to find the same
+    score for a query and a key.  The largest is larger than any other by more than both
+    roundings (asserted), so that it takes all: P is 1 and 0, and P (dO . V - dO . O) 0."""
+    g = torch.Generator().manual_seed(D + heads)
+    T = sum(lengths)
+    Q, K = ((torch.randn((T, h, D), generator=g).clamp(-5, 5) * size).to(dtype).cuda() for h in (heads, kv))
+    V, dO = (torch.randint(-4, 5, (T, h, D), generator=g).to(dtype).cuda() for h in (kv, heads))
+    O_ref, lse_ref = torch.zeros((T, heads, D), device="cuda").double(), torch.zeros((heads, T), device="cuda").double()
+    dV_ref, e_lse = torch.zeros((T, kv, D), device="cuda").double(), torch.zeros_like(lse_ref)
+    clear = torch.ones((T, heads), dtype=torch.bool, device="cuda")
+    lone = torch.ones((T, kv), dtype=torch.bool, device="cuda")
+    for a, b in parts_of(lengths):
+        keep = torch.tril(torch.ones((b - a, b - a), dtype=torch.bool, device="cuda"))
+        for h in range(heads if b > a else 0):
+            j = h * kv // heads
+            q, kt = Q[a:b, h].double(), K[a:b, j].double().t().contiguous()
+            S = torch.where(keep, D ** -0.5 * (q @ kt), -math.inf)
+            e_S = torch.where(keep, 2 * D * u * D ** -0.5 * (q.abs() @ kt.abs()), 0.0)
+            top, at = S.max(1)
+            rivals = (S + e_S >= (top - e_S.gather(1, at.view(-1, 1)).view(-1)).view(-1, 1) - 200).sum(1) > 1
+            clear[a:b, h] = ~rivals
+            # (keys that a row without a clear winner may give weight to)
+            lone[a:b, j] &= ~((S + 2 * e_S.amax(1, keepdim=True) >= top.view(-1, 1) - 200) & rivals.view(-1, 1)).any(0)
+            O_ref[a:b, h], lse_ref[h, a:b] = V[a:b, j].double()[at], top
+            e_lse[h, a:b] = e_S.gather(1, at.view(-1, 1)).view(-1) + 4 * u * top.abs()
+            dV_ref[a:b, j].index_add_(0, at, dO[a:b, h].double())
+    assert float(clear.double().mean()) > 0.99 and float(lone.double().mean()) > 0.5
+    off = offsets_of(lengths)
+    O, lse = pb.attention(Q, K, V, off)                                                                    # noqa: E741
+    dQ, dK, dV = pb.attention_grad(dO, Q, K, V, O, lse, off)
+    torch.cuda.synchronize()
+    assert torch.equal(O.double()[clear], O_ref[clear])
+    close(lse[clear.t()], lse_ref[clear.t()], e_lse[clear.t()], "lse")
+    assert bool((dQ[clear] == 0).all()) and bool((dK[lone] == 0).all())
+    close(dV[lone], dV_ref[lone], rounded(dV_ref[lone], dtype), "dV")
