@@ -80,7 +80,7 @@ DBW_API dbw_status dbw_layer_norm(int32_t n, int64_t T, int32_t d, int32_t dtype
   if (!gamma || !aligned(gamma, 4) || !aligned(beta, 4))
     return set_free_error(DBW_EINVAL, "%s: gamma is NULL, or a pointer is not aligned to its elements", call);
   if (!good_eps(eps)) return set_free_error(DBW_EINVAL, "%s: eps lies in [1e-30, 1e30]", call);
-  if (Y && (Y == X || Y == gamma || Y == beta)) return overlap(call);
+  if (Y && (Y == X || Y == gamma || Y == beta || Y == offsets)) return overlap(call);
   dbw::NormArgs a{};
   a.n = n; a.d = d; a.T = T; a.dtype = dtype; a.offsets = offsets; a.X = X; a.ld_X = ld_X;
   a.gamma = gamma; a.beta = beta; a.eps = static_cast<float>(eps); a.out = Y; a.ld_out = ld_Y;
@@ -107,9 +107,9 @@ DBW_API dbw_status dbw_layer_norm_grad(int32_t n, int64_t T, int32_t d, int32_t 
   if (!gamma || !dgamma || !aligned(gamma, 4))
     return set_free_error(DBW_EINVAL, "%s: gamma or dgamma is NULL, or a pointer is not aligned to its elements", call);
   if (!good_eps(eps)) return set_free_error(DBW_EINVAL, "%s: eps lies in [1e-30, 1e30]", call);
-  if (dX && (dX == dY || dX == X || dX == gamma || dX == dgamma || dX == dbeta)) return overlap(call);
+  if (dX && (dX == dY || dX == X || dX == gamma || dX == dgamma || dX == dbeta || dX == offsets)) return overlap(call);
   for (const void* g : {static_cast<const void*>(dgamma), static_cast<const void*>(dbeta)})
-    if (g && (g == dY || g == X || g == gamma)) return overlap(call);
+    if (g && (g == dY || g == X || g == gamma || g == offsets)) return overlap(call);
   if (dgamma == dbeta) return overlap(call);
   if (dbw_status s = check_workspace(call, dbw::norm_workspace(n, T, d), workspace, workspace_bytes); s != DBW_OK)
     return s;
@@ -141,8 +141,8 @@ DBW_API dbw_status dbw_linear_grad(int32_t n, int64_t T, int32_t C, int32_t dtyp
     if (dbw_status s = check_array(call, r, T, C, e); s != DBW_OK) return s;
   if (dbw_status s = check_array(call, Rows{dbias, ld_dbias, false}, T, C, 4); s != DBW_OK) return s;
   if (!dZ && !dbias && T > 0) return set_free_error(DBW_EINVAL, "%s: neither dZ nor dbias is given", call);
-  if (dZ && (dZ == dY || dZ == Z || dZ == dbias)) return overlap(call);
-  if (dbias && (dbias == dY || dbias == Z)) return overlap(call);
+  if (dZ && (dZ == dY || dZ == Z || dZ == dbias || dZ == offsets)) return overlap(call);
+  if (dbias && (dbias == dY || dbias == Z || dbias == static_cast<const void*>(offsets))) return overlap(call);
   if (dbias)
     if (dbw_status s = check_workspace(call, dbw::linear_grad_workspace(n, T, C), workspace, workspace_bytes); s != DBW_OK)
       return s;
@@ -166,7 +166,7 @@ DBW_API dbw_status dbw_dropout(int32_t n, int64_t T, int32_t d, int32_t dtype, c
   if (!aligned(step, 8)) return set_free_error(DBW_EINVAL, "%s: step is not aligned", call);
   if (Y && ((Y == X && ld_Y != ld_X) || (Y == R && ld_Y != ld_R)))
     return set_free_error(DBW_EINVAL, "%s: Y in the place of an input needs its row stride", call);
-  if (Y && Y == static_cast<const void*>(step)) return overlap(call);
+  if (Y && (Y == static_cast<const void*>(step) || Y == offsets)) return overlap(call);
   dbw::DropoutArgs a{};
   a.n = n; a.d = d; a.T = T; a.dtype = dtype; a.offsets = offsets; a.X = X; a.ld_X = ld_X; a.R = R; a.ld_R = ld_R;
   a.Y = Y; a.ld_Y = ld_Y; a.seed = seed; a.step = step;
@@ -247,7 +247,7 @@ DBW_API dbw_status dbw_attention(const dbw_attention_shape* shape, const int32_t
   if (p.T == 0) return DBW_OK;
   for (const dbw_heads* in : {Q, K, V})
     if (O->data == in->data || (lse && lse == in->data)) return overlap(call);
-  if (lse && lse == O->data) return overlap(call);
+  if (O->data == offsets || (lse && (lse == O->data || lse == static_cast<const void*>(offsets)))) return overlap(call);
   dbw::AttentionArgs a = attention_args(p, offsets);
   a.Q = rows_of(*Q); a.K = rows_of(*K); a.V = rows_of(*V); a.O = rows_of(*O); a.lse = lse;
   return launched(call, dbw::launch_attention(a, static_cast<hipStream_t>(stream)));
@@ -291,7 +291,7 @@ DBW_API dbw_status dbw_attention_grad(const dbw_attention_shape* shape, const in
     for (const auto& y : arrays)
       if (x.out && &x != &y && x.h->data == y.h->data) return overlap(call);
   for (const auto& x : arrays)
-    if (x.out && x.h->data == lse) return overlap(call);
+    if (x.out && (x.h->data == lse || x.h->data == offsets)) return overlap(call);
   if (dbw_status s = check_workspace(call, delta_bytes(p) + sum_bytes(p), workspace, workspace_bytes); s != DBW_OK) return s;
   dbw::AttentionArgs a = attention_args(p, offsets);
   a.Q = rows_of(*Q); a.K = rows_of(*K); a.V = rows_of(*V); a.O = rows_of(*O); a.dO = rows_of(*dO);

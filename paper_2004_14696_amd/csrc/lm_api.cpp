@@ -140,8 +140,9 @@ DBW_API dbw_status dbw_group_linear(const dbw_group_shape* shape, const dbw_line
     return set_free_error(DBW_EINVAL, "%s: Y in the place of R needs its row stride", call);
   if (e.pre && (e.pre == Y || e.pre == X || e.pre == W || e.pre == e.residual))
     return set_free_error(DBW_EINVAL, "%s: Z must not overlap other arrays", call);
-  if (e.bias && (e.bias == Y || e.bias == e.pre))
-    return set_free_error(DBW_EINVAL, "%s: an output must not overlap the bias", call);
+  for (const void* in : {static_cast<const void*>(e.bias), static_cast<const void*>(offsets)})
+    if (in && (in == Y || in == e.pre))
+      return set_free_error(DBW_EINVAL, "%s: an output must not overlap the bias or the offsets", call);
   return group_call(call, shape, &e, offsets, X, W, Y, workspace, workspace_bytes, stream);
 }
 
