@@ -541,7 +541,8 @@ uint32_t dbw_adamw_bits(uint32_t seed, int64_t t, int32_t tensor, int64_t index)
  * and dropout.  The rules above hold here too: no context, a stream, device
  * offsets of n ragged groups (the workers' rows; for attention the sequences),
  * nothing allocated, capturable; rows of no group are not read, and left as
- * they were in outputs.  Outputs must not overlap inputs or each other, but for
+ * they were in outputs.  Row strides are below 2^32, or what is said below
+ * (DBW_EUNSUPPORTED above).  Outputs must not overlap inputs or each other, but for
  * what is said below (DBW_EINVAL where one is the other).  Vectors of weights
  * (gamma, beta, bias) are fp32, as AdamW keeps them, and so are their
  * gradients, one row for each worker: with the row stride P they lie in the
@@ -552,7 +553,8 @@ uint32_t dbw_adamw_bits(uint32_t seed, int64_t t, int32_t tensor, int64_t index)
  *   H[t] = (X[t] - mean) / sqrt(var + eps),   Y[t] = H[t] gamma + beta.
  * X and Y are DEVICE [T][d] of dtype (row strides ld_X, ld_Y, in elements),
  * gamma and beta DEVICE float [d] (beta may be NULL: 0).  Statistics are formed
- * in fp32, the variance from differences to the mean.  n in [1, DBW_MAX_N], d
+ * in fp32, the variance from differences to the mean: their squares' sum has to
+ * be finite there (values below 2^56 in size always have that).  n in [1, DBW_MAX_N], d
  * in [1, 16384] (DBW_EUNSUPPORTED above), T below 2^31, eps in [1e-30, 1e30]. */
 dbw_status dbw_layer_norm(int32_t n, int64_t T, int32_t d, int32_t dtype, const int32_t* offsets, const void* X,
                           int64_t ld_X, const float* gamma, const float* beta, double eps, void* Y, int64_t ld_Y,
@@ -630,7 +632,8 @@ typedef struct {
   int32_t n;               /* sequences, in [1, 65536]                       */
   int32_t heads, kv_heads; /* kv_heads divides heads; heads at most 1024     */
   int32_t D;               /* a multiple of 8, in [8, 128]                   */
-  int64_t T;               /* rows, in [0, 2^31)                             */
+  int64_t T;               /* rows, in [0, 2^31); (floor(T / 64) + n) heads
+                              below 2^23 (DBW_EUNSUPPORTED)                  */
   double scale;            /* in [1e-20, 1e20]                               */
 } dbw_attention_shape;
 dbw_status dbw_attention(const dbw_attention_shape* shape, const int32_t* offsets, const dbw_heads* Q,

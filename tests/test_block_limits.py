@@ -76,3 +76,18 @@ OFFSETS_AS_OUTPUT = {
 def test_offsets_are_refused_as_an_output(lib, name):
     assert OFFSETS_AS_OUTPUT[name](lib) == pb.DBW_EINVAL
     assert b"overlap" in lib.dbw_last_error(None)
+
+
+@pytest.mark.parametrize("n,T,heads", [(65536, 0, 128), (65536, 100, 128), (1, ((1 << 23) // 8 - 1) * 64, 8),
+                                       (8192, 64 * 1023 + 63, 1024), (65536, 65536 * 64, 64)])
+def test_attention_tiles_reach_the_stated_limit(lib, n, T, heads):
+    """(floor(T / 64) + n) heads: 2^23 is refused, and what lies just below is not."""
+    size = (T // 64 + n) * heads
+    work = lambda n: lib.dbw_attention_workspace(ctypes.byref(pb.AttentionShape(                            # noqa: E731
+        dtype=pb.DBW_BF16, n=n, heads=heads, kv_heads=heads, D=64, T=T, scale=0.125)))
+    at_limit = n if size >= 1 << 23 else n + ((1 << 23) - size + heads - 1) // heads
+    if at_limit <= 65536:
+        assert work(at_limit) == -1
+    below = ((1 << 23) - 1) // heads - T // 64
+    if 1 <= below <= 65536:
+        assert work(below) >= 0
