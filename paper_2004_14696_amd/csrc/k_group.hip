@@ -575,20 +575,22 @@ __device__ __forceinline__ void product(const Tile& t, const Epilogue& e, bool o
 
   constexpr int LDS = (WIDE ? STAGES : 2) * STAGE / (THREADS / 64);   // bytes a wave
   char* mine = lds + wave * LDS;
-  if constexpr (EPILOGUE)
+  if constexpr (EPILOGUE) {
     if (!parts && !e.residual) {
       if (out_f32)
         write_acted<E, float, WM, WN, LDS>(acc, t, e, m0, n0, mine, lane);
       else
         write_acted<E, E, WM, WN, LDS>(acc, t, e, m0, n0, mine, lane);
       return;
-    } else if (!parts) {
+    }
+    if (!parts) {
       if (out_f32)
         write_finished<E, float, WM, WN, LDS>(acc, t, e, m0, n0, mine, lane);
       else
         write_finished<E, E, WM, WN, LDS>(acc, t, e, m0, n0, mine, lane);
       return;
     }
+  }
   if (out_f32 || parts)
     write_out<float, WM, WN, LDS, STREAM>(acc, t, m0, n0, mine, lane);
   else
