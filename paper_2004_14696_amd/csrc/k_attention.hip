@@ -23,20 +23,25 @@
 // (a workgroup for keys that adds to dQ would need fp32 atomics whose order is
 // not fixed).
 //
-// What bounds it.  Long sequences: the matrix cores at the clock they hold under
-// load; 1 sequence of 16384 tokens, 8 heads on 2 of 128, forward 547 to 576 us, 955 to
-// 1005 TFLOP/s (a library product 1244), dQ 775 us, 1060 TFLOP/s, dK and dV 1334 us, 825
-// TFLOP/s.  Vector work, 150 instructions and 32 exponentials for 32 products, runs
-// beside the products of the other wave of a SIMD only in part (cores busy 60% of
-// the cycles).  Ragged batches: the tiles on the diagonal, start and end of each
-// workgroup, and the last of them; 8 sequences, 8192 tokens, 16 heads on 4 of 128: 60,
-// 87 and 133 us, 680, 700 and 610 TFLOP/s, cores busy 32 to 38%.  Short sequences: the chain
-// from offsets to keys to products, some 5 us a workgroup (50 sequences, 5000 tokens,
-// 12 heads of 80, fp16: 15, 26 and 28 us).  LDS is read without conflicts (with lines
-// turned for 32 banks half of its cycles were), its reads are builtins so that the
-// compiler places their waits.  Tried, no gain: the priority of waves raised for
-// products.  Not tried: softmax of one stage beside the products of the next
-// within a wave, for which 256 registers do not hold 128 values a head.
+// What bounds it.  The next stage's way to LDS, in every step: the compiler cannot
+// tell the stage that transposing reads take from the one that loads are filling,
+// and waits for all loads before the first of these reads, so that a load overlaps
+// the first products and the exponentials of its step only.  (As statements with
+// their own wait these reads were slower: forward 64 us for 62,
+// dK and dV 142 for 129 in the ragged batch below.)  Long
+// sequences besides: the matrix cores at the clock they hold under load; 1 sequence of
+// 16384 tokens, 8 heads on 2 of 128, forward 529 to 560 us from box to box, 980 to 1040
+// TFLOP/s (a library product 1250), 632 in a run of calls; vector work, 150 instructions and
+// 32 exponentials for 32 products, runs beside the products of the other wave of a
+// SIMD only in part (cores busy 60% of the cycles).  Ragged batches: the tiles on the diagonal,
+// start and end of each workgroup, and the last of them; 8 sequences, 8192 tokens, 16
+// heads on 4 of 128: 61, 88 and 133 us in bf16, 670, 690 and 610 TFLOP/s, cores busy 33 to
+// 38%; 62, 91 and 143 in fp16.  Short sequences: the chain from offsets to keys to products, some
+// 5 us a workgroup (50 sequences, 5000 tokens, 12 heads of 80, fp16: 15, 28 and 28
+// us).  LDS is read without conflicts (with lines turned for 32 banks half of its cycles
+// were).  Tried, no gain: the priority of waves raised for products.  Not tried: softmax
+// of one stage beside the products of the next within a wave, for which 256
+// registers do not hold 128 values a head.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -151,8 +156,8 @@ struct Rows {
   }
   // Sixteen lines from AT bytes behind them on, transposed: in lane 32 h + c,
   // column 32 i + c of lines 4 h .. + 3 and 8 + 4 h .. + 3 (eight lines on, the
-  // turn differs by two chunks).  The wait is in the
-  // statement: as builtins, the compiler would first wait for every load on
+  // turn differs by two chunks).  The reads are builtins, whose waits the compiler
+  // places: for their results, and, before the first of a step, for every load on
   // its way to LDS.
   template <int AT, int N>
   static __device__ __forceinline__ void column(const uint32_t (&p)[N], lm_u32x4 (&f)[N]) {

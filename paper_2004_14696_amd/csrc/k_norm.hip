@@ -19,6 +19,10 @@
 // A branch around the loads of packs behind a row's end made each wait for the
 // one before (gradients 3001 x 1003 17 us for 13); masks of every pack, where only a
 // row's last can need one, filled the registers (16384 x 4090 forward 89 and 165 us).
+// Gradients of the widest rows do not fit them and spill: 4 packs for 16 waves in
+// fp32 (21 registers; 4096 x 16384 240 us, 3.4 TB/s, x 12288 147, 4.1; odd widths 36, x 16383
+// 322 us), 2 packs of 16-bit values in odd widths (19; 8192 x 16380 bf16 315 us, x 16384
+// 199).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
