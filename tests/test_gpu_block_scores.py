@@ -286,3 +286,62 @@ def test_attention_and_its_gradients_where_sums_round(dtype, size, D, lengths, h
     close(lse[clear.t()], lse_ref[clear.t()], e_lse[clear.t()], "lse")
     assert bool((dQ[clear] == 0).all()) and bool((dK[lone] == 0).all())
     close(dV[lone], dV_ref[lone], rounded(dV_ref[lone], dtype), "dV")
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("lengths,heads,kv,D", [([90, 0, 300, 200], 4, 2, 64), ([90, 0, 300, 200], 96, 32, 128)])
+def test_far_sequences_leave_the_others_and_the_rest_as_they_were(dtype, lengths, heads, kv, D):
+    g = gen(50 + D)
+    first, T = 5, sum(lengths) + 11
+    Q, K, V = (normal(g, (T, h, D), dtype) for h in (heads, kv, kv))
+    dO, off = normal(g, (T, heads, D), dtype), offsets_of(lengths, first)
+
+    def run():
+        arrays = [torch.full(x.shape, 7.25, dtype=dtype, device="cuda") for x in (Q, Q, K, V)]
+        lse = torch.full((heads, T), 7.25, device="cuda")
+        O, dQ, dK, dV = arrays                                                                             # noqa: E741
+        pb.attention(Q, K, V, off, out=O, lse=lse)
+        pb.attention_grad(dO, Q, K, V, O, lse, off, dQ=dQ, dK=dK, dV=dV)
+        return [lse.t()] + arrays
+    clean = run()
+    for x in (Q, K, V, dO):
+        x[:first], x[first + sum(lengths):] = float("nan"), float("inf")
+    middle = slice(first + 90, first + 390)
+    Q[middle, :, 0], K[middle, :, 0] = 2048, 4096
+    both = run()
+    assert float(both[0][middle].min()) > 1e5
+    for a, b in zip(clean, both):
+        for rows in (slice(0, first + 90), slice(first + 390, T)):
+            assert torch.equal(a[rows], b[rows])
+        assert bool(torch.isfinite(b.float()).all())
+
+
+def test_attention_captured_with_scores_of_both_kinds():
+    g = gen(60)
+    T, D, heads, kv = 300, 64, 4, 2
+    Q, K, V, dO = (normal(g, (T, h, D), BF16) for h in (heads, kv, kv, heads))
+    off = offsets_of([0, 0, 0])
+
+    def run():
+        O, lse = pb.attention(Q, K, V, off)                                                                # noqa: E741
+        return O, lse, *pb.attention_grad(dO, Q, K, V, O, lse, off)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        run()
+    torch.cuda.current_stream().wait_stream(s)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = run()
+    for i, (lengths, far) in enumerate((([100, 200, 0], False), ([100, 200, 0], True), ([1, 0, 299], False), ([150, 140, 10], True))):
+        for x in (Q, K, V, dO):
+            x.copy_(normal(g, x.shape, BF16))
+        if far:
+            Q[:, :2, 0], K[:, :, 0] = 2048, 4096
+        off.copy_(offsets_of(lengths))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        again = run()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(captured, again)), i
